@@ -1,0 +1,105 @@
+// Plan blobs of include/ssa_evict.h: written by the host planner
+// (ssa_evict_plan.cpp), read unchanged by the kernels.
+//
+//   score plan  [ScoreHeader][ScoreReq x num_reqs][ScoreItem x (the five lists)]
+//   evict plan  [EvictHeader][EvictReq x num_reqs][EvictItem x num_items]
+//
+// A workgroup runs one item for one kv head; a request's fields are copied into
+// its items, so that a workgroup reads one record before it starts.
+#pragma once
+#include <stdint.h>
+
+namespace ssa {
+
+constexpr uint32_t kScoreMagic = 0x31435353u;  // "SSC1"
+constexpr uint32_t kEvictMagic = 0x31565353u;  // "SSV1"
+constexpr int kScoreThreads = 256;             // four waves
+constexpr int kScoreWaveCols = 64;             // stationary columns of a wave (chunk kernels)
+constexpr int kLseMaxKeys = 32768;             // keys of one item of the first chunk pass
+constexpr int kJoinKeys = 1024;                // keys of one item of the decode join
+constexpr int kColsPad = 256;                  // a chunk request's columns are padded to this
+constexpr int kEvictSlots = 64;                // kept keys of one compaction item
+// Columns (row, head in group) of a request: index arithmetic by a 32-bit reciprocal.
+constexpr int64_t kMaxScoreCols = (int64_t)1 << 28;
+
+// The item lists of a score plan, in this order.
+enum ScoreList : int32_t {
+  kListLse = 0,    // chunk requests: log-sum-exp of columns over a key range
+  kListDecode,     // one counted row: logits (and attention) over a key range
+  kListLseJoin,    // log-sum-exps over the pieces of a cut key range
+  kListSum,        // chunk requests: a key tile's weights over all columns
+  kListDecodeJoin, // one counted row: a key range's weights, and the joined attention
+  kNumScoreLists
+};
+
+struct ScoreHeader {
+  uint32_t magic;
+  int32_t last_rows;
+  uint64_t hash;
+  int32_t num_reqs, num_tokens;
+  int32_t hq, hkv, head_dim, page_size, max_pages_per_req, num_pages;
+  float softmax_scale;
+  int32_t max_q_len;
+  int32_t lse_groups, sum_groups;  // column groups (waves side by side) of the chunk kernels
+  int32_t off_items, pad;
+  int32_t count[kNumScoreLists], first[kNumScoreLists];  // items of each list
+  int64_t plan_bytes, ws_bytes;
+};
+static_assert(sizeof(ScoreHeader) == 128, "score header size");
+
+struct ScoreReq {
+  int32_t q_len, ctx_len;
+};
+
+struct ScoreItem {
+  int32_t req;
+  int32_t q_row;    // token row of the first counted row
+  int32_t limit0;   // the last key that row sees
+  int32_t rows;     // counted rows
+  int32_t len;      // keys, u + c
+  int32_t ctx_len;  // u
+  int32_t col0;     // first column (row * G + head in group) of the item
+  int32_t cols_pad; // columns of the request, padded; decode lists: its padded length
+  int32_t key0, key1;
+  int32_t split, nsplit;
+  // float offsets in the workspace for kv head 0:
+  //   chunk lists:   off0 = lse [Hkv][cols_pad], off1 = (m, l) [Hkv][nsplit][cols_pad][2]
+  //   decode lists:  off0 = logits [Hkv][G][cols_pad], off1 = records [Hkv][nsplit][record]
+  int64_t off0, off1;
+};
+static_assert(sizeof(ScoreItem) == 64, "score item size");
+
+// One key range's record of a decode row: m, l and the l of the rounded weights for
+// G heads, padded to four floats, then o [G][D].
+constexpr int score_rec_o(int g) { return (3 * g + 3) / 4 * 4; }
+constexpr int score_rec_floats(int g, int d) { return score_rec_o(g) + g * d; }
+
+struct EvictHeader {
+  uint32_t magic;
+  int32_t sink, recent;
+  int32_t num_reqs;
+  uint64_t hash;
+  int32_t hq, hkv, head_dim, page_size, max_pages_per_req, num_pages;
+  float softmax_scale;
+  int32_t num_items;
+  int32_t off_items, max_len;
+  int64_t num_keep;  // kept keys of one kv head over all requests
+  int64_t plan_bytes, ws_bytes;
+  int64_t pad[5];
+};
+static_assert(sizeof(EvictHeader) == 128, "evict header size");
+
+struct EvictReq {
+  int32_t len, kept;
+  int64_t keep_off;  // n_0 + ... + n_{i-1}
+};
+
+// kept keys slot0 .. slot0 + n - 1 of every kv head of a request that loses keys
+struct EvictItem {
+  int32_t req, slot0, n, len;
+  int32_t kept, pad;
+  int64_t keep_off;
+};
+static_assert(sizeof(EvictItem) == 32, "evict item size");
+
+}  // namespace ssa

@@ -1,0 +1,419 @@
+// Host side of include/ssa_evict.h: argument checks, the score plan and the
+// eviction plan.  Pure host code (no HIP call), so it is testable without a GPU.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "../../include/ssa_evict.h"
+#include "ssa_evict_format.h"
+
+namespace ssa {
+
+int validate_shape(const ssa_shape* s);
+
+namespace {
+
+constexpr int64_t kMaxLen = 1 << 30;
+// Workgroups a launch should have at least: two of four waves run on each of 256
+// compute units, and twice that evens out ranges of different cost.
+constexpr int64_t kFillGroups = 1024;
+// A decode row's key range is cut into pieces of a multiple of 128 keys (one
+// 32-key block for each of four waves), at most kDecodeMaxKeys: a piece costs a
+// record of G (D + 3) floats.
+constexpr int64_t kDecodeStepKeys = 128;
+constexpr int64_t kDecodeMaxKeys = 4096;
+// A piece of a chunk column tile's key range, at least.
+constexpr int64_t kLseMinKeys = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+uint64_t fnv1a(uint64_t h, const void* p, size_t n) {
+  const unsigned char* b = static_cast<const unsigned char*>(p);
+  for (size_t i = 0; i < n; ++i) {
+    h ^= b[i];
+    h *= 1099511628211ull;
+  }
+  return h;
+}
+
+uint64_t hash_shape(const ssa_shape* s, const int32_t* more, int n_more) {
+  uint64_t h = 1469598103934665603ull;
+  const int32_t f[6] = {s->num_q_heads, s->num_kv_heads,     s->head_dim,
+                        s->page_size,   s->num_pages,        s->max_pages_per_req};
+  h = fnv1a(h, f, sizeof f);
+  h = fnv1a(h, &s->softmax_scale, sizeof(float));
+  return fnv1a(h, more, sizeof(int32_t) * n_more);
+}
+
+struct ScorePlan {
+  ScoreHeader hdr;
+  std::vector<ScoreReq> reqs;
+  std::vector<ScoreItem> list[kNumScoreLists];
+};
+
+int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len, int32_t n,
+                int32_t last_rows, ScorePlan* p) {
+  const int rc = validate_shape(s);
+  if (rc) return rc;
+  if (n < 0) return SSA_ERR_LENGTH;
+  if (n > 0 && (!q_len || !ctx_len)) return SSA_ERR_NULL;
+  if (last_rows < 0) return SSA_ERR_ARG;
+  const int hkv = s->num_kv_heads, g = s->num_q_heads / hkv, d = s->head_dim;
+  int64_t tokens = 0, keys = 0, decode_keys = 0, max_q = 0;
+  struct Chunk {
+    int64_t cols, span;
+  };
+  std::vector<Chunk> chunks;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t c = q_len[i], u = ctx_len[i];
+    if (c < 0 || u < 0) return SSA_ERR_LENGTH;
+    tokens += c;
+    keys += c + u;
+    if (tokens > kMaxLen || keys > kMaxLen) return SSA_ERR_LENGTH;
+    if (ceil_div(c + u, SSA_PAGE_SIZE) > s->max_pages_per_req) return SSA_ERR_PAGES;
+    if (c == 0) continue;
+    max_q = std::max(max_q, c);
+    const int64_t r = last_rows ? std::min<int64_t>(c, last_rows) : c;
+    if (r * g > kMaxScoreCols) return SSA_ERR_LENGTH;
+    if (r == 1)
+      decode_keys += c + u;
+    else
+      chunks.push_back({r * g, c + u});
+  }
+  ScoreHeader& h = p->hdr;
+  std::memset(&h, 0, sizeof h);
+
+  // Column groups of the first chunk pass: waves side by side share the keys that
+  // go through LDS, waves one behind the other take different ones.  Four groups
+  // read LDS and cache least; narrow requests fill fewer columns.
+  int64_t waste[3] = {0, 0, 0}, sums[3] = {0, 0, 0};
+  for (const Chunk& c : chunks)
+    for (int k = 0; k < 3; ++k) {
+      const int64_t tile = (int64_t)kScoreWaveCols << k;
+      waste[k] += round_up(c.cols, tile) * c.span * (12 - k) / 10;
+      sums[k] += ceil_div(c.span, tile) * hkv;
+    }
+  int lse_k = 2, sum_k = 2;
+  for (int k = 1; k >= 0; --k)
+    if (waste[k] < waste[lse_k]) lse_k = k;
+  // The second pass: a tile of keys stays in registers, all columns go through LDS.
+  // Narrower tiles where wide ones do not fill the chip.
+  while (sum_k > 0 && sums[sum_k] < kFillGroups / 2) --sum_k;
+  h.lse_groups = 1 << lse_k;
+  h.sum_groups = 1 << sum_k;
+  const int64_t lse_cols = (int64_t)kScoreWaveCols << lse_k, sum_keys = (int64_t)kScoreWaveCols << sum_k;
+  // keys of a piece such that the first pass has about kFillGroups workgroups
+  int64_t tile_keys = 0;
+  for (const Chunk& c : chunks) tile_keys += ceil_div(c.cols, lse_cols) * c.span * hkv;
+  const int64_t piece = std::min<int64_t>(
+      kLseMaxKeys, std::max(kLseMinKeys, round_up(ceil_div(tile_keys, kFillGroups), 128)));
+  const int64_t decode_piece =
+      std::min(kDecodeMaxKeys, std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
+                                                                  kDecodeStepKeys)));
+
+  int64_t ws = 0, row = 0;  // floats; token row
+  auto take = [&](int64_t floats) {
+    const int64_t at = ws;
+    ws += round_up(floats, 64);
+    return at;
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t c = q_len[i], u = ctx_len[i], len = c + u;
+    p->reqs.push_back({q_len[i], ctx_len[i]});
+    if (c == 0) continue;
+    const int64_t r = last_rows ? std::min<int64_t>(c, last_rows) : c;
+    ScoreItem it{};
+    it.req = i;
+    it.q_row = (int32_t)(row + c - r);
+    it.limit0 = (int32_t)(len - r);
+    it.rows = (int32_t)r;
+    it.len = (int32_t)len;
+    it.ctx_len = (int32_t)u;
+    row += c;
+    if (r == 1) {
+      const int64_t padded = round_up(len, 32);
+      it.cols_pad = (int32_t)padded;
+      it.nsplit = (int32_t)ceil_div(len, decode_piece);
+      it.off0 = take(padded * g * hkv);
+      it.off1 = take((int64_t)hkv * it.nsplit * score_rec_floats(g, d));
+      for (int32_t k = 0; k < it.nsplit; ++k) {
+        ScoreItem x = it;
+        x.split = k;
+        x.key0 = (int32_t)(k * decode_piece);
+        x.key1 = (int32_t)std::min(len, (k + 1) * decode_piece);
+        p->list[kListDecode].push_back(x);
+      }
+      for (int64_t k = 0; k < len; k += kJoinKeys) {
+        ScoreItem x = it;
+        x.key0 = (int32_t)k;
+        x.key1 = (int32_t)std::min(len, k + kJoinKeys);
+        p->list[kListDecodeJoin].push_back(x);
+      }
+      continue;
+    }
+    const int64_t cols = r * g, padded = round_up(cols, kColsPad);
+    it.cols_pad = (int32_t)padded;
+    it.nsplit = (int32_t)ceil_div(len, piece);
+    it.off0 = take(padded * hkv);
+    it.off1 = it.nsplit > 1 ? take(padded * hkv * it.nsplit * 2) : 0;
+    for (int64_t col = 0; col < cols; col += lse_cols)
+      for (int32_t k = 0; k < it.nsplit; ++k) {
+        ScoreItem x = it;
+        x.col0 = (int32_t)col;
+        x.split = k;
+        x.key0 = (int32_t)(k * piece);
+        x.key1 = (int32_t)std::min(len, (k + 1) * piece);
+        p->list[kListLse].push_back(x);
+      }
+    if (it.nsplit > 1)
+      for (int64_t col = 0; col < padded; col += kScoreThreads) {
+        ScoreItem x = it;
+        x.col0 = (int32_t)col;
+        p->list[kListLseJoin].push_back(x);
+      }
+    for (int64_t k = 0; k < len; k += sum_keys) {
+      ScoreItem x = it;
+      x.key0 = (int32_t)k;
+      x.key1 = (int32_t)std::min(len, k + sum_keys);
+      p->list[kListSum].push_back(x);
+    }
+  }
+  h.magic = kScoreMagic;
+  h.last_rows = last_rows;
+  h.num_reqs = n;
+  h.num_tokens = (int32_t)tokens;
+  h.hq = s->num_q_heads;
+  h.hkv = hkv;
+  h.head_dim = d;
+  h.page_size = s->page_size;
+  h.max_pages_per_req = s->max_pages_per_req;
+  h.num_pages = s->num_pages;
+  h.softmax_scale = s->softmax_scale;
+  h.max_q_len = (int32_t)max_q;
+  int64_t off = sizeof(ScoreHeader) + (int64_t)sizeof(ScoreReq) * n;
+  off = round_up(off, 64);
+  h.off_items = (int32_t)std::min<int64_t>(off, INT32_MAX);
+  int64_t items = 0;
+  for (int l = 0; l < kNumScoreLists; ++l) {
+    const int64_t count = (int64_t)p->list[l].size();
+    if (items + count > INT32_MAX || count * hkv > INT32_MAX) return SSA_ERR_LENGTH;
+    h.first[l] = (int32_t)items;
+    h.count[l] = (int32_t)count;
+    items += count;
+  }
+  h.plan_bytes = off + items * (int64_t)sizeof(ScoreItem);
+  if (h.plan_bytes > INT32_MAX) return SSA_ERR_LENGTH;
+  h.ws_bytes = std::max<int64_t>(256, ws * 4);
+  uint64_t hv = hash_shape(s, &last_rows, 1);
+  if (n > 0) {
+    hv = fnv1a(hv, q_len, sizeof(int32_t) * n);
+    hv = fnv1a(hv, ctx_len, sizeof(int32_t) * n);
+  }
+  // how the lists are cut is this planner's own
+  const int64_t cut[4] = {items, h.ws_bytes, h.lse_groups, h.sum_groups};
+  h.hash = fnv1a(hv, cut, sizeof cut);
+  return SSA_OK;
+}
+
+struct EvictPlan {
+  EvictHeader hdr;
+  std::vector<EvictReq> reqs;
+  std::vector<EvictItem> items;
+};
+
+int build_evict(const ssa_shape* s, const int32_t* kv_len, const int32_t* budget, int32_t n,
+                int32_t sink, int32_t recent, EvictPlan* p) {
+  const int rc = validate_shape(s);
+  if (rc) return rc;
+  if (n < 0) return SSA_ERR_LENGTH;
+  if (n > 0 && (!kv_len || !budget)) return SSA_ERR_NULL;
+  if (sink < 0 || recent < 0) return SSA_ERR_ARG;
+  EvictHeader& h = p->hdr;
+  std::memset(&h, 0, sizeof h);
+  int64_t keys = 0, keep = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t len = kv_len[i], kept = std::min(kv_len[i], budget[i]);
+    if (len < 0 || budget[i] < 0) return SSA_ERR_LENGTH;
+    keys += len;
+    if (keys > kMaxLen) return SSA_ERR_LENGTH;
+    if (ceil_div(len, SSA_PAGE_SIZE) > s->max_pages_per_req) return SSA_ERR_PAGES;
+    if (kept < len && (int64_t)sink + recent > kept) return SSA_ERR_ARG;
+    p->reqs.push_back({(int32_t)len, (int32_t)kept, keep});
+    if (kept < len)
+      for (int64_t k = 0; k < kept; k += kEvictSlots)
+        p->items.push_back({i, (int32_t)k, (int32_t)std::min<int64_t>(kEvictSlots, kept - k),
+                            (int32_t)len, (int32_t)kept, 0, keep});
+    keep += kept;
+    h.max_len = std::max(h.max_len, (int32_t)len);
+  }
+  h.magic = kEvictMagic;
+  h.sink = sink;
+  h.recent = recent;
+  h.num_reqs = n;
+  h.hq = s->num_q_heads;
+  h.hkv = s->num_kv_heads;
+  h.head_dim = s->head_dim;
+  h.page_size = s->page_size;
+  h.max_pages_per_req = s->max_pages_per_req;
+  h.num_pages = s->num_pages;
+  h.softmax_scale = s->softmax_scale;
+  h.num_keep = keep;
+  const int64_t items = (int64_t)p->items.size();
+  const int64_t off = sizeof(EvictHeader) + (int64_t)sizeof(EvictReq) * n;
+  h.plan_bytes = off + items * (int64_t)sizeof(EvictItem);
+  if (h.plan_bytes > INT32_MAX || items * h.hkv > INT32_MAX || (int64_t)n * h.hkv > INT32_MAX)
+    return SSA_ERR_LENGTH;
+  h.num_items = (int32_t)items;
+  h.off_items = (int32_t)off;
+  h.ws_bytes = 256;
+  const int32_t more[2] = {sink, recent};
+  uint64_t hv = hash_shape(s, more, 2);
+  if (n > 0) {
+    hv = fnv1a(hv, kv_len, sizeof(int32_t) * n);
+    hv = fnv1a(hv, budget, sizeof(int32_t) * n);
+  }
+  const int64_t cut[2] = {items, h.ws_bytes};
+  h.hash = fnv1a(hv, cut, sizeof cut);
+  return SSA_OK;
+}
+
+template <class H>
+int check_header(const ssa_shape* s, const void* plan_host, uint32_t magic, const H** out) {
+  const int rc = validate_shape(s);
+  if (rc) return rc;
+  if (!plan_host) return SSA_ERR_NULL;
+  const H* h = static_cast<const H*>(plan_host);
+  if (h->magic != magic || h->hq != s->num_q_heads || h->hkv != s->num_kv_heads ||
+      h->head_dim != s->head_dim || h->page_size != s->page_size ||
+      h->num_pages != s->num_pages || h->max_pages_per_req != s->max_pages_per_req ||
+      std::memcmp(&h->softmax_scale, &s->softmax_scale, sizeof(float)) != 0)
+    return SSA_ERR_PLAN_MISMATCH;
+  *out = h;
+  return SSA_OK;
+}
+
+}  // namespace
+
+// Check that plan_host is a plan of its kind for this shape; used by the launchers.
+int check_score_plan(const ssa_shape* s, const void* plan_host, const ScoreHeader** out) {
+  return check_header(s, plan_host, kScoreMagic, out);
+}
+int check_evict_plan(const ssa_shape* s, const void* plan_host, const EvictHeader** out) {
+  return check_header(s, plan_host, kEvictMagic, out);
+}
+
+}  // namespace ssa
+
+extern "C" {
+
+int ssa_score_plan_size(const ssa_shape* shape, const int32_t* q_len_host,
+                        const int32_t* ctx_len_host, int32_t num_reqs, int32_t last_rows,
+                        size_t* plan_bytes, size_t* ws_bytes) {
+  if (!plan_bytes || !ws_bytes) return SSA_ERR_NULL;
+  try {
+    ssa::ScorePlan p;
+    const int rc = ssa::build_score(shape, q_len_host, ctx_len_host, num_reqs, last_rows, &p);
+    if (rc) return rc;
+    *plan_bytes = (size_t)p.hdr.plan_bytes;
+    *ws_bytes = (size_t)p.hdr.ws_bytes;
+    return SSA_OK;
+  } catch (const std::bad_alloc&) {
+    return SSA_ERR_LENGTH;
+  }
+}
+
+int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int32_t* ctx_len_host,
+                   int32_t num_reqs, int32_t last_rows, void* plan_host, size_t plan_bytes) {
+  if (!plan_host) return SSA_ERR_NULL;
+  try {
+    ssa::ScorePlan p;
+    const int rc = ssa::build_score(shape, q_len_host, ctx_len_host, num_reqs, last_rows, &p);
+    if (rc) return rc;
+    if (plan_bytes < (size_t)p.hdr.plan_bytes) return SSA_ERR_PLAN_SIZE;
+    char* b = static_cast<char*>(plan_host);
+    std::memcpy(b, &p.hdr, sizeof p.hdr);
+    if (!p.reqs.empty())
+      std::memcpy(b + sizeof p.hdr, p.reqs.data(), sizeof(ssa::ScoreReq) * p.reqs.size());
+    char* at = b + p.hdr.off_items;
+    for (const auto& l : p.list) {
+      if (!l.empty()) std::memcpy(at, l.data(), sizeof(ssa::ScoreItem) * l.size());
+      at += sizeof(ssa::ScoreItem) * l.size();
+    }
+    return SSA_OK;
+  } catch (const std::bad_alloc&) {
+    return SSA_ERR_LENGTH;
+  }
+}
+
+int ssa_evict_plan_size(const ssa_shape* shape, const int32_t* kv_len_host,
+                        const int32_t* budget_host, int32_t num_reqs, int32_t sink,
+                        int32_t recent, size_t* plan_bytes, size_t* ws_bytes) {
+  if (!plan_bytes || !ws_bytes) return SSA_ERR_NULL;
+  try {
+    ssa::EvictPlan p;
+    const int rc = ssa::build_evict(shape, kv_len_host, budget_host, num_reqs, sink, recent, &p);
+    if (rc) return rc;
+    *plan_bytes = (size_t)p.hdr.plan_bytes;
+    *ws_bytes = (size_t)p.hdr.ws_bytes;
+    return SSA_OK;
+  } catch (const std::bad_alloc&) {
+    return SSA_ERR_LENGTH;
+  }
+}
+
+int ssa_evict_plan(const ssa_shape* shape, const int32_t* kv_len_host, const int32_t* budget_host,
+                   int32_t num_reqs, int32_t sink, int32_t recent, void* plan_host,
+                   size_t plan_bytes) {
+  if (!plan_host) return SSA_ERR_NULL;
+  try {
+    ssa::EvictPlan p;
+    const int rc = ssa::build_evict(shape, kv_len_host, budget_host, num_reqs, sink, recent, &p);
+    if (rc) return rc;
+    if (plan_bytes < (size_t)p.hdr.plan_bytes) return SSA_ERR_PLAN_SIZE;
+    char* b = static_cast<char*>(plan_host);
+    std::memcpy(b, &p.hdr, sizeof p.hdr);
+    if (!p.reqs.empty())
+      std::memcpy(b + sizeof p.hdr, p.reqs.data(), sizeof(ssa::EvictReq) * p.reqs.size());
+    if (!p.items.empty())
+      std::memcpy(b + p.hdr.off_items, p.items.data(), sizeof(ssa::EvictItem) * p.items.size());
+    return SSA_OK;
+  } catch (const std::bad_alloc&) {
+    return SSA_ERR_LENGTH;
+  }
+}
+
+int ssa_check_evict_tables(const ssa_shape* shape, const void* plan_host,
+                           const int32_t* block_table_host, const int32_t* new_table_host) {
+  const ssa::EvictHeader* h = nullptr;
+  const int rc = ssa::check_evict_plan(shape, plan_host, &h);
+  if (rc) return rc;
+  if (h->num_reqs > 0 && !block_table_host) return SSA_ERR_NULL;
+  const ssa::EvictReq* reqs = reinterpret_cast<const ssa::EvictReq*>(
+      static_cast<const char*>(plan_host) + sizeof(ssa::EvictHeader));
+  try {
+    std::vector<bool> taken((size_t)h->num_pages, false);
+    for (int32_t i = 0; i < h->num_reqs; ++i) {
+      const int32_t* row = block_table_host + (size_t)i * h->max_pages_per_req;
+      for (int64_t k = 0; k < ssa::ceil_div(reqs[i].len, SSA_PAGE_SIZE); ++k) {
+        if (row[k] < 0 || row[k] >= h->num_pages) return SSA_ERR_PAGES;
+        taken[row[k]] = true;
+      }
+    }
+    for (int32_t i = 0; new_table_host && i < h->num_reqs; ++i) {
+      if (reqs[i].kept == reqs[i].len) continue;
+      const int32_t* row = new_table_host + (size_t)i * h->max_pages_per_req;
+      for (int64_t k = 0; k < ssa::ceil_div(reqs[i].kept, SSA_PAGE_SIZE); ++k) {
+        if (row[k] < 0 || row[k] >= h->num_pages || taken[row[k]]) return SSA_ERR_PAGES;
+        taken[row[k]] = true;
+      }
+    }
+    return SSA_OK;
+  } catch (const std::bad_alloc&) {
+    return SSA_ERR_LENGTH;
+  }
+}
+
+}  // extern "C"

@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/ssa_evict.h"
 #include "../../include/ssa_layer.h"
 #include "ssa_device.h"
 #include "ssa_plan_format.h"
@@ -59,6 +60,8 @@ struct RopeArgs {
   int hq, hkv, maxp;
   int grouped_segs;  // segments run by head groups; the others are single rows
   int workgroups;
+  const int32_t* shift;  // position minus cache index of each request, or null (all zero)
+  int max_position;
 };
 
 // Heads per workgroup of a grouped segment: group y < rot_groups rotates
@@ -100,6 +103,10 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
   const int n = sg.n, slot0 = sg.pos0 % 16, tid = threadIdx.x;
   const size_t stride = (size_t)(a.hq + 2 * a.hkv) * D;
   const size_t pb = (size_t)a.bt[(size_t)sg.req * a.maxp + sg.pos0 / 16] * a.hkv * 16 * D;
+  // the table's row of the segment's first position; the host has checked its own
+  // copy of the shifts, and the bound keeps another one inside the table
+  int at0 = sg.pos0;
+  if (a.shift) at0 = max(0, min(at0 + a.shift[sg.req], a.max_position - n));
   if (single) {
     // one row: its value heads' chunks (slot by slot into the dim-major page)
     // and every query and key head's units, all loads first
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
       if (idx < nu) {
         const int h = idx / UPH, i = (idx % UPH) * 8;
         u32x4 o1, o2;
-        rotate8(x1[j], x2[j], a.cos_sin + (size_t)sg.pos0 * D, HALF, i, &o1, &o2);
+        rotate8(x1[j], x2[j], a.cos_sin + (size_t)at0 * D, HALF, i, &o1, &o2);
         uint16_t* dst = h < a.hq ? a.q_out + ((size_t)sg.row0 * a.hq + h) * D
                                  : a.kc + pb + (size_t)(h - a.hq) * 16 * D + (size_t)slot0 * D;
         st16(dst + i, o1);
@@ -162,7 +169,7 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
       const int r = idx / (nh * UPH), rem = idx % (nh * UPH);
       const int h = h0 + rem / UPH, i = (rem % UPH) * 8;
       u32x4 o1, o2;
-      rotate8(x1[j], x2[j], a.cos_sin + (size_t)(sg.pos0 + r) * D, HALF, i, &o1, &o2);
+      rotate8(x1[j], x2[j], a.cos_sin + (size_t)(at0 + r) * D, HALF, i, &o1, &o2);
       uint16_t* dst = h < a.hq ? a.q_out + ((size_t)(sg.row0 + r) * a.hq + h) * D
                                : a.kc + pb + (size_t)(h - a.hq) * 16 * D + (size_t)(slot0 + r) * D;
       st16(dst + i, o1);
@@ -216,21 +223,23 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
 
 }  // namespace
 
-extern "C" {
+namespace {
 
-int ssa_rope_append(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
-                    const uint16_t* qkv, const float* cos_sin, int32_t max_position,
-                    uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
-                    const int32_t* block_table, void* stream) {
+int rope_append(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                const uint16_t* qkv, const float* cos_sin, int32_t max_position,
+                const int32_t* shift_host, const int32_t* shift_dev, uint16_t* q_out,
+                uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table, void* stream) {
   const PlanHeader* h = nullptr;
   int rc = check_plan(shape, plan_host, &h);
   if (rc) return rc;
   if (!plan_dev) return SSA_ERR_NULL;
   const ReqEntry* reqs = reinterpret_cast<const ReqEntry*>(
       static_cast<const uint8_t*>(plan_host) + h->off_reqs);
-  for (int32_t i = 0; i < h->num_reqs; ++i)
-    if (reqs[i].q_len > 0 && (int64_t)reqs[i].ctx_len + reqs[i].q_len > max_position)
-      return SSA_ERR_ARG;
+  for (int32_t i = 0; i < h->num_reqs; ++i) {
+    if (reqs[i].q_len <= 0) continue;
+    const int64_t shift = shift_host ? shift_host[i] : 0;
+    if (shift < 0 || shift + reqs[i].ctx_len + reqs[i].q_len > max_position) return SSA_ERR_ARG;
+  }
   if (h->num_segments == 0) return SSA_OK;
   if (!qkv || !cos_sin || !q_out || !k_cache || !v_cache || !block_table) return SSA_ERR_NULL;
   (void)hipGetLastError();
@@ -244,7 +253,7 @@ int ssa_rope_append(const ssa_shape* shape, const void* plan_host, const void* p
   if (wgs > INT32_MAX) return SSA_ERR_ARG;
   RopeArgs a{static_cast<const uint8_t*>(plan_dev), h->hash, h->off_segments, qkv, cos_sin,
              q_out, k_cache, v_cache, block_table, h->hq, h->hkv, h->max_pages_per_req, grouped,
-             (int32_t)wgs};
+             (int32_t)wgs, shift_dev, max_position};
   const dim3 grid(wgs < kGridRow ? wgs : kGridRow, (wgs + kGridRow - 1) / kGridRow);
   if (h->head_dim == 128)
     hipLaunchKernelGGL(rope_append_kernel<128>, grid, dim3(kLayerThreads), 0,
@@ -253,6 +262,28 @@ int ssa_rope_append(const ssa_shape* shape, const void* plan_host, const void* p
     hipLaunchKernelGGL(rope_append_kernel<64>, grid, dim3(kLayerThreads), 0,
                        static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ssa_rope_append(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                    const uint16_t* qkv, const float* cos_sin, int32_t max_position,
+                    uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
+                    const int32_t* block_table, void* stream) {
+  return rope_append(shape, plan_host, plan_dev, qkv, cos_sin, max_position, nullptr, nullptr,
+                     q_out, k_cache, v_cache, block_table, stream);
+}
+
+int ssa_rope_append_shifted(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                            const uint16_t* qkv, const float* cos_sin, int32_t max_position,
+                            const int32_t* shift_host, const int32_t* shift_dev, uint16_t* q_out,
+                            uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
+                            void* stream) {
+  if (!shift_host || !shift_dev) return SSA_ERR_NULL;
+  return rope_append(shape, plan_host, plan_dev, qkv, cos_sin, max_position, shift_host, shift_dev,
+                     q_out, k_cache, v_cache, block_table, stream);
 }
 
 }  // extern "C"

@@ -839,6 +839,9 @@ int build(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len, int3
 
 }  // namespace
 
+// The shape checks of every entry point, for the other planners.
+int validate_shape(const ssa_shape* s) { return check_shape(s); }
+
 // Check that plan_host is a plan built for this shape; used by the launchers.
 int check_plan(const ssa_shape* s, const void* plan_host, const PlanHeader** out) {
   int rc = check_shape(s);

@@ -1,0 +1,747 @@
+// HIP kernels for gfx950 of ssa_key_scores and ssa_decode_scored
+// (include/ssa_evict.h): the attention weights of a batch, summed per key.
+//
+// With t = scale log2(e) <q, k>, row j's weight on key t is 2^(t - L_j), L_j the
+// log2 of the sum of 2^t over the keys that it sees.  A key's score is a sum over
+// rows, and L_j a sum over keys, so the weights need L first:
+//
+//   one counted row   The logits are few (Hq per key, against 2 D bytes of K per
+//                     kv head): a first pass reads K, writes the logits (fp32)
+//                     and each key range's maximum and sum; a second joins those
+//                     and turns logits into weights.  K is read once.  With the
+//                     attention output wanted, the first pass also reads V.
+//   several rows      The logits do not fit; K goes through the matrix cores
+//                     twice.  First pass: 64 columns (row, head) a wave stay in
+//                     registers, keys stream through LDS, and every lane keeps a
+//                     running maximum and sum of its two columns.  Second pass:
+//                     64 keys a wave stay in registers, the columns and their L
+//                     stream through LDS, and every lane sums the weights of its
+//                     two keys.  A key belongs to one workgroup: no atomics.
+//
+// Rows stream into LDS with their 16-byte pieces permuted within the row (piece c
+// of row r lies at c ^ r), so that the 32 rows of a fragment read hit all banks.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "../../include/ssa_evict.h"
+#include "ssa_device.h"
+#include "ssa_evict_format.h"
+
+namespace ssa {
+int check_score_plan(const ssa_shape* s, const void* plan_host, const ScoreHeader** out);
+}
+
+namespace {
+using namespace ssa;
+using namespace ssa_dev;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct ScoreArgs {
+  const uint8_t* plan;
+  uint64_t hash;
+  int64_t off_items;  // byte offset of the list's first item
+  int32_t workgroups;
+  int32_t hq, hkv, g, maxp;
+  uint32_t g_magic;  // ceil(2^32 / g)
+  float c;           // softmax scale times log2(e)
+  float decay;
+  const uint16_t* q;
+  const uint16_t* kc;
+  const uint16_t* vc;
+  const int32_t* bt;
+  const float* scores_in;
+  float* scores_out;
+  uint16_t* out;
+  float* ws;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// x < 2^28 over g <= 16
+__device__ __forceinline__ int div_g(const ScoreArgs& a, int x) {
+  return a.g == 1 ? x : (int)__umulhi((uint32_t)x, a.g_magic);
+}
+
+// The workgroup's item and kv head; false: nothing to do (past the grid's end, or
+// another plan than the host's lies at plan_dev).
+__device__ __forceinline__ bool take_item(const ScoreArgs& a, const ScoreItem** item, int* kvh) {
+  const int wg = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  if (wg >= a.workgroups) return false;
+  *kvh = wg % a.hkv;
+  *item = reinterpret_cast<const ScoreItem*>(a.plan + a.off_items) + wg / a.hkv;
+  const ScoreHeader* h = reinterpret_cast<const ScoreHeader*>(a.plan);
+  return h->magic == kScoreMagic && h->hash == a.hash;
+}
+
+// Four keys' new scores (keys k0 .. k0 + 3 of one page); w: their weights.
+__device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem& it, int kvh, int k0,
+                                            int key1, f32x4 w) {
+  const int page = a.bt[(size_t)it.req * a.maxp + k0 / 16];
+  const size_t at = ((size_t)page * a.hkv + kvh) * 16 + k0 % 16;
+  if (k0 + 4 <= key1) {
+    if (a.scores_in && k0 + 4 <= it.ctx_len) {
+      const f32x4 old = *reinterpret_cast<const f32x4*>(a.scores_in + at);
+      w += old * a.decay;
+    } else if (a.scores_in) {
+      for (int i = 0; i < 4; ++i)
+        if (k0 + i < it.ctx_len) w[i] += a.scores_in[at + i] * a.decay;
+    }
+    *reinterpret_cast<f32x4*>(a.scores_out + at) = w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (k0 + i < key1) {
+      float x = w[i];
+      if (a.scores_in && k0 + i < it.ctx_len) x += a.scores_in[at + i] * a.decay;
+      a.scores_out[at + i] = x;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// One counted row: logits over a key range.
+//
+// Each wave takes every fourth 32-key block (two pages).  S^T = K Q^T in 16x16
+// tiles: the A rows of the two tiles are dealt so that a lane ends up with 8
+// consecutive keys of one column (head), which is also the layout of the B operand
+// of the P V product: no data moves between lanes but the block's maximum.
+template <int D, bool OUT>
+__global__ __launch_bounds__(kScoreThreads, OUT ? 3 : 4) void score_decode_kernel(ScoreArgs a) {
+  constexpr int KS = D / 32, DT = D / 16;
+  __shared__ float s_ml[3][4][16];
+  __shared__ __attribute__((aligned(16))) float s_o[OUT ? 4 * 16 * D : 4];
+  const ScoreItem* itp;
+  int kvh;
+  if (!take_item(a, &itp, &kvh)) return;
+  const ScoreItem it = *itp;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, quad = lane >> 4;
+  const int32_t* row = a.bt + (size_t)it.req * a.maxp;
+  const int last_page = (it.len - 1) / 16;
+
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    u32x4 v = {0, 0, 0, 0};
+    if (r16 < a.g)
+      v = ld16(a.q + ((size_t)it.q_row * a.hq + kvh * a.g + r16) * D + s * 32 + quad * 8);
+    qf[s] = as_bf16x8(v);
+  }
+  float* logits = a.ws + it.off0 + ((int64_t)kvh * a.g + r16) * it.cols_pad + 8 * quad;
+  float m = -kInf, l = 0.f, lr = 0.f;
+  f32x4 o[OUT ? DT : 1];
+#pragma unroll
+  for (int t = 0; t < (OUT ? DT : 1); ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int slot0 = 8 * ((r16 >> 2) & 1) + (r16 & 3);
+  for (int kb = it.key0 + wave * 32; kb < it.key1; kb += 128) {
+    const int p0 = row[kb / 16], p1 = row[min(kb / 16 + 1, last_page)];
+    const uint16_t* kp =
+        a.kc + ((size_t)(r16 >> 3 ? p1 : p0) * a.hkv + kvh) * 16 * D + slot0 * D + quad * 8;
+    u32x4 kf[2][KS], vf[OUT ? DT : 1];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) kf[t][s] = ld16(kp + t * 4 * D + s * 32);
+    if constexpr (OUT) {
+      const uint16_t* vp =
+          a.vc + ((size_t)(quad >> 1 ? p1 : p0) * a.hkv + kvh) * 16 * D + r16 * 16 + 8 * (quad & 1);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) vf[t] = ld16(vp + t * 256);
+    }
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      s0 = mfma(as_bf16x8(kf[0][s]), qf[s], s0);
+      s1 = mfma(as_bf16x8(kf[1][s]), qf[s], s1);
+    }
+    float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+    if (r16 < a.g) {
+      float* to = logits + kb;
+      *reinterpret_cast<f32x4*>(to) = s0;
+      *reinterpret_cast<f32x4*>(to + 4) = s1;
+    }
+    const int nv = it.key1 - kb - 8 * quad;  // this lane's keys that exist
+    if (kb + 32 > it.key1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= nv) x[i] = -kInf;
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mn = mx == -kInf ? m : fmaxf(m, mx * a.c);
+    const float ms = mn == -kInf ? 0.f : mn;
+    const float alpha = exp2_fast(m - ms);
+    float p[8], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = exp2_fast(__builtin_fmaf(x[i], a.c, -ms));
+    if (kb + 32 > it.key1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= nv) p[i] = 0.f;  // scale 0 times -inf is NaN
+    }
+    sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    l = l * alpha + sum;
+    m = mn;
+    if constexpr (OUT) {
+      // The weights are rounded to bf16 for the matrix product, and the output is
+      // divided by the sum of the rounded ones: the weights applied add up to 1.
+      u32x4 pk;
+      float rs = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        pk[w] = pack2(p[2 * w], p[2 * w + 1]);
+        rs += bf16_lo(pk[w]) + bf16_hi(pk[w]);
+      }
+      lr = lr * alpha + rs;
+      if (__any(alpha != 1.f)) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] *= alpha;
+      }
+      if (kb + 32 > it.key1) {
+        // a slot past the last key may hold anything, and 0 times NaN is NaN
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            if (2 * w >= nv) vf[t][w] = 0;
+            else if (2 * w + 1 >= nv) vf[t][w] &= 0xFFFFu;
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(pk), o[t]);
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  lr += __shfl_xor(lr, 16, 64);
+  lr += __shfl_xor(lr, 32, 64);
+  if (quad == 0) {
+    s_ml[0][wave][r16] = m;
+    s_ml[1][wave][r16] = l;
+    s_ml[2][wave][r16] = lr;
+  }
+  if constexpr (OUT) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      *reinterpret_cast<f32x4*>(s_o + (wave * 16 + r16) * D + t * 16 + 4 * quad) = o[t];
+  }
+  __syncthreads();
+  float* rec = a.ws + it.off1 + ((int64_t)kvh * it.nsplit + it.split) * score_rec_floats(a.g, D);
+  if (tid < a.g) {
+    float mm = -kInf, ll = 0.f, rr = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[0][w][tid]);
+    const float ms = mm == -kInf ? 0.f : mm;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(s_ml[0][w][tid] - ms);
+      ll += s_ml[1][w][tid] * f;
+      rr += s_ml[2][w][tid] * f;
+    }
+    rec[tid] = mm;
+    rec[a.g + tid] = ll;
+    rec[2 * a.g + tid] = rr;
+  }
+  if constexpr (OUT) {
+    float* ro = rec + score_rec_o(a.g);
+    for (int e = tid * 4; e < a.g * D; e += kScoreThreads * 4) {
+      const int g = e / D, d = e % D;
+      float mm = -kInf;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[0][w][g]);
+      const float ms = mm == -kInf ? 0.f : mm;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        v += *reinterpret_cast<const f32x4*>(s_o + (w * 16 + g) * D + d) *
+             exp2_fast(s_ml[0][w][g] - ms);
+      *reinterpret_cast<f32x4*>(ro + e) = v;
+    }
+  }
+}
+
+// One counted row: join the key ranges' sums, turn a range's logits into scores;
+// the first range's workgroup also joins the attention output.
+template <int D, bool OUT>
+__global__ __launch_bounds__(kScoreThreads) void score_decode_join_kernel(ScoreArgs a) {
+  __shared__ float s_m[16], s_inv[16], s_inv_r[16];
+  const ScoreItem* itp;
+  int kvh;
+  if (!take_item(a, &itp, &kvh)) return;
+  const ScoreItem it = *itp;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int stride = score_rec_floats(a.g, D);
+  const float* recs = a.ws + it.off1 + (int64_t)kvh * it.nsplit * stride;
+  for (int g = wave; g < a.g; g += 4) {
+    float m = -kInf;
+    for (int s = lane; s < it.nsplit; s += 64) m = fmaxf(m, recs[(int64_t)s * stride + g]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+    const float ms = m == -kInf ? 0.f : m;
+    float l = 0.f, lr = 0.f;
+    for (int s = lane; s < it.nsplit; s += 64) {
+      const float* r = recs + (int64_t)s * stride;
+      const float f = exp2_fast(r[g] - ms);
+      l += r[a.g + g] * f;
+      lr += r[2 * a.g + g] * f;
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) {
+      l += __shfl_xor(l, x, 64);
+      lr += __shfl_xor(lr, x, 64);
+    }
+    if (lane == 0) {
+      s_m[g] = ms;
+      s_inv[g] = 1.f / l;
+      s_inv_r[g] = 1.f / lr;
+    }
+  }
+  __syncthreads();
+  const int k0 = it.key0 + tid * 4;
+  if (k0 < it.key1) {
+    const float* lg = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + k0;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < a.g; ++g) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lg + (int64_t)g * it.cols_pad);
+      const float m = s_m[g], inv = s_inv[g];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(x[i], a.c, -m)) * inv;
+    }
+    add_scores4(a, it, kvh, k0, it.key1, w);
+  }
+  if constexpr (OUT) {
+    if (it.key0 == 0) {
+      for (int e = tid * 4; e < a.g * D; e += kScoreThreads * 4) {
+        const int g = e / D, d = e % D;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < it.nsplit; ++s) {
+          const float* r = recs + (int64_t)s * stride;
+          v += *reinterpret_cast<const f32x4*>(r + score_rec_o(a.g) + e) * exp2_fast(r[g] - s_m[g]);
+        }
+        v *= s_inv_r[g];
+        u32x2 b = {pack2(v[0], v[1]), pack2(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + d) = b;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Several rows: both passes.  A wave holds 64 stationary vectors (columns in the
+// first pass, keys in the second) as B operands of the 32x32x16 product and runs
+// the streamed rows (keys, columns) past them in 32-row tiles; NC waves lie side
+// by side over the same rows, 4 / NC one behind the other.  Lane n of a 32x32
+// result owns stationary vector n % 32 and, of the tile, the 16 rows
+// (r & 3) + 8 (r >> 2) + 4 (n / 32): sums over rows stay in the lane to the end.
+__device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+}
+
+template <int D, int NC>
+struct ChunkCfg {
+  static constexpr int RG = 4 / NC;             // row groups
+  static constexpr int ROWS = 32 * RG;          // streamed rows of a stage
+  static constexpr int ROWB = D * 2;
+  static constexpr int CPR = D / 8;             // 16-byte pieces of a row
+  static constexpr int STAGE = ROWS * ROWB;
+  static constexpr int NB = NC == 1 ? 2 : 3;    // stages in LDS
+  static constexpr int LOADS = ROWS * CPR / kScoreThreads;  // copies of a wave per stage
+  static constexpr int KS = D / 16;
+  static constexpr int COLS = kScoreWaveCols * NC;  // stationary vectors of a workgroup
+};
+
+// Issue one stage's copies: `src(row)` is the address of streamed row `row`.
+template <class C, class F>
+__device__ __forceinline__ void stage_rows(const char* buf, int wave, int lane, F src) {
+#pragma unroll
+  for (int i = 0; i < C::LOADS; ++i) {
+    const int p = (wave * C::LOADS + i) * 64 + lane;
+    const int row = p / C::CPR, piece = p % C::CPR;
+    dma16(src(row) + (piece ^ (row & (C::CPR - 1))) * 8, buf + (wave * C::LOADS + i) * 1024);
+  }
+}
+
+template <int D, int NC>
+__device__ __forceinline__ void tile_products(const char* buf, int rg, int lane,
+                                              const bf16x8 (*st)[D / 16], f32x16* acc) {
+  using C = ChunkCfg<D, NC>;
+  const int half = lane >> 5;
+  const char* at = buf + (rg * 32 + (lane & 31)) * C::ROWB;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < C::KS; ++s) {
+    const bf16x8 x = as_bf16x8(ld16(at + ((2 * s + half) ^ (lane & (C::CPR - 1))) * 16));
+    acc[0] = mfma32(x, st[0][s], acc[0]);
+    acc[1] = mfma32(x, st[1][s], acc[1]);
+  }
+}
+
+template <int D, int NC>
+__global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(ScoreArgs a) {
+  using C = ChunkCfg<D, NC>;
+  __shared__ __attribute__((aligned(16))) char s_buf[C::NB * C::STAGE];
+  __shared__ int s_pages[kLseMaxKeys / 16];
+  __shared__ float s_m[C::RG][C::COLS], s_l[C::RG][C::COLS];
+  const ScoreItem* itp;
+  int kvh;
+  if (!take_item(a, &itp, &kvh)) return;
+  const ScoreItem it = *itp;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = wave % NC, rg = wave / NC, half = lane >> 5;
+  const int ncols = it.rows * a.g;
+  const int first_limit = it.limit0 + div_g(a, it.col0);
+  const int last_limit = it.limit0 + div_g(a, min(it.col0 + C::COLS, ncols) - 1);
+  const int kend = min(it.key1, last_limit + 1);  // keys past it are seen by no column
+
+  for (int i = tid; i < (kend - it.key0 + 15) / 16; i += kScoreThreads)
+    s_pages[i] = a.bt[(size_t)it.req * a.maxp + it.key0 / 16 + i];
+  bf16x8 st[2][C::KS];
+  int limit[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int n = min(it.col0 + cg * 64 + t * 32 + (lane & 31), ncols - 1);
+    const int j = div_g(a, n);
+    limit[t] = it.limit0 + j;
+    const uint16_t* p =
+        a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D + half * 8;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) st[t][s] = as_bf16x8(ld16(p + s * 16));
+  }
+  float m[2] = {-kInf, -kInf}, l[2] = {0.f, 0.f};
+  __syncthreads();
+
+  const int stages = kend > it.key0 ? (kend - it.key0 + C::ROWS - 1) / C::ROWS : 0;
+  auto issue = [&](int k) {
+    const int kb = it.key0 + k * C::ROWS;
+    stage_rows<C>(s_buf + (k % C::NB) * C::STAGE, wave, lane, [&](int row) {
+      const int key = min(kb + row, kend - 1);
+      return a.kc + (((size_t)s_pages[(key - it.key0) >> 4] * a.hkv + kvh) * 16 + (key & 15)) * D;
+    });
+  };
+  vm_wait<0>();  // the stationary vectors have landed: the waits below count copies only
+#pragma unroll
+  for (int k = 0; k < C::NB - 1; ++k)
+    if (k < stages) issue(k);
+  for (int k = 0; k < stages; ++k) {
+    if (C::NB == 3 && k + 1 < stages)
+      vm_wait<C::LOADS>();
+    else
+      vm_wait<0>();
+    __syncthreads();
+    if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
+    f32x16 acc[2];
+    tile_products<D, NC>(s_buf + (k % C::NB) * C::STAGE, rg, lane, st, acc);
+    const int kb = it.key0 + k * C::ROWS + rg * 32;
+    const bool whole = kb + 31 <= first_limit && kb + 32 <= kend;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (!whole) {
+        const int lim = min(limit[t], kend - 1) - kb - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((i & 3) + 8 * (i >> 2) > lim) acc[t][i] = -kInf;
+      }
+      float mx = acc[t][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, acc[t][i]);
+      const float mn = mx == -kInf ? m[t] : fmaxf(m[t], mx * a.c);
+      const float ms = mn == -kInf ? 0.f : mn;
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -ms));
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (acc[t][i] == -kInf) p[i] = 0.f;  // scale 0 times -inf is NaN
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < w; ++i) p[i] += p[i + w];
+      l[t] = l[t] * exp2_fast(m[t] - ms) + p[0];
+      m[t] = mn;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float m2 = __shfl_xor(m[t], 32, 64), l2 = __shfl_xor(l[t], 32, 64);
+    const float mm = fmaxf(m[t], m2), ms = mm == -kInf ? 0.f : mm;
+    if (half == 0) {
+      s_m[rg][cg * 64 + t * 32 + lane] = mm;
+      s_l[rg][cg * 64 + t * 32 + lane] = l[t] * exp2_fast(m[t] - ms) + l2 * exp2_fast(m2 - ms);
+    }
+  }
+  __syncthreads();
+  if (tid < C::COLS) {
+    float mm = -kInf, ll = 0.f;
+#pragma unroll
+    for (int r = 0; r < C::RG; ++r) mm = fmaxf(mm, s_m[r][tid]);
+    const float ms = mm == -kInf ? 0.f : mm;
+#pragma unroll
+    for (int r = 0; r < C::RG; ++r) ll += s_l[r][tid] * exp2_fast(s_m[r][tid] - ms);
+    const int n = it.col0 + tid;
+    if (it.nsplit > 1) {
+      if (n < it.cols_pad) {
+        float* to = a.ws + it.off1 + (((int64_t)kvh * it.nsplit + it.split) * it.cols_pad + n) * 2;
+        *reinterpret_cast<f32x2*>(to) = f32x2{mm, ll};
+      }
+    } else if (n < ncols) {
+      a.ws[it.off0 + (int64_t)kvh * it.cols_pad + n] = mm + __builtin_amdgcn_logf(ll);
+    }
+  }
+  // columns that only pad: their weights are zero
+  if (it.nsplit == 1 && it.col0 + C::COLS >= ncols)
+    for (int n = ncols + tid; n < it.cols_pad; n += kScoreThreads)
+      a.ws[it.off0 + (int64_t)kvh * it.cols_pad + n] = kInf;
+}
+
+// L of 256 columns from the pieces of a cut key range.
+__global__ __launch_bounds__(kScoreThreads) void score_lse_join_kernel(ScoreArgs a) {
+  const ScoreItem* itp;
+  int kvh;
+  if (!take_item(a, &itp, &kvh)) return;
+  const ScoreItem it = *itp;
+  const int n = it.col0 + (int)threadIdx.x;  // < cols_pad, a multiple of 256
+  float* to = a.ws + it.off0 + (int64_t)kvh * it.cols_pad + n;
+  if (n >= it.rows * a.g) {
+    *to = kInf;
+    return;
+  }
+  const float* r = a.ws + it.off1 + ((int64_t)kvh * it.nsplit * it.cols_pad + n) * 2;
+  float m = -kInf, l = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < it.nsplit; ++s) {
+    const f32x2 v = *reinterpret_cast<const f32x2*>(r + (int64_t)s * it.cols_pad * 2);
+    const float mn = fmaxf(m, v[0]), ms = mn == -kInf ? 0.f : mn;
+    l = l * exp2_fast(m - ms) + v[1] * exp2_fast(v[0] - ms);
+    m = mn;
+  }
+  *to = m + __builtin_amdgcn_logf(l);
+}
+
+template <int D, int NC>
+__global__ __launch_bounds__(kScoreThreads, 2) void score_sum_kernel(ScoreArgs a) {
+  using C = ChunkCfg<D, NC>;
+  __shared__ __attribute__((aligned(16))) char s_buf[C::NB * C::STAGE];
+  __shared__ __attribute__((aligned(16))) float s_lse[C::NB][4][32];  // one copy a wave
+  __shared__ float s_sum[C::RG][C::COLS];
+  const ScoreItem* itp;
+  int kvh;
+  if (!take_item(a, &itp, &kvh)) return;
+  const ScoreItem it = *itp;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = wave % NC, rg = wave / NC, half = lane >> 5;
+  const int ncols = it.rows * a.g;
+  // columns of earlier rows see none of these keys
+  const int n0 = max(0, it.key0 - it.limit0) * a.g / C::ROWS * C::ROWS;
+  const int stages = (ncols - n0 + C::ROWS - 1) / C::ROWS;
+
+  bf16x8 st[2][C::KS];
+  int key[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    key[t] = it.key0 + cg * 64 + t * 32 + (lane & 31);
+    const int k = min(key[t], it.len - 1);
+    const int page = a.bt[(size_t)it.req * a.maxp + k / 16];
+    const uint16_t* p = a.kc + (((size_t)page * a.hkv + kvh) * 16 + k % 16) * D + half * 8;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) st[t][s] = as_bf16x8(ld16(p + s * 16));
+  }
+  // sums of 16 tiles, then the sums of those: few terms that differ much in size
+  float sum[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
+  const float* lse = a.ws + it.off0 + (int64_t)kvh * it.cols_pad;
+  auto issue = [&](int k) {
+    const int nb = n0 + k * C::ROWS;
+    stage_rows<C>(s_buf + (k % C::NB) * C::STAGE, wave, lane, [&](int row) {
+      const int n = min(nb + row, ncols - 1), j = div_g(a, n);
+      return a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D;
+    });
+    if (lane < 8)
+      dma16(lse + nb + rg * 32 + lane * 4,
+            reinterpret_cast<const char*>(&s_lse[k % C::NB][wave][0]));
+  };
+  vm_wait<0>();  // the stationary vectors have landed: the waits below count copies only
+#pragma unroll
+  for (int k = 0; k < C::NB - 1; ++k)
+    if (k < stages) issue(k);
+  for (int k = 0; k < stages; ++k) {
+    if (C::NB == 3 && k + 1 < stages)
+      vm_wait<C::LOADS + 1>();
+    else
+      vm_wait<0>();
+    __syncthreads();
+    if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
+    f32x16 acc[2];
+    tile_products<D, NC>(s_buf + (k % C::NB) * C::STAGE, rg, lane, st, acc);
+    const int nb = n0 + k * C::ROWS + rg * 32;
+    f32x4 lv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      lv[i] = *reinterpret_cast<const f32x4*>(&s_lse[k % C::NB][wave][8 * i + 4 * half]);
+    const bool whole = it.limit0 + div_g(a, nb) >= it.key0 + C::COLS - 1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        p[i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -lv[i >> 2][i & 3]));
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (it.limit0 + div_g(a, nb + (i & 3) + 8 * (i >> 2) + 4 * half) < key[t]) p[i] = 0.f;
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < w; ++i) p[i] += p[i + w];
+      sum[t] += p[0];
+    }
+    if ((k & 15) == 15) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        total[t] += sum[t];
+        sum[t] = 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    float x = total[t] + sum[t];
+    x += __shfl_xor(x, 32, 64);
+    if (half == 0) s_sum[rg][cg * 64 + t * 32 + lane] = x;
+  }
+  __syncthreads();
+  if (tid * 4 < C::COLS && it.key0 + tid * 4 < it.key1) {
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < C::RG; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] += s_sum[r][tid * 4 + i];
+    add_scores4(a, it, kvh, it.key0 + tid * 4, it.key1, w);
+  }
+}
+
+// ---------------------------------------------------------------------------
+
+// Workgroups go in rows of this many: one row of more than 2^24 workgroups would
+// pass the 2^32 threads of a grid's x dimension.
+constexpr int kGridRow = 1 << 16;
+
+template <class K>
+int launch(K kernel, ScoreArgs a, const ScoreHeader* h, ScoreList list, hipStream_t stream) {
+  const int64_t wgs = (int64_t)h->count[list] * h->hkv;
+  if (wgs == 0) return SSA_OK;
+  a.off_items = h->off_items + (int64_t)h->first[list] * (int64_t)sizeof(ScoreItem);
+  a.workgroups = (int32_t)wgs;
+  const dim3 grid(wgs < kGridRow ? wgs : kGridRow, (wgs + kGridRow - 1) / kGridRow);
+  hipLaunchKernelGGL(kernel, grid, dim3(kScoreThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
+}
+
+template <int D>
+int launch_chunks(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
+  int rc = h->lse_groups == 4   ? launch(score_lse_kernel<D, 4>, a, h, kListLse, s)
+           : h->lse_groups == 2 ? launch(score_lse_kernel<D, 2>, a, h, kListLse, s)
+                                : launch(score_lse_kernel<D, 1>, a, h, kListLse, s);
+  if (rc) return rc;
+  if ((rc = launch(score_lse_join_kernel, a, h, kListLseJoin, s))) return rc;
+  return h->sum_groups == 4   ? launch(score_sum_kernel<D, 4>, a, h, kListSum, s)
+         : h->sum_groups == 2 ? launch(score_sum_kernel<D, 2>, a, h, kListSum, s)
+                              : launch(score_sum_kernel<D, 1>, a, h, kListSum, s);
+}
+
+template <int D, bool OUT>
+int launch_decodes(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
+  const int rc = launch(score_decode_kernel<D, OUT>, a, h, kListDecode, s);
+  return rc ? rc : launch(score_decode_join_kernel<D, OUT>, a, h, kListDecodeJoin, s);
+}
+
+int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_dev,
+               const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
+               const float* scores_in, float decay, float* scores_out, void* workspace,
+               size_t ws_bytes, ScoreArgs* a) {
+  if (!std::isfinite(decay) || decay < 0.f) return SSA_ERR_ARG;
+  if (!plan_dev) return SSA_ERR_NULL;
+  if (h->max_q_len > 0 && (!q || !k_cache || !block_table || !scores_out)) return SSA_ERR_NULL;
+  if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
+  *a = ScoreArgs{};
+  a->plan = static_cast<const uint8_t*>(plan_dev);
+  a->hash = h->hash;
+  a->hq = h->hq;
+  a->hkv = h->hkv;
+  a->g = h->hq / h->hkv;
+  a->maxp = h->max_pages_per_req;
+  a->g_magic = (uint32_t)((((uint64_t)1 << 32) + a->g - 1) / a->g);
+  a->c = (float)((double)shape->softmax_scale * (double)kLog2e);
+  a->decay = decay;
+  a->q = q;
+  a->kc = k_cache;
+  a->bt = block_table;
+  a->scores_in = scores_in;
+  a->scores_out = scores_out;
+  a->ws = static_cast<float*>(workspace);
+  return SSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                   const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
+                   const float* scores_in, float decay, float* scores_out, void* workspace,
+                   size_t ws_bytes, void* stream) {
+  const ScoreHeader* h = nullptr;
+  int rc = check_score_plan(shape, plan_host, &h);
+  if (rc) return rc;
+  ScoreArgs a;
+  if ((rc = score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay, scores_out,
+                       workspace, ws_bytes, &a)))
+    return rc;
+  (void)hipGetLastError();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((rc = h->head_dim == 128 ? launch_chunks<128>(a, h, s) : launch_chunks<64>(a, h, s)))
+    return rc;
+  return h->head_dim == 128 ? launch_decodes<128, false>(a, h, s)
+                            : launch_decodes<64, false>(a, h, s);
+}
+
+int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                      const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
+                      const int32_t* block_table, const float* scores_in, float decay,
+                      float* scores_out, uint16_t* out, void* workspace, size_t ws_bytes,
+                      void* stream) {
+  const ScoreHeader* h = nullptr;
+  int rc = check_score_plan(shape, plan_host, &h);
+  if (rc) return rc;
+  if (h->max_q_len > 1) return SSA_ERR_ARG;
+  ScoreArgs a;
+  if ((rc = score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay, scores_out,
+                       workspace, ws_bytes, &a)))
+    return rc;
+  if (h->max_q_len > 0 && (!v_cache || !out)) return SSA_ERR_NULL;
+  a.vc = v_cache;
+  a.out = out;
+  (void)hipGetLastError();
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return h->head_dim == 128 ? launch_decodes<128, true>(a, h, s)
+                            : launch_decodes<64, true>(a, h, s);
+}
+
+}  // extern "C"

@@ -193,6 +193,19 @@ def _load():
     lib.ssa_layer_workspace_size.argtypes = [P(SsaShape), vp, P(SsaLayerWeights), P(sz)]
     lib.ssa_layer_forward.argtypes = [P(SsaShape), vp, vp, P(SsaLayerWeights), vp, vp, vp, vp, vp,
                                       vp, sz, vp]
+    lib.ssa_score_plan_size.argtypes = [P(SsaShape), vp, vp, i32, i32, P(sz), P(sz)]
+    lib.ssa_score_plan.argtypes = [P(SsaShape), vp, vp, i32, i32, vp, sz]
+    lib.ssa_key_scores.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz,
+                                   vp]
+    lib.ssa_decode_scored.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp,
+                                      vp, vp, sz, vp]
+    lib.ssa_evict_plan_size.argtypes = [P(SsaShape), vp, vp, i32, i32, i32, P(sz), P(sz)]
+    lib.ssa_evict_plan.argtypes = [P(SsaShape), vp, vp, i32, i32, i32, vp, sz]
+    lib.ssa_evict_select.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ssa_evict_compact.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.ssa_check_evict_tables.argtypes = [P(SsaShape), vp, vp, vp]
+    lib.ssa_rope_append_shifted.argtypes = [P(SsaShape), vp, vp, vp, vp, i32, vp, vp, vp, vp, vp,
+                                            vp, vp]
     lib.ssa_priority_sort.argtypes = [P(SsaCandidate), i32, ctypes.c_double, ctypes.c_double,
                                       ctypes.c_double, ip]
     lib.ssa_batch_constructor.argtypes = [P(SsaPredictor), ip, i32, P(SsaCandidate), i32, i32,
@@ -217,7 +230,10 @@ EXPORTED = ("ssa_status_string", "ssa_plan_size", "ssa_plan", "ssa_check_block_t
             "ssa_rope_append", "ssa_rope_table", "ssa_linear_workspace_size", "ssa_linear_plan", "ssa_linear",
             "ssa_rms_norm",
             "ssa_layer_workspace_size", "ssa_layer_forward", "ssa_probe_hbm_read",
-            "ssa_probe_hbm_gather", "ssa_probe_mfma_bf16")
+            "ssa_probe_hbm_gather", "ssa_probe_mfma_bf16", "ssa_score_plan_size",
+            "ssa_score_plan", "ssa_key_scores", "ssa_decode_scored", "ssa_evict_plan_size",
+            "ssa_evict_plan", "ssa_evict_select", "ssa_evict_compact", "ssa_check_evict_tables",
+            "ssa_rope_append_shifted")
 
 EPILOGUE_NONE, EPILOGUE_RESIDUAL, EPILOGUE_SWIGLU = 0, 1, 2
 
@@ -576,6 +592,33 @@ def rope_append(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_cac
         raise SsaError(rc, "ssa_rope_append")
 
 
+def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shift_host, shift_dev,
+                        q_out, k_cache, v_cache, block_table, stream=None):
+    """ssa_rope_append_shifted: rope_append of requests that have lost keys to an
+    eviction; request i's tokens are rotated shift_host[i] (int32 array; shift_dev
+    the same on the device) positions past their cache index."""
+    h = _plan_header(plan_host)
+    T, n = h["num_tokens"], h["num_reqs"]
+    d, hq, hkv = shape.head_dim, shape.num_q_heads, shape.num_kv_heads
+    pool = shape.num_pages * hkv * shape.page_size * d
+    _check_dev("qkv", qkv, T * (hq + 2 * hkv) * d, 2)
+    _check_dev("q_out", q_out, T * hq * d, 2)
+    _check_dev("cos_sin", cos_sin, d, 4)
+    _check_dev("k_cache", k_cache, pool, 2)
+    _check_dev("v_cache", v_cache, pool, 2)
+    _check_dev("block_table", block_table, n * shape.max_pages_per_req, 4)
+    _check_dev("shift_dev", shift_dev, n, 4)
+    shift, shift_ptr = _lens(shift_host)
+    if shift.shape[0] != n:
+        raise ValueError(f"{shift.shape[0]} shifts for {n} requests")
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_rope_append_shifted(
+        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(qkv)),
+        vp(_ptr(cos_sin)), int(cos_sin.numel() // d), vp(shift_ptr), vp(_ptr(shift_dev)),
+        vp(_ptr(q_out)), vp(_ptr(k_cache)), vp(_ptr(v_cache)), vp(_ptr(block_table)),
+        vp(_stream(stream))), "ssa_rope_append_shifted")
+
+
 def linear_workspace_size(m: int, n: int, k: int) -> int:
     """Bytes of the workspace ssa_linear needs for an [m, k] x [n, k]^T product."""
     ws = ctypes.c_size_t(0)
@@ -839,3 +882,153 @@ def bind_plan(shape: SsaShape, q_len, ctx_len, tuning, out, info: SsaPlanInfo) -
     call = BoundCall(LIB.ssa_plan, "ssa_plan", args)
     call._keep = (ql, cl)  # the length arrays must outlive the call
     return call
+
+
+# Eviction from the cache by accumulated attention weight (include/ssa_evict.h).
+
+def _plan_buffer(out, nbytes: int):
+    """(buffer, address, bytes) of a plan: `out`, or a new numpy array."""
+    if out is None:
+        out = np.zeros(nbytes, dtype=np.uint8)
+    return out, _ptr(out), (out.nbytes if isinstance(out, np.ndarray)
+                            else out.numel() * out.element_size())
+
+
+def score_plan(shape: SsaShape, q_len, ctx_len, last_rows: int = 0, out=None):
+    """Plan blob of key_scores and decode_scored (a host buffer: numpy uint8, or
+    written into `out`), and their workspace's bytes."""
+    ql, pq = _lens(q_len)
+    cl, pc = _lens(ctx_len)
+    if ql.shape != cl.shape:
+        raise ValueError("q_len and ctx_len differ in length")
+    pb, wb = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(LIB.ssa_score_plan_size(ctypes.byref(shape), pq, pc, ql.shape[0], int(last_rows),
+                                   ctypes.byref(pb), ctypes.byref(wb)), "ssa_score_plan_size")
+    out, ptr, cap = _plan_buffer(out, pb.value)
+    _check(LIB.ssa_score_plan(ctypes.byref(shape), pq, pc, ql.shape[0], int(last_rows), ptr, cap),
+           "ssa_score_plan")
+    return out, wb.value
+
+
+def evict_plan(shape: SsaShape, kv_len, budget, sink: int, recent: int, out=None):
+    """Plan blob of evict_select and evict_compact, and the workspace's bytes."""
+    kl, pk = _lens(kv_len)
+    bl, pb_ = _lens(budget)
+    if kl.shape != bl.shape:
+        raise ValueError("kv_len and budget differ in length")
+    pb, wb = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(LIB.ssa_evict_plan_size(ctypes.byref(shape), pk, pb_, kl.shape[0], int(sink),
+                                   int(recent), ctypes.byref(pb), ctypes.byref(wb)),
+           "ssa_evict_plan_size")
+    out, ptr, cap = _plan_buffer(out, pb.value)
+    _check(LIB.ssa_evict_plan(ctypes.byref(shape), pk, pb_, kl.shape[0], int(sink), int(recent),
+                              ptr, cap), "ssa_evict_plan")
+    return out, wb.value
+
+
+def _evict_header(plan_host):
+    """num_reqs (and tokens of a score plan, kept keys of an eviction plan) of a blob
+    (ssa_evict_format.h)."""
+    b = np.asarray(_as_np(plan_host))[:128].tobytes()
+    i, q = np.frombuffer(b, dtype=np.int32), np.frombuffer(b, dtype=np.int64)
+    if i[0] == 0x31435353:  # a score plan
+        return {"num_reqs": int(i[4]), "num_tokens": int(i[5])}
+    return {"num_reqs": int(i[3]), "num_keep": int(q[8])}
+
+
+def _scored_args(name, shape, plan_host, plan_dev, q, k_cache, block_table, scores_in, decay,
+                 scores_out, workspace):
+    h = _evict_header(plan_host)
+    slots = shape.num_pages * shape.num_kv_heads * shape.page_size
+    rows = h.get("num_tokens", 0) * shape.num_q_heads * shape.head_dim
+    _check_dev("q", q, rows, 2)
+    _check_dev("k_cache", k_cache, slots * shape.head_dim, 2)
+    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
+    _check_dev("scores_in", scores_in, slots, 4)
+    _check_dev("scores_out", scores_out, slots, 4)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return rows, ws_bytes
+
+
+def key_scores(shape: SsaShape, plan_host, plan_dev, q, k_cache, block_table, scores_in,
+               decay: float, scores_out, workspace, stream=None):
+    """ssa_key_scores: a batch's attention weights, added per cached key and kv head
+    (fp32 [num_pages, Hkv, 16]) to decay times scores_in (None: to nothing)."""
+    _, ws_bytes = _scored_args("ssa_key_scores", shape, plan_host, plan_dev, q, k_cache,
+                               block_table, scores_in, decay, scores_out, workspace)
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_key_scores(
+        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(q)),
+        vp(_ptr(k_cache)), vp(_ptr(block_table)), vp(_ptr(scores_in)), float(decay),
+        vp(_ptr(scores_out)), vp(_ptr(workspace)), ctypes.c_size_t(ws_bytes),
+        vp(_stream(stream))), "ssa_key_scores")
+
+
+def decode_scored(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, block_table,
+                  scores_in, decay: float, scores_out, out, workspace, stream=None):
+    """ssa_decode_scored: attention of a pure-decode batch (out as
+    ssa_mixed_attention's) and its weights (scores_out as key_scores')."""
+    rows, ws_bytes = _scored_args("ssa_decode_scored", shape, plan_host, plan_dev, q, k_cache,
+                                  block_table, scores_in, decay, scores_out, workspace)
+    _check_dev("v_cache", v_cache,
+               shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim, 2)
+    _check_dev("out", out, rows, 2)
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_decode_scored(
+        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(q)),
+        vp(_ptr(k_cache)), vp(_ptr(v_cache)), vp(_ptr(block_table)), vp(_ptr(scores_in)),
+        float(decay), vp(_ptr(scores_out)), vp(_ptr(out)), vp(_ptr(workspace)),
+        ctypes.c_size_t(ws_bytes), vp(_stream(stream))), "ssa_decode_scored")
+
+
+def evict_select(shape: SsaShape, plan_host, plan_dev, scores, block_table, keep, workspace,
+                 stream=None):
+    """ssa_evict_select: the kept keys' cache indexes (int32, flat: per request Hkv
+    ascending lists) by the plan's sinks, recent keys and highest scores."""
+    h = _evict_header(plan_host)
+    _check_dev("scores", scores, shape.num_pages * shape.num_kv_heads * shape.page_size, 4)
+    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
+    _check_dev("keep", keep, h.get("num_keep", 0) * shape.num_kv_heads, 4)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_evict_select(
+        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(scores)),
+        vp(_ptr(block_table)), vp(_ptr(keep)), vp(_ptr(workspace)), ctypes.c_size_t(ws_bytes),
+        vp(_stream(stream))), "ssa_evict_select")
+
+
+def evict_compact(shape: SsaShape, plan_host, plan_dev, keep, block_table, new_table, k_cache,
+                  v_cache, scores=None, stream=None):
+    """ssa_evict_compact: the kept keys, values and scores move to the pages of
+    new_table (as check_evict_tables wants them)."""
+    h = _evict_header(plan_host)
+    slots = shape.num_pages * shape.num_kv_heads * shape.page_size
+    _check_dev("keep", keep, h.get("num_keep", 0) * shape.num_kv_heads, 4)
+    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
+    _check_dev("new_table", new_table, h["num_reqs"] * shape.max_pages_per_req, 4)
+    _check_dev("k_cache", k_cache, slots * shape.head_dim, 2)
+    _check_dev("v_cache", v_cache, slots * shape.head_dim, 2)
+    _check_dev("scores", scores, slots, 4)
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_evict_compact(
+        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(keep)),
+        vp(_ptr(block_table)), vp(_ptr(new_table)), vp(_ptr(k_cache)), vp(_ptr(v_cache)),
+        vp(_ptr(scores)), vp(_stream(stream))), "ssa_evict_compact")
+
+
+def check_evict_tables(shape: SsaShape, plan_host, block_table_host, new_table_host=None) -> None:
+    """ssa_check_evict_tables on host copies (int32 [num_reqs, max_pages_per_req]);
+    raises SsaError on a page outside the pool or a new page that is not free."""
+    n = _evict_header(plan_host)["num_reqs"]
+    tables = []
+    for t in (block_table_host, new_table_host):
+        if t is not None:
+            t = np.ascontiguousarray(t, dtype=np.int32)
+            if t.shape != (n, shape.max_pages_per_req):
+                raise ValueError(f"table of shape {t.shape}, the plan needs "
+                                 f"({n}, {shape.max_pages_per_req})")
+        tables.append(t)
+    vp = ctypes.c_void_p
+    _check(LIB.ssa_check_evict_tables(ctypes.byref(shape), vp(_ptr(plan_host)),
+                                      vp(_ptr(tables[0])), vp(_ptr(tables[1]))),
+           "ssa_check_evict_tables")

@@ -1,0 +1,629 @@
+"""GPU parity of the eviction entry points (include/ssa_evict.h) with the float64
+oracle (oracle/evict.py), and a run of them together.
+
+Bars, from the arithmetic:
+* scores.  A logit is a sum of D exact products accumulated in fp32: it is off by at
+  most D 2^-24 A, A = max sum |scale q_i k_i| over the request's pairs, and so are the
+  logarithms of the sums; the exponents' fma and the exponential add a few 2^-24 of
+  their argument (<= 2 A log2 e) and value; sums of positive terms add at most one
+  2^-24 each along the longest chain (here under L / 32 + 128, L keys, for a
+  sum over keys, and under R / 32 + 128 for one over R columns).  So
+      |err| <= ref 2^-24 (2 D A + 8 A + 2 (L + R) / 32 + 512).
+* attention outputs: that relative error and two roundings to bf16 (the weight's and
+  the sum's of rounded weights) of every |w v|, and the result's own rounding:
+      |err| <= 2^-8 |ref| + (2^-7 + 2 rel) sum |w v|.
+* keys, values, indexes: bit for bit.
+"""
+import sys
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def torch_dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def dev(torch, a):
+    if a.dtype == np.uint16:
+        return torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).cuda().view(torch.bfloat16)
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+class Scored:
+    """A batch on the device, appended, with its score plan."""
+
+    def __init__(self, torch, b, window=0, old=True, q_scale=1, plan="device"):
+        from oracle import oracle
+        from paper_2606_05933_amd import ssa, workload
+        self.b, self.ssa, self.torch, self.window = b, ssa, torch, window
+        if q_scale != 1:
+            b.q = workload.f32_to_bf16_bits(workload.bf16_bits_to_f32(b.q) * np.float32(q_scale))
+        self.kc, self.vc = oracle.batch_kv_append(b)
+        s = b.shape
+        self.shape = ssa.make_shape(s.hq, s.hkv, s.d, b.num_pages, b.max_pages_per_req,
+                                    s.softmax_scale)
+        self.plan, ws = ssa.score_plan(self.shape, b.q_len, b.ctx_len, window)
+        if plan == "pinned":
+            self.plan_dev = torch.from_numpy(self.plan).pin_memory()
+            self.plan = self.plan_dev
+        else:
+            self.plan_dev = dev(torch, self.plan)
+        # a workspace that holds anything
+        self.ws = torch.full((ws,), 0xFF, dtype=torch.uint8, device="cuda")
+        self.q, self.k, self.v = dev(torch, b.q), dev(torch, self.kc), dev(torch, self.vc)
+        self.table = dev(torch, b.block_table)
+        rng = np.random.default_rng(b.seed)
+        self.old = rng.lognormal(-1, 2, (b.num_pages, s.hkv, 16)).astype(np.float32) if old else None
+        # scores of keys that are new, and of no key, hold NaN
+        if old:
+            known = np.zeros(self.old.shape, bool)
+            for i in range(b.num_reqs):
+                t = np.arange(b.ctx_len[i])
+                known[b.block_table[i, t // 16], :, t % 16] = True
+            self.old[~known] = np.nan
+        self.old_dev = dev(torch, self.old) if old else None
+        self.out_scores = torch.full((b.num_pages, s.hkv, 16), -7.0, device="cuda")
+        self.out = torch.zeros((b.num_tokens, s.hq, s.d), dtype=torch.bfloat16, device="cuda")
+
+    def scores(self, decay=1.0, out=None, stream=None):
+        self.ssa.key_scores(self.shape, self.plan, self.plan_dev, self.q, self.k, self.table,
+                            self.old_dev, decay, self.out_scores if out is None else out, self.ws,
+                            stream)
+
+    def decode(self, decay=1.0, stream=None):
+        self.ssa.decode_scored(self.shape, self.plan, self.plan_dev, self.q, self.k, self.v,
+                               self.table, self.old_dev, decay, self.out_scores, self.out, self.ws,
+                               stream)
+
+    def rel(self, size):
+        n = int((self.b.q_len + self.b.ctx_len).max())
+        r = int(self.b.q_len.max()) * self.b.shape.group
+        return 2.0 ** -24 * ((2 * self.b.shape.d + 8) * size + 2 * (n + r) / 32 + 512)
+
+    def check_scores(self, decay=1.0, got=None):
+        from oracle import evict
+        ref, size = evict.key_scores(self.b, self.kc, self.window, self.old, decay)
+        got = (self.out_scores if got is None else got).cpu().numpy().astype(np.float64)
+        untouched = np.isnan(ref)
+        assert (got[untouched] == -7.0).all(), "slots of no key, or of idle requests, were written"
+        err, tol = np.abs(got - ref), self.rel(size) * np.abs(ref)
+        bad = ~untouched & ~(err <= tol)
+        assert not bad.any(), (int(bad.sum()), float(np.nanmax(err / ref)), np.argwhere(bad)[:5])
+        return float(np.sqrt(np.nansum(err ** 2) / np.nansum(ref ** 2)))
+
+    def check_out(self):
+        from oracle import evict, oracle
+        ref, _ = oracle.batch_attention(self.b, self.kc, self.vc)
+        b = self.b
+        plus = np.where(self.vc == 0x7FC0, 0, self.vc & 0x7FFF).astype(np.uint16)
+        mass, _ = oracle.batch_attention(b, self.kc, plus)
+        _, size = evict.key_scores(b, self.kc, self.window)
+        rel = self.rel(np.nanmax(size))
+        got = self.out.float().cpu().numpy().astype(np.float64)
+        err, tol = np.abs(got - ref), 2.0 ** -8 * np.abs(ref) + (2.0 ** -7 + 2 * rel) * mass
+        assert (err <= tol).all(), (float(np.nanmax(err)), np.argwhere(~(err <= tol))[:5])
+
+
+def batch(hq, hkv, d, c, u, seed=0, scale=None):
+    from paper_2606_05933_amd import workload
+    b = workload.make_batch(workload.Shape(hq, hkv, d, scale=scale), c, u, seed=seed, spare_pages=5,
+                            extra_pages_per_req=2)
+    say(f"[gpu evict] hq/hkv/d={hq}/{hkv}/{d} c={list(c)[:8]} u={list(u)[:8]} seed={seed}")
+    return b
+
+
+HEADS = [(8, 8, 64), (4, 2, 128), (28, 4, 128), (16, 1, 64), (64, 8, 128), (5, 5, 64), (13, 1, 128)]
+EDGES = [0, 1, 14, 15, 16, 30, 31, 32, 33, 126, 127, 128, 129, 255, 256, 500]
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("out", [False, True])
+def test_decode_rows_at_every_block_edge(torch_dev, heads, out):
+    u = EDGES + [0, 47]
+    c = [1] * len(EDGES) + [0, 0]
+    x = Scored(torch_dev, batch(*heads, c, u, seed=3))
+    x.decode(0.75) if out else x.scores(0.75)
+    torch_dev.cuda.synchronize()
+    x.check_scores(0.75)
+    if out:
+        x.check_out()
+
+
+@pytest.mark.parametrize("heads,u", [((8, 2, 128), [20001, 4097, 9]), ((64, 8, 128), [33000]),
+                                     ((2, 1, 64), [70000, 1])])
+def test_long_decodes_join_their_pieces(torch_dev, heads, u):
+    x = Scored(torch_dev, batch(*heads, [1] * len(u), u, seed=4), q_scale=2)
+    x.decode()
+    torch_dev.cuda.synchronize()
+    say("    scores", x.check_scores())
+    x.check_out()
+    x.out_scores.fill_(-7.0)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    x.check_scores()
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("window", [0, 1, 2, 40])
+def test_hybrid_batches(torch_dev, heads, window):
+    c = [3, 1, 0, 64, 1, 33, 2, 130]
+    u = [0, 100, 40, 0, 0, 257, 15, 31]
+    x = Scored(torch_dev, batch(*heads, c, u, seed=5), window=window)
+    x.scores(0.5)
+    torch_dev.cuda.synchronize()
+    x.check_scores(0.5)
+
+
+@pytest.mark.parametrize("c,u,heads", [
+    ([700], [900], (8, 2, 128)),           # tiles of every width: see the plan's groups
+    ([64], [192], (8, 8, 64)),
+    ([20], [3000], (8, 8, 64)),
+    ([2], [5000], (4, 1, 128)),
+    ([1030], [0], (28, 4, 128)),
+    ([300, 45, 2], [5000, 1, 9000], (32, 8, 128)),
+    ([17], [40000], (4, 2, 64))])          # key ranges in pieces
+@pytest.mark.parametrize("q_scale", [1, 4])
+def test_chunks(torch_dev, c, u, heads, q_scale):
+    x = Scored(torch_dev, batch(*heads, c, u, seed=6), q_scale=q_scale)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    say("    scores", x.check_scores(), "groups", x.plan[:128].view(np.int32)[14:16])
+
+
+def test_every_width_of_tile_runs(torch_dev):
+    """Both passes in tiles of 64, 128 and 256 columns, D 64 and 128: the planner's
+    choices over batches of different sizes."""
+    seen = set()
+    for d in (64, 128):
+        for hq, hkv, c, u in ((2, 2, 20, 100), (4, 2, 40, 2000), (8, 8, 100, 4000), (8, 4, 512, 200),
+                              (16, 16, 130, 4500), (16, 16, 60, 9000)):
+            x = Scored(torch_dev, batch(hq, hkv, d, [c], [u], seed=7), old=False)
+            x.scores()
+            torch_dev.cuda.synchronize()
+            x.check_scores()
+            lse, sums = x.plan[:128].view(np.int32)[14:16]
+            seen |= {("lse", d, int(lse)), ("sum", d, int(sums))}
+    assert seen == {(k, d, n) for k in ("lse", "sum") for d in (64, 128) for n in (1, 2, 4)}, seen
+
+
+@pytest.mark.parametrize("chunk", [1, 50])
+def test_uniform_weights_with_scale_zero(torch_dev, chunk):
+    x = Scored(torch_dev, batch(8, 2, 64, [chunk], [200], seed=8, scale=0.0), old=False)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    x.check_scores()
+    if chunk == 1:
+        x.decode()
+        torch_dev.cuda.synchronize()
+        x.check_scores()
+        x.check_out()
+
+
+def test_scores_in_place_and_from_pinned_plans(torch_dev):
+    """scores_in may be scores_out; the plan may be read from pinned host memory."""
+    torch = torch_dev
+    for plan in ("device", "pinned"):
+        x = Scored(torch, batch(8, 2, 128, [1, 40, 1], [100, 60, 1500], seed=9), plan=plan)
+        both = x.old_dev.clone()
+        both[x.old_dev.isnan()] = -7.0
+        x.old_dev = both
+        x.scores(0.9, out=both)
+        torch.cuda.synchronize()
+        x.check_scores(0.9, got=both)
+
+
+def test_one_key_takes_all_and_extreme_logits(torch_dev):
+    """Logits of +-1e4: one key's weight is 1, the others underflow to 0."""
+    torch = torch_dev
+    from paper_2606_05933_amd import workload
+    for c in (1, 20):
+        b = batch(4, 2, 64, [c], [300], seed=10)
+        b.q = workload.f32_to_bf16_bits(workload.bf16_bits_to_f32(b.q) * np.float32(3e3))
+        x = Scored(torch, b, old=False)
+        x.scores()
+        torch.cuda.synchronize()
+        got = x.out_scores.cpu().numpy()
+        t = np.arange(300 + c)
+        got = got[b.block_table[0, t // 16], :, t % 16]
+        assert np.isfinite(got).all() and (got >= 0).all()
+        # each counted row gives every kv head its G heads' weights, 1 apiece
+        assert np.allclose(got.sum(axis=0), 2 * c, rtol=1e-4)
+
+
+def test_scored_calls_are_deterministic_on_a_side_stream_and_in_a_graph(torch_dev):
+    torch = torch_dev
+    x = Scored(torch, batch(8, 2, 128, [1, 1, 1], [5000, 77, 16], seed=11))
+    y = Scored(torch, batch(8, 2, 128, [70, 1, 9], [2000, 77, 600], seed=12))
+    x.decode()
+    y.scores()
+    torch.cuda.synchronize()
+    want = [x.out_scores.clone(), x.out.clone(), y.out_scores.clone()]
+    x.check_scores()
+    y.check_scores()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def both(stream=None):
+        x.decode(stream=stream)
+        y.scores(stream=stream)
+
+    def same():
+        got = [x.out_scores, x.out, y.out_scores]
+        return all(torch.equal(a, b) for a, b in zip(got, want))
+
+    def clear():
+        for t in (x.out_scores, y.out_scores):
+            t.fill_(-7.0)
+        x.out.zero_()
+        for t in (x.ws, y.ws):
+            t.fill_(0xA5)
+        torch.cuda.synchronize()
+
+    clear()
+    both(side)
+    side.synchronize()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            both()
+    for r in range(4):
+        clear()
+        graph.replay()
+        torch.cuda.synchronize()
+        say("    replay", r)
+        assert same()
+
+
+def test_a_stale_device_plan_writes_nothing(torch_dev):
+    torch = torch_dev
+    x = Scored(torch, batch(8, 2, 64, [1, 30], [100, 60], seed=13))
+    good = x.plan_dev
+    x.plan_dev = good.clone()
+    x.plan_dev[8] ^= 1  # its hash
+    x.scores()
+    torch.cuda.synchronize()
+    assert bool((x.out_scores == -7.0).all())
+
+
+# ---------------------------------------------------------------------------
+# selection and compaction
+
+def table_of(rng, lens, width, num_pages, first=None):
+    t = np.full((len(lens), width), -1, dtype=np.int32)
+    order = rng.permutation(num_pages).astype(np.int32) if first is None else first
+    at = 0
+    for i, n in enumerate(lens):
+        k = -(-int(n) // 16)
+        t[i, :k] = order[at:at + k]
+        at += k
+    return t, order[at:]
+
+
+class Evicted:
+    def __init__(self, torch, lens, budget, sink, recent, hkv=2, d=64, seed=0, scores=None):
+        from paper_2606_05933_amd import ssa, workload
+        self.torch, self.ssa = torch, ssa
+        rng = np.random.default_rng(seed)
+        self.lens = np.asarray(lens)
+        self.kept = np.minimum(self.lens, budget)
+        pages = int((-(-self.lens // 16)).sum() + (-(-self.kept // 16)).sum()) + 3
+        width = max(1, int((-(-self.lens // 16)).max())) + 1
+        self.table, free = table_of(rng, self.lens, width, pages)
+        self.new, _ = table_of(rng, np.where(self.kept < self.lens, self.kept, 0), width, pages, free)
+        self.shape = ssa.make_shape(hkv * 2, hkv, d, pages, width, 0.1)
+        say(f"[gpu evict] lens={lens[:6]} budget={budget} sink/recent={sink}/{recent} hkv/d={hkv}/{d}")
+        self.plan, ws = ssa.evict_plan(self.shape, lens, np.broadcast_to(budget, (len(lens),)), sink,
+                                       recent)
+        ssa.check_evict_tables(self.shape, self.plan, self.table, self.new)
+        x = rng.lognormal(-1, 2, (pages, hkv, 16)).astype(np.float32)
+        x[rng.random(x.shape) < 0.2] = 0
+        self.scores = x if scores is None else scores(rng, x)
+        self.k = workload.normal_bf16((pages, hkv, 16, d), seed)
+        self.v = workload.normal_bf16((pages, hkv, d, 16), seed + 1)
+        from oracle import evict
+        self.want = []
+        for i, n in enumerate(self.lens):
+            t = np.arange(n)
+            self.want.append([evict.select(self.scores[self.table[i, t // 16], h, t % 16],
+                                           int(self.kept[i]), sink, recent) for h in range(hkv)])
+        self.flat = np.concatenate([np.concatenate(w) for w in self.want]).astype(np.int32)
+        self.plan_dev = dev(torch, self.plan)
+        self.dev = [dev(torch, a) for a in (self.scores, self.table, self.new, self.k, self.v)]
+        self.keep = torch.full((len(self.flat) + 8,), -5, dtype=torch.int32, device="cuda")
+        self.ws = torch.full((ws,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def select(self, stream=None):
+        s, t, *_ = self.dev
+        self.ssa.evict_select(self.shape, self.plan, self.plan_dev, s, t, self.keep, self.ws, stream)
+
+    def check_select(self):
+        got = self.keep.cpu().numpy()
+        n = len(self.flat)
+        assert (got[n:] == -5).all()
+        assert np.array_equal(got[:n], self.flat), np.flatnonzero(got[:n] != self.flat)[:5]
+
+    def compact(self, keep=None, scores=True, stream=None):
+        s, t, new, k, v = self.dev
+        self.ssa.evict_compact(self.shape, self.plan, self.plan_dev,
+                               self.keep if keep is None else keep, t, new, k, v,
+                               s if scores else None, stream)
+
+    def check_compact(self, scores=True):
+        from oracle import evict
+        from paper_2606_05933_amd.device import bits_of
+        k, v, s = evict.compact(self.k, self.v, self.scores, self.table, self.new, self.lens,
+                                self.want)
+        assert np.array_equal(bits_of(self.dev[3]).reshape(k.shape), k)
+        assert np.array_equal(bits_of(self.dev[4]).reshape(v.shape), v)
+        got = self.dev[0].cpu().numpy()
+        assert np.array_equal(got.view(np.int32), (s if scores else self.scores).view(np.int32))
+
+
+LENGTHS = [1, 2, 15, 16, 17, 63, 64, 65, 255, 256, 257, 300, 1000, 4096]
+
+
+@pytest.mark.parametrize("budget,sink,recent", [(1, 0, 0), (1, 1, 0), (1, 0, 1), (20, 4, 8), (64, 0, 0),
+                                                (65, 0, 65), (255, 4, 200), (999, 0, 1), (5000, 9, 9)])
+def test_select_and_compact(torch_dev, budget, sink, recent):
+    x = Evicted(torch_dev, LENGTHS, budget, sink, recent, hkv=3, d=64, seed=1)
+    x.select()
+    x.compact()
+    torch_dev.cuda.synchronize()
+    x.check_select()
+    x.check_compact()
+
+
+@pytest.mark.parametrize("lens,budget", [([4097, 5], 4096), ([33000, 20000], 1000), ([70001], 69999),
+                                         ([40000], 17), ([131072, 9000, 1], 8192)])
+def test_long_lists(torch_dev, lens, budget):
+    x = Evicted(torch_dev, lens, budget, 4, 5, hkv=2, d=128, seed=2)
+    x.select()
+    x.compact()
+    torch_dev.cuda.synchronize()
+    x.check_select()
+    x.check_compact()
+
+
+def equal(rng, x):
+    return np.full_like(x, 0.25)
+
+
+def few_values(rng, x):
+    return rng.choice(np.array([0.0, -0.0, 1.0, -1.0, 1e-42, 3e38], np.float32), x.shape)
+
+
+def not_finite(rng, x):
+    return rng.choice(np.array([np.nan, np.inf, -np.inf, 0.5, -np.nan, -3.0], np.float32), x.shape)
+
+
+def near(rng, x):
+    return (np.float32(1) + rng.integers(0, 4, x.shape) * np.float32(2 ** -23)).astype(np.float32)
+
+
+@pytest.mark.parametrize("scores", [equal, few_values, not_finite, near])
+@pytest.mark.parametrize("lens", [[300, 4000], [50000]])
+def test_ties_and_odd_values(torch_dev, scores, lens):
+    x = Evicted(torch_dev, lens, 137, 3, 10, seed=3, scores=scores)
+    x.select()
+    torch_dev.cuda.synchronize()
+    x.check_select()
+
+
+def test_no_budget_and_no_keys(torch_dev):
+    x = Evicted(torch_dev, [0, 40, 0, 33], np.array([5, 0, 0, 20]), 0, 0, seed=4)
+    x.select()
+    x.compact(scores=False)
+    torch_dev.cuda.synchronize()
+    x.check_select()
+    x.check_compact(scores=False)
+
+
+def test_indexes_outside_a_request_are_not_followed(torch_dev):
+    torch = torch_dev
+    x = Evicted(torch, [100, 60], 40, 0, 0, seed=5)
+    bad = x.flat.copy()
+    bad[3], bad[50], bad[-1] = -1, 100, 2 ** 31 - 1
+    x.compact(keep=dev(torch, bad))
+    torch.cuda.synchronize()
+    from paper_2606_05933_amd.device import bits_of
+    k = bits_of(x.dev[3]).reshape(x.k.shape)
+    for flat, i, h, r in ((3, 0, 0, 3), (50, 0, 1, 10), (len(bad) - 1, 1, 1, 39)):
+        page = x.new[i, r // 16]
+        assert np.array_equal(k[page, h, r % 16], x.k[page, h, r % 16])
+    page, t = x.new[0, 0], x.flat[4]
+    assert np.array_equal(k[page, 0, 4], x.k[x.table[0, t // 16], 0, t % 16])
+
+
+def test_eviction_in_a_graph_and_on_a_side_stream(torch_dev):
+    torch = torch_dev
+    x = Evicted(torch, [3000, 40000, 100], 900, 4, 32, hkv=2, d=128, seed=6)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    x.select(side)
+    x.compact(stream=side)
+    side.synchronize()
+    x.check_select()
+    x.check_compact()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            x.select()
+            x.compact()
+    for r in range(4):
+        x.keep.fill_(-5)
+        for t, a in zip((x.dev[0], x.dev[3], x.dev[4]), (x.scores, x.k, x.v)):
+            t.copy_(dev(torch, a))
+        x.ws.fill_(0x5A)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        say("    replay", r)
+        x.check_select()
+        x.check_compact()
+
+
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,cu,shift", [
+    ((32, 8, 128), [(1, 100), (1, 15), (33, 40), (0, 9), (1, 0)], [900, 0, 5, 77, 31]),
+    ((8, 8, 64), [(70, 0), (1, 63)], [0, 4000]),
+    ((128, 16, 128), [(1, 7), (3, 14)], [11, 12])])
+def test_rope_append_shifted(torch_dev, heads, cu, shift):
+    """The rotation of ssa_rope_append at the shifted positions, bit for bit, in the
+    unshifted slots."""
+    torch = torch_dev
+    from oracle import layer as olay
+    from paper_2606_05933_amd import ssa, workload
+    from paper_2606_05933_amd.device import bits_of
+    hq, hkv, d = heads
+    b = batch(hq, hkv, d, [c for c, _ in cu], [u for _, u in cu], seed=14)
+    shape = ssa.make_shape(hq, hkv, d, b.num_pages, b.max_pages_per_req, 0.1)
+    plan, _ = ssa.ssa_plan(shape, b.q_len, b.ctx_len)
+    qkv = np.concatenate([b.q, b.k_new, b.v_new], axis=1)
+    most = max(c + u + s for (c, u), s in zip(cu, shift) if c)
+    cos_sin = dev(torch, ssa.rope_cos_sin(most, d))
+    shift = np.asarray(shift, np.int32)
+
+    def call(fn, *more):
+        k, v = dev(torch, b.k_cache), dev(torch, b.v_cache)
+        q = torch.zeros((b.num_tokens, hq, d), dtype=torch.bfloat16, device="cuda")
+        fn(shape, plan, dev(torch, plan), dev(torch, qkv), cos_sin, *more, q, k, v,
+           dev(torch, b.block_table))
+        torch.cuda.synchronize()
+        return [bits_of(t) for t in (q, k, v)]
+
+    got = call(ssa.rope_append_shifted, shift, dev(torch, shift))
+    f = workload.bf16_bits_to_f32
+    pos = olay.positions(b.q_len, b.ctx_len) + np.repeat(shift, b.q_len)
+    ref = olay.rope(f(b.q).astype(np.float64), pos)
+    assert np.all(np.abs(f(got[0]).reshape(ref.shape) - ref) <= 2.0 ** -8 * np.abs(ref) + 1e-6)
+    kref = olay.rope(f(b.k_new).astype(np.float64), pos)
+    k = got[1].reshape(b.k_cache.shape)
+    new = np.zeros(k.shape, bool)
+    t = 0
+    for i in range(b.num_reqs):
+        for j in range(b.q_len[i]):
+            p = b.ctx_len[i] + j
+            page = b.block_table[i, p // 16]
+            new[page, :, p % 16] = True
+            assert np.all(np.abs(f(k[page, :, p % 16]) - kref[t]) <= 2.0 ** -8 * np.abs(kref[t]) + 1e-6)
+            t += 1
+    assert np.array_equal(k[~new], b.k_cache[~new])
+    # without a shift: rope_append, bit for bit, and the values always
+    plain = call(ssa.rope_append)
+    none = call(ssa.rope_append_shifted, 0 * shift, dev(torch, 0 * shift))
+    assert all(np.array_equal(x, y) for x, y in zip(plain, none))
+    assert np.array_equal(plain[2], got[2])
+
+
+def test_a_request_decodes_over_its_budget_and_goes_on(torch_dev):
+    """The operators together: a prompt is read in chunks whose rows vote, decode rows
+    add their weights, the cache is cut to its budget and moved, and decoding goes on
+    over the kept keys at the true positions.  Every step against the float64
+    oracle on the device's own state."""
+    torch = torch_dev
+    from oracle import evict as oev
+    from oracle import oracle as orc
+    from paper_2606_05933_amd import ssa, workload
+    from paper_2606_05933_amd.device import bits_of
+    hq, hkv, d, pages, width = 8, 2, 128, 64, 24
+    shape = ssa.make_shape(hq, hkv, d, pages, width, d ** -0.5)
+    rng = np.random.default_rng(20)
+    order = rng.permutation(pages).astype(np.int32)
+    table = np.full((2, width), -1, np.int32)
+    free = order.tolist()
+    k = torch.full((pages, hkv, 16, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    v = torch.full((pages, hkv, d, 16), float("nan"), dtype=torch.bfloat16, device="cuda")
+    scores = torch.full((pages, hkv, 16), float("nan"), device="cuda")
+    cos_sin = dev(torch, ssa.rope_cos_sin(2048, d))
+    u, shift = np.array([0, 0]), np.array([0, 0], np.int32)
+    f = workload.bf16_bits_to_f32
+
+    def iteration(c, step):
+        nonlocal u
+        c = np.asarray(c)
+        T = int(c.sum())
+        for i in range(2):  # pages for the new keys
+            for p in range(-(-int(u[i]) // 16), -(-int(u[i] + c[i]) // 16)):
+                table[i, p] = free.pop()
+        qkv = dev(torch, workload.normal_bf16((T, (hq + 2 * hkv) * d), 100 + step))
+        plan, _ = ssa.ssa_plan(shape, c, u)
+        plan_dev = dev(torch, plan)
+        t = dev(torch, table)
+        q = torch.empty((T, hq, d), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(q)
+        ssa.rope_append_shifted(shape, plan, plan_dev, qkv, cos_sin, shift, dev(torch, shift), q, k,
+                                v, t)
+        sp, ws = ssa.score_plan(shape, c, u, 32)
+        ws = torch.empty(ws, dtype=torch.uint8, device="cuda")
+        before = scores.cpu().numpy()
+        if c.max() > 1:
+            aw = torch.zeros(ssa.ssa_plan_size(shape, c, u)[1], dtype=torch.uint8, device="cuda")
+            ssa.ssa_mixed_attention(shape, plan, plan_dev, q, k, v, t, out, aw)
+            ssa.key_scores(shape, sp, dev(torch, sp), q, k, t, scores, 0.9, scores, ws)
+        else:
+            ssa.decode_scored(shape, sp, dev(torch, sp), q, k, v, t, scores, 0.9, scores, out, ws)
+        torch.cuda.synchronize()
+        b = workload.Batch(workload.Shape(hq, hkv, d), c, u, table, pages, bits_of(q), None, None,
+                           None, None)
+        kc, vc = bits_of(k), bits_of(v)
+        ref, _ = orc.batch_attention(b, kc, vc)
+        err = np.abs(out.float().cpu().numpy() - ref)
+        assert err.max() <= 2e-2 and err.mean() <= 2e-3
+        want, _ = oev.key_scores(b, kc, 32, before, 0.9)
+        got = scores.cpu().numpy()
+        at = ~np.isnan(want)
+        # weights are off by well under 1e-4 of themselves (the bar of the tests above)
+        assert np.allclose(got[at], want[at], rtol=1e-4, atol=0)
+        u = u + c
+
+    say("[gpu evict] together")
+    iteration([100, 60], 0)
+    iteration([150, 1], 1)
+    iteration([1, 1], 2)
+    for turn in range(2):
+        lens = u.copy()
+        plan, ws = ssa.evict_plan(shape, lens, [120, 50], 4, 16)
+        kept = np.minimum(lens, [120, 50])
+        new = np.full((2, width), -1, np.int32)
+        for i in range(2):
+            assert kept[i] < lens[i]
+            for p in range(-(-int(kept[i]) // 16)):
+                new[i, p] = free.pop()
+        ssa.check_evict_tables(shape, plan, table, new)
+        keep = torch.empty(int(kept.sum()) * hkv, dtype=torch.int32, device="cuda")
+        ws = torch.empty(ws, dtype=torch.uint8, device="cuda")
+        sc, kb, vb = scores.cpu().numpy(), bits_of(k), bits_of(v)
+        pd = dev(torch, plan)
+        ssa.evict_select(shape, plan, pd, scores, dev(torch, table), keep, ws)
+        ssa.evict_compact(shape, plan, pd, keep, dev(torch, table), dev(torch, new), k, v, scores)
+        torch.cuda.synchronize()
+        want = []
+        for i, n in enumerate(lens):
+            t = np.arange(n)
+            want.append([oev.select(sc[table[i, t // 16], h, t % 16], int(kept[i]), 4, 16)
+                         for h in range(hkv)])
+        assert np.array_equal(keep.cpu().numpy(), np.concatenate([np.concatenate(w) for w in want]))
+        k2, v2, s2 = oev.compact(kb, vb, sc, table, new, lens, want)
+        assert np.array_equal(bits_of(k), k2) and np.array_equal(bits_of(v), v2)
+        assert np.array_equal(scores.cpu().numpy().view(np.int32), s2.view(np.int32))
+        free += [int(p) for i in range(2) for p in table[i, :-(-int(lens[i]) // 16)]]
+        table = new
+        shift = (shift + lens - kept).astype(np.int32)
+        u = kept
+        iteration([1, 1], 10 + 2 * turn)
+        iteration([20, 1], 11 + 2 * turn)
+    assert shift.tolist() == [131 + 21, 12 + 2]
