@@ -32,6 +32,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Memory that no launch that reads it writes (plans, block tables), at a
+// wave-uniform address: read by the scalar unit, whose loads do not wait behind the
+// vector loads in flight.
+template <class T>
+using uniform_ptr = const __attribute__((address_space(4))) T*;
+template <class T>
+__device__ __forceinline__ uniform_ptr<T> as_uniform(const void* p) {
+  return (uniform_ptr<T>)(uintptr_t)p;
+}
+
 // One wave-wide global -> LDS copy of 16 bytes per lane (global_load_lds_dwordx4):
 // lane i's 16 bytes from g land at LDS address l + 16 i (l wave-uniform).  It
 // is inline assembly, so the compiler's memory-counter tracking does not make
@@ -56,6 +66,19 @@ __device__ __forceinline__ void dma16(const void* g, const char* l) {
 __device__ __forceinline__ void dma16_stream(const void* g, const char* l) {
   const uint32_t a = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)l;
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(g), "{m0}"(a) : "memory");
+}
+
+// dma16 from a wave-uniform base and a byte offset per lane: the address costs no
+// 64-bit vector arithmetic.  A vector instruction may have written the base's scalar
+// registers last (v_readfirstlane), and a vector-memory instruction that reads them
+// needs five wait states then, which cover M0's as well.
+__device__ __forceinline__ void dma16_base(const void* base, uint32_t offset, const char* l) {
+  const uint32_t a = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)l;
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);  // the builtin returns int
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+  const uint64_t u = ((uint64_t)hi << 32) | lo;
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(u), "{m0}"(a) : "memory");
 }
 
 // s_waitcnt vmcnt(N): all but this wave's N most recent vector-memory

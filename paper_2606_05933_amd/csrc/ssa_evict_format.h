@@ -14,7 +14,8 @@ namespace ssa {
 constexpr uint32_t kScoreMagic = 0x31435353u;  // "SSC1"
 constexpr uint32_t kEvictMagic = 0x31565353u;  // "SSV1"
 constexpr int kScoreThreads = 256;             // four waves
-constexpr int kScoreWaveCols = 64;             // stationary columns of a wave (chunk kernels)
+constexpr int kScoreWaveCols = 64;             // stationary vectors of a wave (chunk kernels)
+constexpr int kSumKeys = 4 * kScoreWaveCols;   // keys of a tile of the second chunk pass
 constexpr int kLseMaxKeys = 32768;             // keys of one item of the first chunk pass
 constexpr int kJoinKeys = 1024;                // keys of one item of the decode join
 constexpr int kColsPad = 256;                  // a chunk request's columns are padded to this
@@ -40,8 +41,10 @@ struct ScoreHeader {
   int32_t hq, hkv, head_dim, page_size, max_pages_per_req, num_pages;
   float softmax_scale;
   int32_t max_q_len;
-  int32_t lse_groups, sum_groups;  // column groups (waves side by side) of the chunk kernels
-  int32_t off_items, pad;
+  int32_t lse_groups;   // waves side by side over the columns in the first chunk pass
+  int32_t sum_cols;     // columns of an item of the second, a multiple of 32
+  int32_t off_items;
+  int32_t num_tickets;  // of the second: int32 words at the start of the workspace
   int32_t count[kNumScoreLists], first[kNumScoreLists];  // items of each list
   int64_t plan_bytes, ws_bytes;
 };
@@ -54,8 +57,8 @@ struct ScoreReq {
 struct ScoreItem {
   int32_t req;
   int32_t q_row;    // token row of the first counted row
-  int32_t limit0;   // the last key that row sees
-  int32_t rows;     // counted rows
+  int32_t ticket;   // kListSum, of several pieces: the tile's ticket for kv head 0
+  int32_t rows;     // counted rows; row j sees keys 0 .. len - rows + j
   int32_t len;      // keys, u + c
   int32_t ctx_len;  // u
   int32_t col0;     // first column (row * G + head in group) of the item
@@ -63,7 +66,8 @@ struct ScoreItem {
   int32_t key0, key1;
   int32_t split, nsplit;
   // float offsets in the workspace for kv head 0:
-  //   chunk lists:   off0 = lse [Hkv][cols_pad], off1 = (m, l) [Hkv][nsplit][cols_pad][2]
+  //   chunk lists:   off0 = lse [Hkv][cols_pad]; off1 = (m, l) [Hkv][nsplit][cols_pad][2],
+  //                  kListSum: sums [pieces][Hkv][len, padded to kSumKeys]
   //   decode lists:  off0 = logits [Hkv][G][cols_pad], off1 = records [Hkv][nsplit][record]
   int64_t off0, off1;
 };

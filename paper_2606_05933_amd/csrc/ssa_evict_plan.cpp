@@ -24,8 +24,13 @@ constexpr int64_t kFillGroups = 1024;
 // record of G (D + 3) floats.
 constexpr int64_t kDecodeStepKeys = 128;
 constexpr int64_t kDecodeMaxKeys = 4096;
-// A piece of a chunk column tile's key range, at least.
+// A piece of a chunk column tile's key range, at least, and pieces of one, at most.
 constexpr int64_t kLseMinKeys = 256;
+constexpr int64_t kMaxPieces = 64;
+// The chunk passes' estimate.
+constexpr int64_t kCus = 256;
+constexpr double kItemTiles = 3;
+constexpr double kAlone = 1.2;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
@@ -89,32 +94,70 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   // Column groups of the first chunk pass: waves side by side share the keys that
   // go through LDS, waves one behind the other take different ones.  Four groups
   // read LDS and cache least; narrow requests fill fewer columns.
-  int64_t waste[3] = {0, 0, 0}, sums[3] = {0, 0, 0};
-  for (const Chunk& c : chunks)
-    for (int k = 0; k < 3; ++k) {
-      const int64_t tile = (int64_t)kScoreWaveCols << k;
-      waste[k] += round_up(c.cols, tile) * c.span * (12 - k) / 10;
-      sums[k] += ceil_div(c.span, tile) * hkv;
-    }
-  int lse_k = 2, sum_k = 2;
+  int64_t waste[3] = {0, 0, 0}, longest = 0, widest = 0;
+  for (const Chunk& c : chunks) {
+    for (int k = 0; k < 3; ++k)
+      waste[k] += round_up(c.cols, (int64_t)kScoreWaveCols << k) * c.span * (12 - k) / 10;
+    longest = std::max(longest, c.span);
+    widest = std::max(widest, c.cols);
+  }
+  int lse_k = 2;
   for (int k = 1; k >= 0; --k)
     if (waste[k] < waste[lse_k]) lse_k = k;
-  // The second pass: a tile of keys stays in registers, all columns go through LDS.
-  // Narrower tiles where wide ones do not fill the chip.
-  while (sum_k > 0 && sums[sum_k] < kFillGroups / 2) --sum_k;
+  const int64_t lse_cols = (int64_t)kScoreWaveCols << lse_k;
+  // Its pieces of the key ranges are cut for the shortest estimate: the workgroups of the busiest compute unit times their 32-row
+  // tiles, kItemTiles for starting one, and kAlone more where there are not two to a
+  // unit to fill each other's waits.
+  auto estimate = [&](int64_t wgs, double tiles) {
+    const int64_t per_cu = std::max<int64_t>(1, ceil_div(wgs, kCus));
+    return (double)per_cu * (tiles + kItemTiles) * (per_cu == 1 ? kAlone : 1.0);
+  };
+  int64_t piece = kLseMaxKeys;
+  double best = 0;
+  for (int64_t n = 1; n <= kMaxPieces && !chunks.empty(); ++n) {
+    const int64_t p = std::max(kLseMinKeys, round_up(ceil_div(longest, n), 128));
+    if (p > kLseMaxKeys) continue;
+    int64_t wgs = 0;
+    double tiles = 0;
+    for (const Chunk& c : chunks) {
+      const int64_t w = ceil_div(c.cols, lse_cols) * ceil_div(c.span, p) * hkv;
+      wgs += w;
+      tiles += (double)w * std::min(p, c.span) / (32 * (4 >> lse_k));
+    }
+    const double cost = estimate(wgs, tiles / wgs);
+    if (best == 0 || cost < best) {
+      best = cost;
+      piece = p;
+    }
+  }
+  // The second pass: 256 keys stay in registers, columns go through LDS.  Its column
+  // ranges, by the same estimate over tiles of equal length and one item's time for
+  // the end.
+  int64_t sum_cols = 32;
+  best = 0;
+  for (int64_t n = 1; n <= kMaxPieces && !chunks.empty(); ++n) {
+    const int64_t p = round_up(ceil_div(widest, n), 32);
+    double wgs = 0, tiles = 0;
+    for (const Chunk& c : chunks) {
+      const double k = (double)ceil_div(c.span, kSumKeys) * hkv;
+      wgs += k * ceil_div(c.cols, p);
+      tiles += k * c.cols / 32;
+    }
+    const double cost = std::max(1.0, std::ceil(wgs / kCus) * kCus / wgs) * (tiles + wgs * kItemTiles) / kCus +
+                        p / 32 + kItemTiles;
+    if (best == 0 || cost < best) {
+      best = cost;
+      sum_cols = p;
+    }
+  }
   h.lse_groups = 1 << lse_k;
-  h.sum_groups = 1 << sum_k;
-  const int64_t lse_cols = (int64_t)kScoreWaveCols << lse_k, sum_keys = (int64_t)kScoreWaveCols << sum_k;
-  // keys of a piece such that the first pass has about kFillGroups workgroups
-  int64_t tile_keys = 0;
-  for (const Chunk& c : chunks) tile_keys += ceil_div(c.cols, lse_cols) * c.span * hkv;
-  const int64_t piece = std::min<int64_t>(
-      kLseMaxKeys, std::max(kLseMinKeys, round_up(ceil_div(tile_keys, kFillGroups), 128)));
+  h.sum_cols = (int32_t)sum_cols;
   const int64_t decode_piece =
       std::min(kDecodeMaxKeys, std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
                                                                   kDecodeStepKeys)));
 
   int64_t ws = 0, row = 0;  // floats; token row
+  std::vector<ScoreItem> sums;  // a chunk request's fields each
   auto take = [&](int64_t floats) {
     const int64_t at = ws;
     ws += round_up(floats, 64);
@@ -128,7 +171,6 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     ScoreItem it{};
     it.req = i;
     it.q_row = (int32_t)(row + c - r);
-    it.limit0 = (int32_t)(len - r);
     it.rows = (int32_t)r;
     it.len = (int32_t)len;
     it.ctx_len = (int32_t)u;
@@ -174,13 +216,42 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
         x.col0 = (int32_t)col;
         p->list[kListLseJoin].push_back(x);
       }
-    for (int64_t k = 0; k < len; k += sum_keys) {
-      ScoreItem x = it;
-      x.key0 = (int32_t)k;
-      x.key1 = (int32_t)std::min(len, k + sum_keys);
-      p->list[kListSum].push_back(x);
+    sums.push_back(it);
+  }
+  std::stable_sort(sums.begin(), sums.end(),
+                   [](const ScoreItem& a, const ScoreItem& b) { return a.rows > b.rows; });
+  int64_t tickets = 0;
+  for (const ScoreItem& it : sums) {
+    // tiles from the first key on (the most rows see those), each column range that
+    // sees some of the tile
+    const int64_t cols = (int64_t)it.rows * g, pieces = ceil_div(cols, sum_cols);
+    const int64_t off = pieces > 1 ? take(pieces * hkv * round_up(it.len, kSumKeys)) : 0;
+    for (int64_t k = 0; k < it.len; k += kSumKeys) {
+      const int64_t first = std::max<int64_t>(0, k - (it.len - it.rows)) * g / sum_cols;
+      for (int64_t c = first; c < pieces; ++c) {
+        ScoreItem x = it;
+        x.key0 = (int32_t)k;
+        x.key1 = (int32_t)std::min<int64_t>(it.len, k + kSumKeys);
+        x.col0 = (int32_t)(c * sum_cols);
+        x.split = (int32_t)(c - first);
+        x.nsplit = (int32_t)(pieces - first);
+        x.off1 = off;
+        if (x.nsplit > 1) x.ticket = (int32_t)tickets;
+        p->list[kListSum].push_back(x);
+      }
+      if (pieces - first > 1) tickets += hkv;
+      if (tickets > INT32_MAX / 4) return SSA_ERR_LENGTH;
     }
   }
+  h.num_tickets = (int32_t)tickets;
+  // the tickets come first in the workspace
+  const int64_t shift = round_up(tickets, 64);
+  ws += shift;
+  for (auto& l : p->list)
+    for (ScoreItem& x : l) {
+      x.off0 += shift;
+      x.off1 += shift;
+    }
   h.magic = kScoreMagic;
   h.last_rows = last_rows;
   h.num_reqs = n;
@@ -199,7 +270,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   int64_t items = 0;
   for (int l = 0; l < kNumScoreLists; ++l) {
     const int64_t count = (int64_t)p->list[l].size();
-    if (items + count > INT32_MAX || count * hkv > INT32_MAX) return SSA_ERR_LENGTH;
+    if ((items + count) * hkv > INT32_MAX) return SSA_ERR_LENGTH;  // workgroups of a launch
     h.first[l] = (int32_t)items;
     h.count[l] = (int32_t)count;
     items += count;
@@ -213,7 +284,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     hv = fnv1a(hv, ctx_len, sizeof(int32_t) * n);
   }
   // how the lists are cut is this planner's own
-  const int64_t cut[4] = {items, h.ws_bytes, h.lse_groups, h.sum_groups};
+  const int64_t cut[4] = {items, h.ws_bytes, h.lse_groups, h.sum_cols};
   h.hash = fnv1a(hv, cut, sizeof cut);
   return SSA_OK;
 }

@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/ssa_evict.h"
 #include "ssa_device.h"
@@ -45,10 +46,13 @@ constexpr float kLog2e = 1.44269504088896340736f;
 struct ScoreArgs {
   const uint8_t* plan;
   uint64_t hash;
-  int64_t off_items;  // byte offset of the list's first item
-  int32_t workgroups;
+  // the launch's items: chunk items, then items of requests with one counted row
+  int64_t off_chunk, off_decode;  // byte offsets of the lists
+  int32_t chunk_groups, workgroups;
+  int32_t sum_cols, num_tickets;
   int32_t hq, hkv, g, maxp;
-  uint32_t g_magic;  // ceil(2^32 / g)
+  uint32_t g_magic;    // ceil(2^32 / g)
+  int32_t g_magic12;   // ceil(2^12 / g): exact for x < 32
   float c;           // softmax scale times log2(e)
   float decay;
   const uint16_t* q;
@@ -69,12 +73,21 @@ __device__ __forceinline__ int div_g(const ScoreArgs& a, int x) {
 
 // The workgroup's item and kv head; false: nothing to do (past the grid's end, or
 // another plan than the host's lies at plan_dev).
-__device__ __forceinline__ bool take_item(const ScoreArgs& a, const ScoreItem** item, int* kvh) {
-  const int wg = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+struct Work {
+  ScoreItem it;
+  int kvh;
+  bool chunk;
+};
+__device__ __forceinline__ bool take_item(const ScoreArgs& a, Work* w) {
+  int wg = (int)(blockIdx.y * gridDim.x + blockIdx.x);
   if (wg >= a.workgroups) return false;
-  *kvh = wg % a.hkv;
-  *item = reinterpret_cast<const ScoreItem*>(a.plan + a.off_items) + wg / a.hkv;
-  const ScoreHeader* h = reinterpret_cast<const ScoreHeader*>(a.plan);
+  w->chunk = wg < a.chunk_groups;
+  if (!w->chunk) wg -= a.chunk_groups;
+  w->kvh = wg % a.hkv;
+  const auto h = as_uniform<ScoreHeader>(a.plan);
+  const auto it = as_uniform<ScoreItem>(a.plan + (w->chunk ? a.off_chunk : a.off_decode)) + wg / a.hkv;
+  w->it = ScoreItem{it->req,      it->q_row, it->ticket, it->rows,  it->len,    it->ctx_len, it->col0,
+                    it->cols_pad, it->key0,  it->key1,   it->split, it->nsplit, it->off0,    it->off1};
   return h->magic == kScoreMagic && h->hash == a.hash;
 }
 
@@ -111,18 +124,20 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // consecutive keys of one column (head), which is also the layout of the B operand
 // of the P V product: no data moves between lanes but the block's maximum.
 template <int D, bool OUT>
-__global__ __launch_bounds__(kScoreThreads, OUT ? 3 : 4) void score_decode_kernel(ScoreArgs a) {
+struct DecodeLds {
+  float ml[3][4][16];
+  __attribute__((aligned(16))) float o[OUT ? 4 * 16 * D : 4];
+};
+template <int D, bool OUT>
+__device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
+                                            DecodeLds<D, OUT>& lds) {
   constexpr int KS = D / 32, DT = D / 16;
-  __shared__ float s_ml[3][4][16];
-  __shared__ __attribute__((aligned(16))) float s_o[OUT ? 4 * 16 * D : 4];
-  const ScoreItem* itp;
-  int kvh;
-  if (!take_item(a, &itp, &kvh)) return;
-  const ScoreItem it = *itp;
+  auto& s_ml = lds.ml;
+  float* const s_o = lds.o;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, quad = lane >> 4;
-  const int32_t* row = a.bt + (size_t)it.req * a.maxp;
+  const auto row = as_uniform<int32_t>(a.bt + (size_t)it.req * a.maxp);
   const int last_page = (it.len - 1) / 16;
 
   bf16x8 qf[KS];
@@ -272,13 +287,13 @@ __global__ __launch_bounds__(kScoreThreads, OUT ? 3 : 4) void score_decode_kerne
 
 // One counted row: join the key ranges' sums, turn a range's logits into scores;
 // the first range's workgroup also joins the attention output.
+struct JoinLds {
+  float m[16], inv[16], inv_r[16];
+};
 template <int D, bool OUT>
-__global__ __launch_bounds__(kScoreThreads) void score_decode_join_kernel(ScoreArgs a) {
-  __shared__ float s_m[16], s_inv[16], s_inv_r[16];
-  const ScoreItem* itp;
-  int kvh;
-  if (!take_item(a, &itp, &kvh)) return;
-  const ScoreItem it = *itp;
+__device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
+                                                 JoinLds& lds) {
+  auto &s_m = lds.m, &s_inv = lds.inv, &s_inv_r = lds.inv_r;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int stride = score_rec_floats(a.g, D);
   const float* recs = a.ws + it.off1 + (int64_t)kvh * it.nsplit * stride;
@@ -348,12 +363,15 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
 }
 
+constexpr int kTiles = kScoreWaveCols / 32;
+
 template <int D, int NC>
 struct ChunkCfg {
   static constexpr int RG = 4 / NC;             // row groups
   static constexpr int ROWS = 32 * RG;          // streamed rows of a stage
   static constexpr int ROWB = D * 2;
   static constexpr int CPR = D / 8;             // 16-byte pieces of a row
+  static constexpr int RPD = 64 / CPR;          // rows of one copy instruction
   static constexpr int STAGE = ROWS * ROWB;
   static constexpr int NB = NC == 1 ? 2 : 3;    // stages in LDS
   static constexpr int LOADS = ROWS * CPR / kScoreThreads;  // copies of a wave per stage
@@ -361,139 +379,226 @@ struct ChunkCfg {
   static constexpr int COLS = kScoreWaveCols * NC;  // stationary vectors of a workgroup
 };
 
-// Issue one stage's copies: `src(row)` is the address of streamed row `row`.
-template <class C, class F>
-__device__ __forceinline__ void stage_rows(const char* buf, int wave, int lane, F src) {
+// A wave copies LOADS x RPD rows of a stage, RPD at a time: copy i starts at the
+// stage's row copy_row(wave, i).  Lane n takes piece n % CPR of row n / CPR, from the
+// permuted place; copy_offset is its byte offset from the first row where rows lie one
+// after the other.
+template <class C>
+__device__ __forceinline__ int copy_row(int wave, int i) {
+  return (wave * C::LOADS + i) * C::RPD;
+}
+template <class C>
+__device__ __forceinline__ uint32_t copy_offset(int lane, int row0) {
+  const int row = lane / C::CPR;
+  const uint32_t first = row * C::ROWB + ((lane % C::CPR) ^ (row & (C::CPR - 1))) * 16;
+  return first ^ (uint32_t)((row0 & (C::CPR - 1)) * 16);  // row0 is a multiple of RPD
+}
+
+// Where a lane reads the fragments of its row of the first stage.
+template <int D, int NC>
+__device__ __forceinline__ void fragment_addresses(const char* buf, int rg, int lane,
+                                                   const char* (&at)[D / 16]) {
+  using C = ChunkCfg<D, NC>;
 #pragma unroll
-  for (int i = 0; i < C::LOADS; ++i) {
-    const int p = (wave * C::LOADS + i) * 64 + lane;
-    const int row = p / C::CPR, piece = p % C::CPR;
-    dma16(src(row) + (piece ^ (row & (C::CPR - 1))) * 8, buf + (wave * C::LOADS + i) * 1024);
+  for (int s = 0; s < C::KS; ++s)
+    at[s] = buf + (rg * 32 + (lane & 31)) * C::ROWB +
+            ((2 * s + (lane >> 5)) ^ (lane & (C::CPR - 1))) * 16;
+}
+
+// Run `stage(k, buffer)` for k = 0 .. stages - 1, the buffer k % NB a constant of each
+// copy of the body: LDS addresses are then a register and an immediate.
+template <int NB, class F>
+__device__ __forceinline__ void for_stages(int stages, F stage) {
+  for (int k = 0; k < stages; k += NB) {
+    stage(k, std::integral_constant<int, 0>{});
+    if (k + 1 >= stages) break;
+    stage(k + 1, std::integral_constant<int, 1>{});
+    if constexpr (NB == 3) {
+      if (k + 2 >= stages) break;
+      stage(k + 2, std::integral_constant<int, 2>{});
+    }
   }
 }
 
+// One 32-row tile's products with the wave's 64 vectors.  All of the tile's
+// fragments are on their way before the first product.
 template <int D, int NC>
-__device__ __forceinline__ void tile_products(const char* buf, int rg, int lane,
+__device__ __forceinline__ void tile_products(const char* const (&at)[D / 16], int offset,
                                               const bf16x8 (*st)[D / 16], f32x16* acc) {
   using C = ChunkCfg<D, NC>;
-  const int half = lane >> 5;
-  const char* at = buf + (rg * 32 + (lane & 31)) * C::ROWB;
+  bf16x8 x[C::KS];
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int s = 0; s < C::KS; ++s) x[s] = as_bf16x8(ld16(at[s] + offset));
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+  for (int t = 0; t < kTiles; ++t) acc[t] = f32x16{};
 #pragma unroll
-  for (int s = 0; s < C::KS; ++s) {
-    const bf16x8 x = as_bf16x8(ld16(at + ((2 * s + half) ^ (lane & (C::CPR - 1))) * 16));
-    acc[0] = mfma32(x, st[0][s], acc[0]);
-    acc[1] = mfma32(x, st[1][s], acc[1]);
+  for (int s = 0; s < C::KS; ++s)
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) acc[t] = mfma32(x[s], st[t][s], acc[t]);
+  __builtin_amdgcn_s_setprio(0);
+}
+
+__device__ __forceinline__ float sum16(float* p) {
+#pragma unroll
+  for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+    for (int i = 0; i < w; ++i) p[i] += p[i + w];
+  return p[0];
+}
+// row of a tile that register i of a lane holds, less 4 (lane / 32)
+__device__ __forceinline__ constexpr int tile_row(int i) { return (i & 3) + 8 * (i >> 2); }
+
+// The first guess at a tile's exponentials may be this much over 1 (the sum of them
+// is far from overflow); past it the column's reference is raised.
+constexpr float kRaise = 0x1p40f;
+
+// A column's reference m and the sum l of 2^(t - m) over one more tile.  m is a
+// maximum over some of the keys, not all: exponentials are formed against it as it
+// is, which saves the maximum over the tile, and only a tile that has one of over
+// 2^40 raises it.  L = m + log2(l) does not depend on m.
+__device__ __forceinline__ void lse_add(const f32x16& x, float c, float* m, float* l) {
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = exp2_fast(__builtin_fmaf(x[i], c, -*m));
+  const float sum = sum16(v);
+  if (__any(!(sum < kRaise))) {
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    const float mn = fmaxf(*m, mx * c);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = exp2_fast(__builtin_fmaf(x[i], c, -mn));
+    *l = *l * exp2_fast(*m - mn) + sum16(v);
+    *m = mn;
+  } else {
+    *l += sum;
   }
 }
 
+// The same with the maximum taken first, for the first tile and for MASK: rows past
+// `limit` are not seen.
+__device__ __forceinline__ void lse_update(const f32x16& x, float c, int limit, float* m, float* l) {
+  float v[16], mx = -kInf;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = tile_row(i) > limit ? -kInf : x[i];
+    mx = fmaxf(mx, v[i]);
+  }
+  // nothing seen: the maximum stays, and may be -inf
+  const float mn = mx == -kInf ? *m : fmaxf(*m, mx * c);
+  const float ms = mn == -kInf ? 0.f : mn;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = exp2_fast(__builtin_fmaf(v[i], c, -ms));
+    if (tile_row(i) > limit) v[i] = 0.f;  // scale 0 times -inf is NaN
+  }
+  *l = *l * exp2_fast(*m - ms) + sum16(v);
+  *m = mn;
+}
+
 template <int D, int NC>
-__global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(ScoreArgs a) {
+struct LseLds {
   using C = ChunkCfg<D, NC>;
-  __shared__ __attribute__((aligned(16))) char s_buf[C::NB * C::STAGE];
-  __shared__ int s_pages[kLseMaxKeys / 16];
-  __shared__ float s_m[C::RG][C::COLS], s_l[C::RG][C::COLS];
-  const ScoreItem* itp;
-  int kvh;
-  if (!take_item(a, &itp, &kvh)) return;
-  const ScoreItem it = *itp;
+  __attribute__((aligned(16))) char buf[C::NB * C::STAGE];
+  float m[C::RG][C::COLS], l[C::RG][C::COLS];
+};
+template <int D, int NC>
+__device__ __forceinline__ void lse_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
+                                         LseLds<D, NC>& lds) {
+  using C = ChunkCfg<D, NC>;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cg = wave % NC, rg = wave / NC, half = lane >> 5;
-  const int ncols = it.rows * a.g;
-  const int first_limit = it.limit0 + div_g(a, it.col0);
-  const int last_limit = it.limit0 + div_g(a, min(it.col0 + C::COLS, ncols) - 1);
+  const int ncols = it.rows * a.g, limit0 = it.len - it.rows;
+  const int first_limit = limit0 + div_g(a, it.col0);
+  const int last_limit = limit0 + div_g(a, min(it.col0 + C::COLS, ncols) - 1);
   const int kend = min(it.key1, last_limit + 1);  // keys past it are seen by no column
 
-  for (int i = tid; i < (kend - it.key0 + 15) / 16; i += kScoreThreads)
-    s_pages[i] = a.bt[(size_t)it.req * a.maxp + it.key0 / 16 + i];
-  bf16x8 st[2][C::KS];
-  int limit[2];
+  bf16x8 st[kTiles][C::KS];
+  int limit[kTiles];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int n = min(it.col0 + cg * 64 + t * 32 + (lane & 31), ncols - 1);
+  for (int t = 0; t < kTiles; ++t) {
+    const int n = min(it.col0 + cg * kScoreWaveCols + t * 32 + (lane & 31), ncols - 1);
     const int j = div_g(a, n);
-    limit[t] = it.limit0 + j;
+    limit[t] = min(limit0 + j, kend - 1) - 4 * half;
     const uint16_t* p =
         a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D + half * 8;
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) st[t][s] = as_bf16x8(ld16(p + s * 16));
   }
-  float m[2] = {-kInf, -kInf}, l[2] = {0.f, 0.f};
-  __syncthreads();
+  float m[kTiles], l[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    m[t] = -kInf;
+    l[t] = 0.f;
+  }
 
   const int stages = kend > it.key0 ? (kend - it.key0 + C::ROWS - 1) / C::ROWS : 0;
-  auto issue = [&](int k) {
-    const int kb = it.key0 + k * C::ROWS;
-    stage_rows<C>(s_buf + (k % C::NB) * C::STAGE, wave, lane, [&](int row) {
-      const int key = min(kb + row, kend - 1);
-      return a.kc + (((size_t)s_pages[(key - it.key0) >> 4] * a.hkv + kvh) * 16 + (key & 15)) * D;
-    });
+  // Rows past kend are copied as they lie in the last page (and are not seen): whole
+  // pages are there to read.
+  const auto row = as_uniform<int32_t>(a.bt + (size_t)it.req * a.maxp);
+  // A wave's rows of a stage lie in NP pages, named one stage ahead.
+  constexpr int RPW = C::LOADS * C::RPD, NP = RPW < 16 ? 1 : RPW / 16;
+  const int page0 = it.key0 / 16 + wave * RPW / 16, last_page = (kend - 1) / 16;
+  int page[NP];
+  auto name_pages = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) page[i] = row[min(page0 + k * (C::ROWS / 16) + i, last_page)];
   };
+  auto issue = [&](int k) {
+    char* buf = lds.buf + (k % C::NB) * C::STAGE;
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) {
+      const int row0 = copy_row<C>(wave, i);
+      dma16_base(a.kc + (((size_t)page[i * C::RPD / 16] * a.hkv + kvh) * 16 + row0 % 16) * D,
+                 copy_offset<C>(lane, row0), buf + row0 * C::ROWB);
+    }
+    name_pages(k + 1);
+  };
+  if (stages > 0) name_pages(0);
   vm_wait<0>();  // the stationary vectors have landed: the waits below count copies only
 #pragma unroll
   for (int k = 0; k < C::NB - 1; ++k)
     if (k < stages) issue(k);
-  for (int k = 0; k < stages; ++k) {
+  const char* at[C::KS];
+  fragment_addresses<D, NC>(lds.buf, rg, lane, at);
+  for_stages<C::NB>(stages, [&](int k, auto buffer) {
     if (C::NB == 3 && k + 1 < stages)
       vm_wait<C::LOADS>();
     else
       vm_wait<0>();
     __syncthreads();
     if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
-    f32x16 acc[2];
-    tile_products<D, NC>(s_buf + (k % C::NB) * C::STAGE, rg, lane, st, acc);
+    f32x16 acc[kTiles];
+    tile_products<D, NC>(at, buffer() * C::STAGE, st, acc);
     const int kb = it.key0 + k * C::ROWS + rg * 32;
-    const bool whole = kb + 31 <= first_limit && kb + 32 <= kend;
+    if (k > 0 && kb + 31 <= first_limit && kb + 32 <= kend) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (!whole) {
-        const int lim = min(limit[t], kend - 1) - kb - 4 * half;
+      for (int t = 0; t < kTiles; ++t) lse_add(acc[t], a.c, &m[t], &l[t]);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if ((i & 3) + 8 * (i >> 2) > lim) acc[t][i] = -kInf;
-      }
-      float mx = acc[t][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, acc[t][i]);
-      const float mn = mx == -kInf ? m[t] : fmaxf(m[t], mx * a.c);
-      const float ms = mn == -kInf ? 0.f : mn;
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -ms));
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (acc[t][i] == -kInf) p[i] = 0.f;  // scale 0 times -inf is NaN
-      }
-#pragma unroll
-      for (int w = 8; w > 0; w >>= 1)
-#pragma unroll
-        for (int i = 0; i < w; ++i) p[i] += p[i + w];
-      l[t] = l[t] * exp2_fast(m[t] - ms) + p[0];
-      m[t] = mn;
+      for (int t = 0; t < kTiles; ++t) lse_update(acc[t], a.c, limit[t] - kb, &m[t], &l[t]);
     }
-  }
+  });
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     const float m2 = __shfl_xor(m[t], 32, 64), l2 = __shfl_xor(l[t], 32, 64);
     const float mm = fmaxf(m[t], m2), ms = mm == -kInf ? 0.f : mm;
     if (half == 0) {
-      s_m[rg][cg * 64 + t * 32 + lane] = mm;
-      s_l[rg][cg * 64 + t * 32 + lane] = l[t] * exp2_fast(m[t] - ms) + l2 * exp2_fast(m2 - ms);
+      lds.m[rg][cg * kScoreWaveCols + t * 32 + lane] = mm;
+      lds.l[rg][cg * kScoreWaveCols + t * 32 + lane] = l[t] * exp2_fast(m[t] - ms) + l2 * exp2_fast(m2 - ms);
     }
   }
   __syncthreads();
   if (tid < C::COLS) {
     float mm = -kInf, ll = 0.f;
 #pragma unroll
-    for (int r = 0; r < C::RG; ++r) mm = fmaxf(mm, s_m[r][tid]);
+    for (int r = 0; r < C::RG; ++r) mm = fmaxf(mm, lds.m[r][tid]);
     const float ms = mm == -kInf ? 0.f : mm;
 #pragma unroll
-    for (int r = 0; r < C::RG; ++r) ll += s_l[r][tid] * exp2_fast(s_m[r][tid] - ms);
+    for (int r = 0; r < C::RG; ++r) ll += lds.l[r][tid] * exp2_fast(lds.m[r][tid] - ms);
     const int n = it.col0 + tid;
     if (it.nsplit > 1) {
       if (n < it.cols_pad) {
@@ -511,11 +616,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(ScoreArgs a
 }
 
 // L of 256 columns from the pieces of a cut key range.
-__global__ __launch_bounds__(kScoreThreads) void score_lse_join_kernel(ScoreArgs a) {
-  const ScoreItem* itp;
-  int kvh;
-  if (!take_item(a, &itp, &kvh)) return;
-  const ScoreItem it = *itp;
+__device__ __forceinline__ void lse_join_item(const ScoreArgs& a, const ScoreItem& it, int kvh) {
   const int n = it.col0 + (int)threadIdx.x;  // < cols_pad, a multiple of 256
   float* to = a.ws + it.off0 + (int64_t)kvh * it.cols_pad + n;
   if (n >= it.rows * a.g) {
@@ -534,107 +635,201 @@ __global__ __launch_bounds__(kScoreThreads) void score_lse_join_kernel(ScoreArgs
   *to = m + __builtin_amdgcn_logf(l);
 }
 
-template <int D, int NC>
-__global__ __launch_bounds__(kScoreThreads, 2) void score_sum_kernel(ScoreArgs a) {
+template <int D>
+struct SumLds {
+  using C = ChunkCfg<D, 4>;
+  __attribute__((aligned(16))) char buf[C::NB * C::STAGE];
+  __attribute__((aligned(16))) float lse[C::NB][4][32];  // one copy a wave
+  __attribute__((aligned(16))) float sum[C::COLS];
+  int last;
+};
+template <int D>
+__device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
+                                         SumLds<D>& lds) {
+  constexpr int NC = 4;
   using C = ChunkCfg<D, NC>;
-  __shared__ __attribute__((aligned(16))) char s_buf[C::NB * C::STAGE];
-  __shared__ __attribute__((aligned(16))) float s_lse[C::NB][4][32];  // one copy a wave
-  __shared__ float s_sum[C::RG][C::COLS];
-  const ScoreItem* itp;
-  int kvh;
-  if (!take_item(a, &itp, &kvh)) return;
-  const ScoreItem it = *itp;
+  static_assert(C::RG == 1 && C::COLS == kSumKeys, "one row group");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cg = wave % NC, rg = wave / NC, half = lane >> 5;
-  const int ncols = it.rows * a.g;
+  const int half = lane >> 5;
+  const int ncols = min(it.rows * a.g, it.col0 + a.sum_cols), limit0 = it.len - it.rows;
   // columns of earlier rows see none of these keys
-  const int n0 = max(0, it.key0 - it.limit0) * a.g / C::ROWS * C::ROWS;
+  const int n0 = max(it.col0, max(0, it.key0 - limit0) * a.g / C::ROWS * C::ROWS);
   const int stages = (ncols - n0 + C::ROWS - 1) / C::ROWS;
 
-  bf16x8 st[2][C::KS];
-  int key[2];
+  // sums of 16 tiles, then the sums of those: few terms that differ much in size
+  float sum[kTiles] = {}, total[kTiles] = {};
+  const float* lse = a.ws + it.off0 + (int64_t)kvh * it.cols_pad;
+  auto issue = [&](int k) {
+    const int nb = n0 + k * C::ROWS;
+    char* buf = lds.buf + (k % C::NB) * C::STAGE;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    key[t] = it.key0 + cg * 64 + t * 32 + (lane & 31);
+    for (int i = 0; i < C::LOADS; ++i) {
+      const int row0 = copy_row<C>(wave, i), n = nb + row0, j = div_g(a, n);
+      const uint16_t* p = a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D;
+      // a lane's row is `more` heads on, or in a later token
+      const int more = min(lane / C::CPR, max(0, ncols - 1 - n));
+      const int wrap = ((n - j * a.g + more) * a.g_magic12) >> 12;
+      if (n < ncols)
+        dma16_base(p, copy_offset<C>(lane, row0) + (more - lane / C::CPR + wrap * (a.hq - a.g)) * C::ROWB,
+                   buf + row0 * C::ROWB);
+      else  // past the last column: any row of the request
+        dma16_base(a.q + ((size_t)it.q_row * a.hq + kvh * a.g) * D, copy_offset<C>(lane, row0) % C::ROWB,
+                   buf + row0 * C::ROWB);
+    }
+    if (lane < 8)
+      dma16(lse + nb + lane * 4,
+            reinterpret_cast<const char*>(&lds.lse[k % C::NB][wave][0]));
+  };
+#pragma unroll
+  for (int k = 0; k < C::NB - 1; ++k)
+    if (k < stages) issue(k);
+  bf16x8 st[kTiles][C::KS];
+  int key[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    key[t] = it.key0 + wave * kScoreWaveCols + t * 32 + (lane & 31);
     const int k = min(key[t], it.len - 1);
     const int page = a.bt[(size_t)it.req * a.maxp + k / 16];
     const uint16_t* p = a.kc + (((size_t)page * a.hkv + kvh) * 16 + k % 16) * D + half * 8;
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) st[t][s] = as_bf16x8(ld16(p + s * 16));
   }
-  // sums of 16 tiles, then the sums of those: few terms that differ much in size
-  float sum[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
-  const float* lse = a.ws + it.off0 + (int64_t)kvh * it.cols_pad;
-  auto issue = [&](int k) {
-    const int nb = n0 + k * C::ROWS;
-    stage_rows<C>(s_buf + (k % C::NB) * C::STAGE, wave, lane, [&](int row) {
-      const int n = min(nb + row, ncols - 1), j = div_g(a, n);
-      return a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D;
-    });
-    if (lane < 8)
-      dma16(lse + nb + rg * 32 + lane * 4,
-            reinterpret_cast<const char*>(&s_lse[k % C::NB][wave][0]));
-  };
-  vm_wait<0>();  // the stationary vectors have landed: the waits below count copies only
-#pragma unroll
-  for (int k = 0; k < C::NB - 1; ++k)
-    if (k < stages) issue(k);
-  for (int k = 0; k < stages; ++k) {
+  vm_wait<0>();  // all of it has landed: the waits below count later copies only
+  const char* at[C::KS];
+  fragment_addresses<D, NC>(lds.buf, 0, lane, at);
+  const float* lse_at = &lds.lse[0][wave][4 * half];
+  for_stages<C::NB>(stages, [&](int k, auto buffer) {
     if (C::NB == 3 && k + 1 < stages)
       vm_wait<C::LOADS + 1>();
     else
       vm_wait<0>();
     __syncthreads();
     if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
-    f32x16 acc[2];
-    tile_products<D, NC>(s_buf + (k % C::NB) * C::STAGE, rg, lane, st, acc);
-    const int nb = n0 + k * C::ROWS + rg * 32;
+    f32x16 acc[kTiles];
     f32x4 lv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      lv[i] = *reinterpret_cast<const f32x4*>(&s_lse[k % C::NB][wave][8 * i + 4 * half]);
-    const bool whole = it.limit0 + div_g(a, nb) >= it.key0 + C::COLS - 1;
+      lv[i] = *reinterpret_cast<const f32x4*>(lse_at + buffer() * 128 + 8 * i);
+    tile_products<D, NC>(at, buffer() * C::STAGE, st, acc);
+    const int nb = n0 + k * C::ROWS;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      float p[16];
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        p[i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -lv[i >> 2][i & 3]));
-      if (!whole) {
+        acc[t][i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -lv[i >> 2][i & 3]));
+    if (limit0 + div_g(a, nb) < it.key0 + C::COLS - 1) {  // some row does not see some key
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (it.limit0 + div_g(a, nb + (i & 3) + 8 * (i >> 2) + 4 * half) < key[t]) p[i] = 0.f;
+      for (int i = 0; i < 16; ++i) {
+        const int limit = limit0 + div_g(a, nb + tile_row(i) + 4 * half);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+          if (limit < key[t]) acc[t][i] = 0.f;
       }
+    }
 #pragma unroll
-      for (int w = 8; w > 0; w >>= 1)
+    for (int t = 0; t < kTiles; ++t) {
+      float p[16];
 #pragma unroll
-        for (int i = 0; i < w; ++i) p[i] += p[i + w];
-      sum[t] += p[0];
+      for (int i = 0; i < 16; ++i) p[i] = acc[t][i];
+      sum[t] += sum16(p);
     }
     if ((k & 15) == 15) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < kTiles; ++t) {
         total[t] += sum[t];
         sum[t] = 0.f;
       }
     }
-  }
+  });
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     float x = total[t] + sum[t];
     x += __shfl_xor(x, 32, 64);
-    if (half == 0) s_sum[rg][cg * 64 + t * 32 + lane] = x;
+    if (half == 0) lds.sum[wave * kScoreWaveCols + t * 32 + lane] = x;
   }
   __syncthreads();
-  if (tid * 4 < C::COLS && it.key0 + tid * 4 < it.key1) {
-    f32x4 w = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int r = 0; r < C::RG; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] += s_sum[r][tid * 4 + i];
-    add_scores4(a, it, kvh, it.key0 + tid * 4, it.key1, w);
+  f32x4 w = *reinterpret_cast<const f32x4*>(&lds.sum[tid * 4 % C::COLS]);
+  if (it.nsplit > 1) {
+    // One of several column ranges: the last workgroup of the tile to finish adds all
+    // of them in their order.  The sums go past this die's cache (device scope), and
+    // have arrived before the ticket is taken.
+    const int pad = (it.len + C::COLS - 1) / C::COLS * C::COLS;
+    float* part = a.ws + it.off1 + (int64_t)kvh * pad + it.key0 + tid;
+    const int64_t stride = (int64_t)a.hkv * pad;
+    __hip_atomic_store(part + it.split * stride, lds.sum[tid], __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+    vm_wait<0>();
+    __syncthreads();
+    if (tid == 0)
+      lds.last = __hip_atomic_fetch_add(reinterpret_cast<int*>(a.ws) + it.ticket + kvh, 1,
+                                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.nsplit - 1;
+    __syncthreads();
+    if (!lds.last) return;
+    float x = 0.f;
+    for (int k = 0; k < it.nsplit; ++k)
+      x += __hip_atomic_load(part + k * stride, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    lds.sum[tid] = x;
+    __syncthreads();
+    w = *reinterpret_cast<const f32x4*>(&lds.sum[tid * 4 % C::COLS]);
   }
+  if (tid * 4 < C::COLS && it.key0 + tid * 4 < it.key1)
+    add_scores4(a, it, kvh, it.key0 + tid * 4, it.key1, w);
+}
+
+// ---------------------------------------------------------------------------
+// The launches.  A hybrid batch's decode rows, which wait for memory, run beside its
+// chunk tiles, which wait for the matrix and vector units.
+
+template <int D, bool OUT>
+__global__ __launch_bounds__(kScoreThreads, OUT ? 3 : 4) void score_decode_kernel(ScoreArgs a) {
+  __shared__ DecodeLds<D, OUT> lds;
+  Work w;
+  if (take_item(a, &w)) decode_item<D, OUT>(a, w.it, w.kvh, lds);
+}
+
+template <int D, bool OUT>
+__global__ __launch_bounds__(kScoreThreads) void score_decode_join_kernel(ScoreArgs a) {
+  __shared__ JoinLds lds;
+  Work w;
+  if (take_item(a, &w)) decode_join_item<D, OUT>(a, w.it, w.kvh, lds);
+}
+
+template <int D, int NC>
+__global__ __launch_bounds__(kScoreThreads, 2) void score_first_kernel(ScoreArgs a) {
+  __shared__ union {
+    LseLds<D, NC> lse;
+    DecodeLds<D, false> decode;
+  } lds;
+  Work w;
+  if (!take_item(a, &w)) return;
+  // tickets of the second pass
+  for (int64_t i = (int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * kScoreThreads + threadIdx.x;
+       i < a.num_tickets; i += (int64_t)a.workgroups * kScoreThreads)
+    reinterpret_cast<int*>(a.ws)[i] = 0;
+  if (w.chunk)
+    lse_item<D, NC>(a, w.it, w.kvh, lds.lse);
+  else
+    decode_item<D, false>(a, w.it, w.kvh, lds.decode);
+}
+
+__global__ __launch_bounds__(kScoreThreads) void score_lse_join_kernel(ScoreArgs a) {
+  Work w;
+  if (take_item(a, &w)) lse_join_item(a, w.it, w.kvh);
+}
+
+template <int D>
+__global__ __launch_bounds__(kScoreThreads, 2) void score_second_kernel(ScoreArgs a) {
+  __shared__ union {
+    SumLds<D> sum;
+    JoinLds join;
+  } lds;
+  Work w;
+  if (!take_item(a, &w)) return;
+  if (w.chunk)
+    sum_item<D>(a, w.it, w.kvh, lds.sum);
+  else
+    decode_join_item<D, false>(a, w.it, w.kvh, lds.join);
 }
 
 // ---------------------------------------------------------------------------
@@ -644,32 +839,40 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_sum_kernel(ScoreArgs a
 constexpr int kGridRow = 1 << 16;
 
 template <class K>
-int launch(K kernel, ScoreArgs a, const ScoreHeader* h, ScoreList list, hipStream_t stream) {
-  const int64_t wgs = (int64_t)h->count[list] * h->hkv;
+int launch(K kernel, ScoreArgs a, const ScoreHeader* h, int chunk_list, int decode_list,
+           hipStream_t stream) {
+  const int64_t chunks = chunk_list < 0 ? 0 : (int64_t)h->count[chunk_list] * h->hkv;
+  const int64_t decodes = decode_list < 0 ? 0 : (int64_t)h->count[decode_list] * h->hkv;
+  const int64_t wgs = chunks + decodes;
   if (wgs == 0) return SSA_OK;
-  a.off_items = h->off_items + (int64_t)h->first[list] * (int64_t)sizeof(ScoreItem);
+  auto offset = [&](int list) {
+    return list < 0 ? 0 : h->off_items + (int64_t)h->first[list] * (int64_t)sizeof(ScoreItem);
+  };
+  a.off_chunk = offset(chunk_list);
+  a.off_decode = offset(decode_list);
+  a.chunk_groups = (int32_t)chunks;
   a.workgroups = (int32_t)wgs;
   const dim3 grid(wgs < kGridRow ? wgs : kGridRow, (wgs + kGridRow - 1) / kGridRow);
   hipLaunchKernelGGL(kernel, grid, dim3(kScoreThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
 }
 
-template <int D>
-int launch_chunks(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
-  int rc = h->lse_groups == 4   ? launch(score_lse_kernel<D, 4>, a, h, kListLse, s)
-           : h->lse_groups == 2 ? launch(score_lse_kernel<D, 2>, a, h, kListLse, s)
-                                : launch(score_lse_kernel<D, 1>, a, h, kListLse, s);
-  if (rc) return rc;
-  if ((rc = launch(score_lse_join_kernel, a, h, kListLseJoin, s))) return rc;
-  return h->sum_groups == 4   ? launch(score_sum_kernel<D, 4>, a, h, kListSum, s)
-         : h->sum_groups == 2 ? launch(score_sum_kernel<D, 2>, a, h, kListSum, s)
-                              : launch(score_sum_kernel<D, 1>, a, h, kListSum, s);
-}
-
 template <int D, bool OUT>
 int launch_decodes(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
-  const int rc = launch(score_decode_kernel<D, OUT>, a, h, kListDecode, s);
-  return rc ? rc : launch(score_decode_join_kernel<D, OUT>, a, h, kListDecodeJoin, s);
+  const int rc = launch(score_decode_kernel<D, OUT>, a, h, -1, kListDecode, s);
+  return rc ? rc : launch(score_decode_join_kernel<D, OUT>, a, h, -1, kListDecodeJoin, s);
+}
+
+template <int D>
+int launch_scores(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
+  if (h->count[kListSum] == 0) return launch_decodes<D, false>(a, h, s);
+  auto first = h->lse_groups == 4   ? score_first_kernel<D, 4>
+               : h->lse_groups == 2 ? score_first_kernel<D, 2>
+                                    : score_first_kernel<D, 1>;
+  int rc = launch(first, a, h, kListLse, kListDecode, s);
+  if (rc) return rc;
+  if ((rc = launch(score_lse_join_kernel, a, h, kListLseJoin, -1, s))) return rc;
+  return launch(score_second_kernel<D>, a, h, kListSum, kListDecodeJoin, s);
 }
 
 int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_dev,
@@ -688,8 +891,11 @@ int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_de
   a->g = h->hq / h->hkv;
   a->maxp = h->max_pages_per_req;
   a->g_magic = (uint32_t)((((uint64_t)1 << 32) + a->g - 1) / a->g);
+  a->g_magic12 = (4096 + a->g - 1) / a->g;
   a->c = (float)((double)shape->softmax_scale * (double)kLog2e);
   a->decay = decay;
+  a->sum_cols = h->sum_cols;
+  a->num_tickets = h->num_tickets;
   a->q = q;
   a->kc = k_cache;
   a->bt = block_table;
@@ -716,10 +922,7 @@ int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* pl
     return rc;
   (void)hipGetLastError();
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((rc = h->head_dim == 128 ? launch_chunks<128>(a, h, s) : launch_chunks<64>(a, h, s)))
-    return rc;
-  return h->head_dim == 128 ? launch_decodes<128, false>(a, h, s)
-                            : launch_decodes<64, false>(a, h, s);
+  return h->head_dim == 128 ? launch_scores<128>(a, h, s) : launch_scores<64>(a, h, s);
 }
 
 int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void* plan_dev,

@@ -14,10 +14,10 @@ LISTS = ("lse", "decode", "lse_join", "sum", "decode_join")
 HEADER = np.dtype([("magic", "<u4"), ("last_rows", "<i4"), ("hash", "<u8"), ("num_reqs", "<i4"),
                    ("num_tokens", "<i4"), ("hq", "<i4"), ("hkv", "<i4"), ("d", "<i4"),
                    ("page", "<i4"), ("maxp", "<i4"), ("num_pages", "<i4"), ("scale", "<f4"),
-                   ("max_q", "<i4"), ("lse_groups", "<i4"), ("sum_groups", "<i4"),
-                   ("off_items", "<i4"), ("pad", "<i4"), ("count", "<i4", 5), ("first", "<i4", 5),
+                   ("max_q", "<i4"), ("lse_groups", "<i4"), ("sum_cols", "<i4"),
+                   ("off_items", "<i4"), ("num_tickets", "<i4"), ("count", "<i4", 5), ("first", "<i4", 5),
                    ("plan_bytes", "<i8"), ("ws_bytes", "<i8")])
-ITEM = np.dtype([(n, "<i4") for n in ("req", "q_row", "limit0", "rows", "len", "ctx", "col0",
+ITEM = np.dtype([(n, "<i4") for n in ("req", "q_row", "ticket", "rows", "len", "ctx", "col0",
                                       "cols_pad", "key0", "key1", "split", "nsplit")]
                 + [("off0", "<i8"), ("off1", "<i8")])
 assert HEADER.itemsize == 128 and ITEM.itemsize == 64
@@ -52,14 +52,13 @@ def test_score_plans_cover_the_batch_once_and_stay_in_the_workspace(seed):
     assert h["plan_bytes"] == plan.nbytes and h["ws_bytes"] == ws_bytes >= 256
     assert h["num_tokens"] == c.sum() and h["max_q"] == max(c, default=0)
     start = np.cumsum(c) - c
-    taken = []  # workspace ranges, in floats
+    taken, tickets = [], []  # workspace ranges, in floats
     for i in range(len(c)):
         rows = min(c[i], last) if last else c[i]
         mine = {n: x[x["req"] == i] for n, x in items.items()}
         for x in mine.values():
             assert (x["q_row"] == start[i] + c[i] - rows).all() and (x["rows"] == rows).all()
             assert (x["len"] == c[i] + u[i]).all() and (x["ctx"] == u[i]).all()
-            assert (x["limit0"] == c[i] + u[i] - rows).all()
             assert (x["key0"] < x["key1"]).all() or not len(x) or (x is mine["lse_join"])
         used = ("decode", "decode_join") if rows == 1 else ("lse", "lse_join", "sum")
         assert all(not len(mine[n]) for n in LISTS if c[i] == 0 or n not in used)
@@ -93,16 +92,31 @@ def test_score_plans_cover_the_batch_once_and_stay_in_the_workspace(seed):
             partition(x)
             assert len(x) == ns and (x["key0"] % 128 == 0).all()
             assert (x["key1"] - x["key0"] <= 32768).all()
-        partition(mine["sum"])
-        assert (mine["sum"]["key1"] - mine["sum"]["key0"] <= 64 * h["sum_groups"]).all()
-        assert (mine["sum"]["key0"] % (64 * h["sum_groups"]) == 0).all()
+        sums, per = mine["sum"], int(h["sum_cols"])
+        assert per % 32 == 0 and (sums["key0"] % 256 == 0).all()
+        partition(sums[sums["col0"] == sums["col0"].max()])  # the last rows see every key
+        pieces = -(-cols // per)
+        for k in set(sums["key0"]):
+            # the column ranges from the first row that sees the tile on
+            x = np.sort(sums[sums["key0"] == k], order="col0")
+            first = max(0, k - (length - rows)) * g // per
+            assert x["col0"].tolist() == [per * p for p in range(first, pieces)]
+            assert x["split"].tolist() == list(range(len(x))) and (x["nsplit"] == len(x)).all()
+            assert len(set(x["key1"])) == 1 and x["key1"][0] == min(length, k + 256)
+            if len(x) > 1:
+                tickets += list(range(x["ticket"][0], x["ticket"][0] + hkv))
+                assert len(set(x["ticket"])) == 1
+        if pieces > 1:
+            taken.append((int(sums["off1"][0]), pieces * hkv * -(-length // 256) * 256))
         taken.append((int(lse["off0"][0]), hkv * pad))
         if ns > 1:
             assert sorted(mine["lse_join"]["col0"]) == list(range(0, pad, 256))
             taken.append((int(lse["off1"][0]), hkv * ns * pad * 2))
         else:
             assert not len(mine["lse_join"])
+    assert sorted(tickets) == list(range(h["num_tickets"]))
     taken.sort()
+    assert not taken or taken[0][0] >= h["num_tickets"]
     for (a, n), (b, _) in zip(taken, taken[1:]):
         assert a + n <= b
     assert all(a % 64 == 0 for a, _ in taken)

@@ -179,23 +179,24 @@ def test_chunks(torch_dev, c, u, heads, q_scale):
     x = Scored(torch_dev, batch(*heads, c, u, seed=6), q_scale=q_scale)
     x.scores()
     torch_dev.cuda.synchronize()
-    say("    scores", x.check_scores(), "groups", x.plan[:128].view(np.int32)[14:16])
+    say("    scores", x.check_scores(), "groups, sum_cols", x.plan[:128].view(np.int32)[14:16])
 
 
-def test_every_width_of_tile_runs(torch_dev):
-    """Both passes in tiles of 64, 128 and 256 columns, D 64 and 128: the planner's
-    choices over batches of different sizes."""
+def test_every_width_and_cut_runs(torch_dev):
+    """The first pass in tiles of 64, 128 and 256 columns, the second with and without
+    cut column ranges, D 64 and 128: batches for which the planner chooses each."""
     seen = set()
     for d in (64, 128):
-        for hq, hkv, c, u in ((2, 2, 20, 100), (4, 2, 40, 2000), (8, 8, 100, 4000), (8, 4, 512, 200),
-                              (16, 16, 130, 4500), (16, 16, 60, 9000)):
+        for hq, hkv, c, u in ((2, 2, 20, 100), (4, 2, 60, 2000), (8, 8, 100, 4000), (8, 4, 512, 200),
+                              (16, 16, 130, 4500), (7, 1, 700, 300)):
             x = Scored(torch_dev, batch(hq, hkv, d, [c], [u], seed=7), old=False)
             x.scores()
             torch_dev.cuda.synchronize()
             x.check_scores()
-            lse, sums = x.plan[:128].view(np.int32)[14:16]
-            seen |= {("lse", d, int(lse)), ("sum", d, int(sums))}
-    assert seen == {(k, d, n) for k in ("lse", "sum") for d in (64, 128) for n in (1, 2, 4)}, seen
+            h = x.plan[:128].view(np.int32)
+            seen |= {("lse", d, int(h[14])), ("cut", d, bool(h[17]))}
+    assert seen == {(k, d, n) for d in (64, 128) for k, n in
+                    (("lse", 1), ("lse", 2), ("lse", 4), ("cut", False), ("cut", True))}, seen
 
 
 @pytest.mark.parametrize("chunk", [1, 50])
