@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/ssa_evict.h"
 #include "ssa_device.h"
 #include "ssa_evict_format.h"
@@ -19,11 +21,14 @@ using namespace ssa_dev;
 struct EvictArgs {
   const uint8_t* plan;
   uint64_t hash;
-  int32_t workgroups, off_items;
+  int32_t workgroups, off_items;  // of the launch, and where its items lie in the plan
+  int32_t lists;                  // long lists
   int32_t hkv, maxp, sink, recent;
   const float* scores;
   const int32_t* bt;
   int32_t* keep;
+  uint8_t* ws;
+  int64_t ws_counts, ws_cands;
   // compaction
   const int32_t* keep_in;
   const int32_t* nt;
@@ -41,12 +46,10 @@ __device__ __forceinline__ int workgroup_id() {
 }
 
 // ---------------------------------------------------------------------------
-// Selection: one workgroup a list.  Scores map to 32-bit keys in the same order;
-// three histogram passes (11, 11, 10 bits, highest first) find the key T of the
-// last score that stays and how many of its equals do; one ordered pass writes the
-// indexes.  Keys are held in LDS, up to CAP of them; longer lists read the others
-// again from the cache.
-constexpr int kBins = 2048;
+// Selection.  Scores map to 32-bit keys in the same order.  The candidates (all but
+// the first `sink` and the last `recent`) are searched for the key T of the last score
+// that stays, by histograms of its bits from the highest on, and for how many of T's
+// equals do; an ordered pass writes the indexes.
 
 // A total order of scores: NaN as -infinity, -0 as +0.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -58,146 +61,415 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
                                         __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
+// Four keys of one page from index i on.
+__device__ __forceinline__ u32x4 read_keys(const EvictArgs& a, const int32_t* row, int kvh, int i) {
+  const f32x4 x = *reinterpret_cast<const f32x4*>(
+      a.scores + ((size_t)row[i / 16] * a.hkv + kvh) * 16 + i % 16);
+  return u32x4{order_key(x[0]), order_key(x[1]), order_key(x[2]), order_key(x[3])};
+}
 
-template <int THREADS, int CAP>
-__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
-  constexpr int WAVES = THREADS / 64, BPT = kBins / THREADS;
-  __shared__ __attribute__((aligned(16))) uint32_t s_key[CAP];
-  __shared__ int s_hist[kBins];
-  __shared__ int s_part[WAVES], s_eq[WAVES];
-  __shared__ int s_bin, s_above;
+// Inclusive sum over the lanes of a wave, within the vector registers.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xF>(x);  // from the lane 1, 2, 4, 8 before, in rows of 16
+  x = dpp_add<0x112, 0xF>(x);
+  x = dpp_add<0x114, 0xF>(x);
+  x = dpp_add<0x118, 0xF>(x);
+  x = dpp_add<0x142, 0xA>(x);  // the last lane of the row before, to rows 1 and 3
+  return dpp_add<0x143, 0xC>(x);  // lane 31, to rows 2 and 3
+}
+
+struct Found {
+  int bin, above, in_bin;  // the bin, and how many lie above and in it
+};
+template <int THREADS>
+struct FindLds {
+  int part[THREADS / 64];
+  Found found;
+};
+// The bin of a histogram in LDS, counted from its top, that holds the need-th entry
+// (1 <= need <= entries).  All threads call it; the histogram may be written again
+// after it.
+template <int THREADS, int BINS>
+__device__ __forceinline__ Found find_bin(const int* hist, int need, FindLds<THREADS>& lds) {
+  constexpr int PER = BINS / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int mine[PER], total = 0;
+#pragma unroll
+  for (int b = 0; b < PER; ++b) {
+    mine[b] = hist[BINS - 1 - (tid * PER + b)];
+    total += mine[b];
+  }
+  const int scan = wave_scan(total);
+  if (lane == 63) lds.part[wave] = scan;
+  __syncthreads();
+  int above = scan - total;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) above += w < wave ? lds.part[w] : 0;
+#pragma unroll
+  for (int b = 0; b < PER; ++b) {
+    if (above < need && above + mine[b] >= need)
+      lds.found = Found{BINS - 1 - (tid * PER + b), above, mine[b]};
+    above += mine[b];
+  }
+  __syncthreads();
+  return lds.found;
+}
+
+// The flags of four keys: kept for sure, and equal to T.
+struct Flags {
+  bool in[4], eq[4];
+};
+// Indexes before these four of the lane, in the wave's lane-major order.
+__device__ __forceinline__ void count_before(const Flags& f, int* in, int* eq, int* all_in,
+                                             int* all_eq) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint64_t bi = __ballot(f.in[j]), be = __ballot(f.eq[j]);
+    *in += lanes_below(bi);
+    *eq += lanes_below(be);
+    *all_in += (int)__popcll(bi);
+    *all_eq += (int)__popcll(be);
+  }
+}
+
+// Short lists: one workgroup, four 4-key groups a thread in registers.  It is a chain of
+// latencies (plan, table, scores, then histograms of 11, 11 and 10 bits, of which
+// the last is left out where all of a bin stays): 512 lists of 600 to 4096 keys, of
+// which 1000 stay, take 13 us.
+constexpr int kShortThreads = 512;
+constexpr int kShortGroups = kShortList / 4 / kShortThreads;
+constexpr int kShortBins = 2048;
+
+__global__ __launch_bounds__(kShortThreads) void evict_select_kernel(EvictArgs a) {
+  constexpr int THREADS = kShortThreads, WAVES = THREADS / 64, NG = kShortGroups;
+  __shared__ int s_hist[kShortBins];
+  __shared__ FindLds<THREADS> s_find;
+  __shared__ int s_count[NG * WAVES];
   const int wg = workgroup_id();
   if (wg >= a.workgroups || !plan_ok(a)) return;
-  const EvictReq rq = reinterpret_cast<const EvictReq*>(a.plan + sizeof(EvictHeader))[wg / a.hkv];
-  const int kvh = wg % a.hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const EvictShort rq = reinterpret_cast<const EvictShort*>(a.plan + a.off_items)[wg / a.hkv];
+  const int kvh = wg % a.hkv, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int32_t* out = a.keep + rq.keep_off * a.hkv + (int64_t)kvh * rq.kept;
   const int len = rq.len;
   if (rq.kept == len) {
     for (int i = tid; i < len; i += THREADS) out[i] = i;
     return;
   }
-  const int32_t* row = a.bt + (size_t)(wg / a.hkv) * a.maxp;
+  const int32_t* row = a.bt + (size_t)rq.req * a.maxp;
   const int lo = a.sink, hi = len - a.recent;  // candidates
   int need = rq.kept - a.sink - a.recent;      // of which this many stay
-
-  // four scores of one page
-  auto read4 = [&](int i) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(
-        a.scores + ((size_t)row[i / 16] * a.hkv + kvh) * 16 + i % 16);
-    return u32x4{order_key(x[0]), order_key(x[1]), order_key(x[2]), order_key(x[3])};
-  };
-  auto keys4 = [&](int i) {
-    return i < CAP ? *reinterpret_cast<const u32x4*>(s_key + i) : read4(i);
-  };
-  for (int i = tid * 4; i < len && i < CAP; i += THREADS * 4)
-    *reinterpret_cast<u32x4*>(s_key + i) = read4(i);
-
-  uint32_t prefix = 0;  // the bits of T found so far
+  const int groups = (len + THREADS * 4 - 1) / (THREADS * 4);  // that hold keys
+  u32x4 k[NG];
+#pragma unroll
+  for (int n = 0; n < NG; ++n) {
+    const int i = (n * THREADS + tid) * 4;
+    k[n] = i < len ? read_keys(a, row, kvh, i) : u32x4{0, 0, 0, 0};
+  }
+  uint32_t t = 0xFFFFFFFFu;  // above every score's key
   if (need > 0) {
+    t = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-      const uint32_t digit_mask = pass == 2 ? 1023u : 2047u;
+      const uint32_t digits = pass == 2 ? 1023u : 2047u;
       const uint32_t done = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10;
-#pragma unroll
-      for (int b = 0; b < BPT; ++b) s_hist[b * THREADS + tid] = 0;
+      for (int b = tid; b < kShortBins; b += THREADS) s_hist[b] = 0;
       __syncthreads();
-      for (int i = tid * 4; i < len; i += THREADS * 4) {
-        const u32x4 k = keys4(i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (i + j >= lo && i + j < hi && (k[j] & done) == prefix)
-            atomicAdd(&s_hist[(k[j] >> shift) & digit_mask], 1);
-      }
-      __syncthreads();
-      // thread t owns bins from the top: kBins - 1 - t BPT downwards
-      int mine[BPT], total = 0;
+      for (int n = 0; n < NG; ++n) {
+        if (n >= groups) break;
 #pragma unroll
-      for (int b = 0; b < BPT; ++b) {
-        mine[b] = s_hist[kBins - 1 - (tid * BPT + b)];
-        total += mine[b];
-      }
-      int scan = total;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(scan, o, 64);
-        if (lane >= o) scan += v;
-      }
-      if (lane == 63) s_part[wave] = scan;
-      __syncthreads();
-      int above = scan - total;
-      for (int w = 0; w < wave; ++w) above += s_part[w];
-#pragma unroll
-      for (int b = 0; b < BPT; ++b) {
-        if (above < need && above + mine[b] >= need) {
-          s_bin = kBins - 1 - (tid * BPT + b);
-          s_above = above;
+        for (int j = 0; j < 4; ++j) {
+          const int i = (n * THREADS + tid) * 4 + j;
+          if (i >= lo && i < hi && (k[n][j] & done) == t)
+            atomicAdd(&s_hist[(k[n][j] >> shift) & digits], 1);
         }
-        above += mine[b];
       }
       __syncthreads();
-      prefix |= (uint32_t)s_bin << shift;
-      need -= s_above;
+      const Found f = find_bin<THREADS, kShortBins>(s_hist, need, s_find);
+      t |= (uint32_t)f.bin << shift;
+      need -= f.above;
+      if (f.in_bin == need) {  // the whole bin stays: every key above t - 1
+        t -= 1;                // t is not 0: -infinity's key is not
+        need = 0;
+        break;
+      }
     }
-  } else {
-    prefix = 0xFFFFFFFFu;  // above every score's key: no candidate stays
-    __syncthreads();
   }
-
-  // Each wave takes a run of 256-key units, counts what stays above T and equal to
-  // it, and after a scan over the waves writes its indexes in order.
-  const int units = (len + 255) / 256, per = (units + WAVES - 1) / WAVES;
-  const int u0 = wave * per, u1 = min(units, u0 + per);
-  auto flags = [&](int i, bool* in, bool* eq) {
-    u32x4 k = {0, 0, 0, 0};
-    if (i < len) k = keys4(i);
+  auto flags = [&](int n) {
+    Flags f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int at = i + j;
-      const bool cand = at >= lo && at < hi;
-      in[j] = at < len && (!cand || k[j] > prefix);
-      eq[j] = at < len && cand && k[j] == prefix;
+      const int i = (n * THREADS + tid) * 4 + j;
+      const bool cand = i >= lo && i < hi;
+      f.in[j] = i < len && (!cand || k[n][j] > t);
+      f.eq[j] = i < len && cand && k[n][j] == t;
     }
+    return f;
   };
-  int n_in = 0, n_eq = 0;
-  for (int u = u0; u < u1; ++u) {
-    bool in[4], eq[4];
-    flags(u * 256 + lane * 4, in, eq);
+  // kept and equal ones before each wave's keys of each group, in one scan of the
+  // NG x WAVES pairs (16 bits each hold a list's length)
+  static_assert(NG * WAVES <= 64 && kShortList < 1 << 15, "one wave, one word");
+  int before_in[NG], before_eq[NG];
+#pragma unroll
+  for (int n = 0; n < NG; ++n) {
+    if (n >= groups) break;
+    int all_in = 0, all_eq = 0;
+    before_in[n] = before_eq[n] = 0;
+    count_before(flags(n), &before_in[n], &before_eq[n], &all_in, &all_eq);
+    if (lane == 0) s_count[n * WAVES + wave] = all_in | all_eq << 16;
+  }
+  __syncthreads();
+  const int mine = lane < groups * WAVES ? s_count[lane] : 0, scan = wave_scan(mine) - mine;
+#pragma unroll
+  for (int n = 0; n < NG; ++n) {
+    if (n >= groups) break;
+    const int before = __builtin_amdgcn_readlane(scan, n * WAVES + wave);
+    before_in[n] += before & 0xFFFF;
+    before_eq[n] += before >> 16;
+    const Flags f = flags(n);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      n_in += (int)__popcll(__ballot(in[j]));
-      n_eq += (int)__popcll(__ballot(eq[j]));
+      if (f.in[j] || (f.eq[j] && before_eq[n] < need))
+        out[before_in[n] + min(before_eq[n], need)] = (n * THREADS + tid) * 4 + j;
+      before_in[n] += f.in[j];
+      before_eq[n] += f.eq[j];
+    }
+  }
+}
+
+// Long lists: segments of 8192 keys, four launches (clear, histogram, candidates, write),
+// because one workgroup would read a list at one compute unit's rate (8 lists of 131072
+// keys: 123 us in one workgroup each).
+//   histogram   of the first 12 bits, added up over the segments (integers: their
+//               order does not matter);
+//   candidates  every segment finds the threshold's bin, counts what lies above it
+//               and lists the scores in it, (key, index) in one word that orders them;
+//   write       every segment finds the last candidate that stays (few: about 1 in
+//               200 where scores spread over a dozen octaves), and from the counts and
+//               the candidates before it the place of its first index.
+constexpr int kSegThreads = 512;
+constexpr int kSegGroups = kSegKeys / 4 / kSegThreads;
+constexpr int kCandDigit = 10, kCandBins = 1 << kCandDigit;
+constexpr int kCandHeld = 4096;  // candidates held in LDS; more are read again
+
+__device__ __forceinline__ int* seg_hist(const EvictArgs& a, int list) {
+  return reinterpret_cast<int*>(a.ws) + (int64_t)list * kSegBins;
+}
+__device__ __forceinline__ SegState* seg_state(const EvictArgs& a, int list) {
+  return reinterpret_cast<SegState*>(a.ws + (int64_t)a.lists * kSegBins * 4) + list;
+}
+// (key, index), the higher the better: the lower index of equal keys first.
+__device__ __forceinline__ uint64_t cand_word(uint32_t key, int i) {
+  return (uint64_t)key << 32 | (uint32_t)~i;
+}
+
+__global__ __launch_bounds__(256) void evict_clear_kernel(EvictArgs a) {
+  if (!plan_ok(a)) return;
+  const int64_t words = (int64_t)a.lists * (kSegBins + sizeof(SegState) / 4);
+  for (int64_t i = ((int64_t)workgroup_id() * 256 + threadIdx.x) * 4; i < words;
+       i += (int64_t)a.workgroups * 1024)
+    *reinterpret_cast<u32x4*>(a.ws + i * 4) = u32x4{0, 0, 0, 0};
+}
+
+struct SegWork {
+  EvictSeg sg;
+  int kvh, list, tid;
+  int lo, hi, end;  // candidates are lo .. hi - 1; the segment's keys end before `end`
+  u32x4 k[kSegGroups];
+};
+__device__ __forceinline__ int seg_index(const SegWork& w, int n) {
+  return w.sg.key0 + (n * kSegThreads + w.tid) * 4;
+}
+__device__ __forceinline__ bool seg_work(const EvictArgs& a, SegWork* w) {
+  const int wg = workgroup_id();
+  if (wg >= a.workgroups || !plan_ok(a)) return false;
+  w->sg = reinterpret_cast<const EvictSeg*>(a.plan + a.off_items)[wg / a.hkv];
+  w->kvh = wg % a.hkv;
+  w->list = w->sg.long_index * a.hkv + w->kvh;
+  w->tid = threadIdx.x;
+  w->lo = a.sink;
+  w->hi = w->sg.len - a.recent;
+  w->end = min(w->sg.len, w->sg.key0 + kSegKeys);
+  const int32_t* row = a.bt + (size_t)w->sg.req * a.maxp;
+#pragma unroll
+  for (int n = 0; n < kSegGroups; ++n) {
+    const int i = seg_index(*w, n);
+    w->k[n] = i < w->end ? read_keys(a, row, w->kvh, i) : u32x4{0, 0, 0, 0};
+  }
+  return true;
+}
+
+__global__ __launch_bounds__(kSegThreads) void evict_histogram_kernel(EvictArgs a) {
+  __shared__ int s_hist[kSegBins];
+  SegWork w;
+  if (!seg_work(a, &w)) return;
+  for (int b = w.tid; b < kSegBins; b += kSegThreads) s_hist[b] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < kSegGroups; ++n)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = seg_index(w, n) + j;
+      if (i >= w.lo && i < w.hi && i < w.end) atomicAdd(&s_hist[w.k[n][j] >> 20], 1);
+    }
+  __syncthreads();
+  int* hist = seg_hist(a, w.list);
+  for (int b = w.tid; b < kSegBins; b += kSegThreads)
+    if (s_hist[b]) atomicAdd(hist + b, s_hist[b]);
+}
+
+__global__ __launch_bounds__(kSegThreads) void evict_candidates_kernel(EvictArgs a) {
+  constexpr int WAVES = kSegThreads / 64;
+  __shared__ __attribute__((aligned(16))) int s_hist[kSegBins];
+  __shared__ FindLds<kSegThreads> s_find;
+  __shared__ int s_in[WAVES], s_eq[WAVES], s_base;
+  SegWork w;
+  if (!seg_work(a, &w)) return;
+  const int* hist = seg_hist(a, w.list);
+  for (int b = w.tid * 4; b < kSegBins; b += kSegThreads * 4)
+    *reinterpret_cast<u32x4*>(s_hist + b) = ld16(hist + b);
+  __syncthreads();
+  const int need = w.sg.kept - a.sink - a.recent;
+  Found f{kSegBins, 0, 0};  // nothing but sinks and recent keys stays: above every bin
+  if (need > 0) f = find_bin<kSegThreads, kSegBins>(s_hist, need, s_find);
+  SegState* state = seg_state(a, w.list);
+  if (w.sg.key0 == 0 && w.tid == 0) {
+    state->bin = f.bin;
+    state->need = need - f.above;
+  }
+  const int lane = w.tid & 63, wave = w.tid >> 6;
+  int n_in = 0, n_eq = 0, before[kSegGroups];
+#pragma unroll
+  for (int n = 0; n < kSegGroups; ++n) {
+    before[n] = n_eq;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = seg_index(w, n) + j, bin = (int)(w.k[n][j] >> 20);
+      const bool cand = i >= w.lo && i < w.hi;
+      const uint64_t eq = __ballot(i < w.end && cand && bin == f.bin);
+      n_in += (int)__popcll(__ballot(i < w.end && (!cand || bin > f.bin)));
+      n_eq += (int)__popcll(eq);
     }
   }
   if (lane == 0) {
-    s_part[wave] = n_in;
+    s_in[wave] = n_in;
     s_eq[wave] = n_eq;
   }
   __syncthreads();
-  n_in = n_eq = 0;
-  for (int w = 0; w < wave; ++w) {
-    n_in += s_part[w];
-    n_eq += s_eq[w];
+  if (w.tid == 0) {
+    int in = 0, eq = 0;
+    for (int x = 0; x < WAVES; ++x) {
+      in += s_in[x];
+      eq += s_eq[x];
+    }
+    reinterpret_cast<int*>(a.ws + a.ws_counts)[((int64_t)w.sg.seg0 + w.sg.key0 / kSegKeys) * a.hkv + w.kvh] =
+        in;
+    s_base = eq ? atomicAdd(&state->num_cands, eq) : 0;
   }
-  for (int u = u0; u < u1; ++u) {
-    const int i = u * 256 + lane * 4;
-    bool in[4], eq[4];
-    flags(i, in, eq);
-    int before_in = n_in, before_eq = n_eq;
+  __syncthreads();
+  int base = s_base;
+  for (int x = 0; x < wave; ++x) base += s_eq[x];
+  uint64_t* cands = reinterpret_cast<uint64_t*>(a.ws + a.ws_cands) + w.sg.cand_off * a.hkv +
+                    (int64_t)w.kvh * w.sg.len;
+#pragma unroll
+  for (int n = 0; n < kSegGroups; ++n) {
+    int at = base + before[n];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint64_t bi = __ballot(in[j]), be = __ballot(eq[j]);
-      before_in += lanes_below(bi);
-      before_eq += lanes_below(be);
-      n_in += (int)__popcll(bi);
-      n_eq += (int)__popcll(be);
+      const int i = seg_index(w, n) + j;
+      const bool eq = i < w.end && i >= w.lo && i < w.hi && (int)(w.k[n][j] >> 20) == f.bin;
+      const uint64_t mask = __ballot(eq);
+      if (eq) cands[at + lanes_below(mask)] = cand_word(w.k[n][j], i);
+      at += (int)__popcll(mask);
     }
+  }
+}
+
+__global__ __launch_bounds__(kSegThreads) void evict_write_kernel(EvictArgs a) {
+  constexpr int WAVES = kSegThreads / 64, NG = kSegGroups;
+  __shared__ uint64_t s_cand[kCandHeld];
+  __shared__ int s_hist[kCandBins];
+  __shared__ FindLds<kSegThreads> s_find;
+  __shared__ int s_in[NG * WAVES], s_before;
+  SegWork w;
+  if (!seg_work(a, &w)) return;
+  const SegState st = *seg_state(a, w.list);
+  const uint64_t* cands = reinterpret_cast<const uint64_t*>(a.ws + a.ws_cands) +
+                          w.sg.cand_off * a.hkv + (int64_t)w.kvh * w.sg.len;
+  const int held = min(st.num_cands, kCandHeld);
+  for (int c = w.tid; c < held; c += kSegThreads) s_cand[c] = cands[c];
+  if (w.tid == 0) s_before = 0;
+  // the word of the last candidate that stays: its 20 lower key bits, then the index
+  uint64_t t = (uint64_t)st.bin << 52;
+  int need = st.need;
+  if (need > 0 && need < st.num_cands) {
+    for (int shift = 52 - kCandDigit; shift > -kCandDigit; shift -= kCandDigit) {
+      const int sh = max(shift, 0);
+      const uint64_t done = ~0ull << (shift + kCandDigit);
+      for (int b = w.tid; b < kCandBins; b += kSegThreads) s_hist[b] = 0;
+      __syncthreads();
+      for (int c = w.tid; c < st.num_cands; c += kSegThreads) {
+        const uint64_t x = c < kCandHeld ? s_cand[c] : cands[c];
+        // the last digit has fewer bits: those of the digit before it are t's
+        if ((x & done) == (t & done)) atomicAdd(&s_hist[(x >> sh) & (kCandBins - 1)], 1);
+      }
+      __syncthreads();
+      const Found f = find_bin<kSegThreads, kCandBins>(s_hist, need, s_find);
+      t = (t & done) | (uint64_t)f.bin << sh;
+      need -= f.above;
+      if (f.in_bin == need) break;  // every candidate from t on stays
+    }
+  } else if (need <= 0) {
+    t = ~0ull;  // no candidate does
+  }
+  // what stays before this segment
+  __syncthreads();
+  int n = 0;
+  const int* counts = reinterpret_cast<const int*>(a.ws + a.ws_counts) + (int64_t)w.sg.seg0 * a.hkv + w.kvh;
+  for (int s = w.tid; s < w.sg.key0 / kSegKeys; s += kSegThreads) n += counts[(int64_t)s * a.hkv];
+  for (int c = w.tid; c < st.num_cands; c += kSegThreads) {
+    const uint64_t x = c < kCandHeld ? s_cand[c] : cands[c];
+    n += x >= t && (int)~(uint32_t)x < w.sg.key0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  const int lane = w.tid & 63, wave = __builtin_amdgcn_readfirstlane(w.tid >> 6);
+  if (lane == 0 && n) atomicAdd(&s_before, n);
+  int before[NG];
+  auto keep = [&](int g, int j) {
+    const int i = seg_index(w, g) + j, bin = (int)(w.k[g][j] >> 20);
+    if (i >= w.end) return false;
+    if (i < w.lo || i >= w.hi) return true;
+    return bin > st.bin || (bin == st.bin && cand_word(w.k[g][j], i) >= t);
+  };
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    int all = 0;
+    before[g] = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (in[j] || (eq[j] && before_eq < need)) out[before_in + min(before_eq, need)] = i + j;
-      before_in += in[j];
-      before_eq += eq[j];
+      const uint64_t mask = __ballot(keep(g, j));
+      before[g] += lanes_below(mask);
+      all += (int)__popcll(mask);
     }
+    if (lane == 0) s_in[g * WAVES + wave] = all;
+  }
+  __syncthreads();
+  static_assert(NG * WAVES <= 64, "one wave");
+  int32_t* out = a.keep + w.sg.keep_off * a.hkv + (int64_t)w.kvh * w.sg.kept + s_before;
+  const int mine = lane < NG * WAVES ? s_in[lane] : 0, scan = wave_scan(mine) - mine;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    before[g] += __builtin_amdgcn_readlane(scan, g * WAVES + wave);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (keep(g, j)) out[before[g]++] = seg_index(w, g) + j;
   }
 }
 
@@ -275,9 +547,6 @@ __global__ __launch_bounds__(256) void evict_compact_kernel(EvictArgs a) {
 }
 
 constexpr int kGridRow = 1 << 16;  // workgroups in a row of the grid (2^32 threads at most)
-// Lists of at most this many keys run in small workgroups, several to a compute unit.
-constexpr int kShortList = 4096;
-constexpr int kLongCap = 32768;
 
 template <class K>
 int launch(K kernel, const EvictArgs& a, int threads, hipStream_t stream) {
@@ -310,19 +579,32 @@ int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* 
                      const float* scores, const int32_t* block_table, int32_t* keep,
                      void* workspace, size_t ws_bytes, void* stream) {
   const EvictHeader* h = nullptr;
-  const int rc = check_evict_plan(shape, plan_host, &h);
+  int rc = check_evict_plan(shape, plan_host, &h);
   if (rc) return rc;
   if (!plan_dev) return SSA_ERR_NULL;
   if (h->num_keep > 0 && (!scores || !block_table || !keep)) return SSA_ERR_NULL;
   if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
   if (h->num_keep == 0) return SSA_OK;
   EvictArgs a = evict_args(h, plan_dev, block_table);
-  a.workgroups = h->num_reqs * h->hkv;
   a.scores = scores;
   a.keep = keep;
+  a.ws = static_cast<uint8_t*>(workspace);
+  a.ws_counts = h->ws_counts;
+  a.ws_cands = h->ws_cands;
+  a.lists = h->num_long * h->hkv;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return h->max_len <= kShortList ? launch(evict_select_kernel<256, kShortList>, a, 256, s)
-                                  : launch(evict_select_kernel<1024, kLongCap>, a, 1024, s);
+  a.workgroups = h->num_short * h->hkv;
+  a.off_items = h->off_short;
+  rc = launch(evict_select_kernel, a, kShortThreads, s);
+  if (rc || a.lists == 0) return rc;
+  // 16 KB of histogram a list, in workgroups of 4 KB at a time
+  a.workgroups = std::min(a.lists * 4, 1024);
+  if ((rc = launch(evict_clear_kernel, a, 256, s))) return rc;
+  a.workgroups = h->num_segs * h->hkv;
+  a.off_items = h->off_segs;
+  if ((rc = launch(evict_histogram_kernel, a, kSegThreads, s))) return rc;
+  if ((rc = launch(evict_candidates_kernel, a, kSegThreads, s))) return rc;
+  return launch(evict_write_kernel, a, kSegThreads, s);
 }
 
 int ssa_evict_compact(const ssa_shape* shape, const void* plan_host, const void* plan_dev,

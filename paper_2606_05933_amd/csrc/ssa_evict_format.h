@@ -20,6 +20,9 @@ constexpr int kLseMaxKeys = 32768;             // keys of one item of the first 
 constexpr int kJoinKeys = 1024;                // keys of one item of the decode join
 constexpr int kColsPad = 256;                  // a chunk request's columns are padded to this
 constexpr int kEvictSlots = 64;                // kept keys of one compaction item
+constexpr int kShortList = 8192;               // keys of a list that one workgroup selects from
+constexpr int kSegKeys = 8192;                 // keys of a segment of a longer one
+constexpr int kSegBins = 4096;                 // its first histogram: 12 bits
 // Columns (row, head in group) of a request: index arithmetic by a 32-bit reciprocal.
 constexpr int64_t kMaxScoreCols = (int64_t)1 << 28;
 
@@ -68,7 +71,7 @@ struct ScoreItem {
   // float offsets in the workspace for kv head 0:
   //   chunk lists:   off0 = lse [Hkv][cols_pad]; off1 = (m, l) [Hkv][nsplit][cols_pad][2],
   //                  kListSum: sums [pieces][Hkv][len, padded to kSumKeys]
-  //   decode lists:  off0 = logits [Hkv][G][cols_pad], off1 = records [Hkv][nsplit][record]
+  //   decode lists:  off0 = logits [Hkv][cols_pad / 32][32 G], off1 = records [Hkv][nsplit][record]
   int64_t off0, off1;
 };
 static_assert(sizeof(ScoreItem) == 64, "score item size");
@@ -85,17 +88,46 @@ struct EvictHeader {
   uint64_t hash;
   int32_t hq, hkv, head_dim, page_size, max_pages_per_req, num_pages;
   float softmax_scale;
-  int32_t num_items;
-  int32_t off_items, max_len;
+  int32_t num_short, num_segs, num_items;           // selection: short lists, segments; compaction
+  int32_t off_short, off_segs, off_items, num_long;  // num_long: requests of more than kShortList keys
   int64_t num_keep;  // kept keys of one kv head over all requests
   int64_t plan_bytes, ws_bytes;
-  int64_t pad[5];
+  int64_t ws_counts, ws_cands;  // byte offsets in the workspace
+  int64_t pad;
 };
 static_assert(sizeof(EvictHeader) == 128, "evict header size");
 
 struct EvictReq {
   int32_t len, kept;
   int64_t keep_off;  // n_0 + ... + n_{i-1}
+};
+
+// A request of at most kShortList keys: one workgroup a kv head.
+struct EvictShort {
+  int32_t req, len, kept, pad;
+  int64_t keep_off;
+};
+static_assert(sizeof(EvictShort) == 24, "short list size");
+
+// kSegKeys keys of a longer one.  Workspace, for list = long_index * Hkv + kv head:
+//   int32 [lists][kSegBins]   histogram of the scores' first 12 bits, at 0
+//   SegState [lists]          after it
+//   int32 [segments][Hkv]     kept for sure, at ws_counts
+//   uint64 candidates         at ws_cands: list's from Hkv * cand_off + kv head * len on
+struct EvictSeg {
+  int32_t req, len, kept;
+  int32_t key0;        // the segment's first key
+  int32_t seg0;        // index of the request's first segment in the plan
+  int32_t long_index;  // of the request among those of more than kShortList keys
+  int64_t keep_off;
+  int64_t cand_off;    // keys of the long requests before
+};
+static_assert(sizeof(EvictSeg) == 40, "segment size");
+
+struct SegState {
+  int32_t num_cands;  // scores whose first 12 bits are the threshold's
+  int32_t bin, need;  // those bits, and how many candidates stay
+  int32_t pad;
 };
 
 // kept keys slot0 .. slot0 + n - 1 of every kv head of a request that loses keys

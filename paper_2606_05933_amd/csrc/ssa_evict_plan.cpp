@@ -21,9 +21,11 @@ constexpr int64_t kMaxLen = 1 << 30;
 constexpr int64_t kFillGroups = 1024;
 // A decode row's key range is cut into pieces of a multiple of 128 keys (one
 // 32-key block for each of four waves), at most kDecodeMaxKeys: a piece costs a
-// record of G (D + 3) floats.
+// record of G (D + 3) floats, and long ones leave compute units idle at the end (32
+// rows of 8k to 33k keys, 64/8 heads: 596 us in pieces of 2048, 585 of 1024, 592 of
+// 512).
 constexpr int64_t kDecodeStepKeys = 128;
-constexpr int64_t kDecodeMaxKeys = 4096;
+constexpr int64_t kDecodeMaxKeys = 1024;
 // A piece of a chunk column tile's key range, at least, and pieces of one, at most.
 constexpr int64_t kLseMinKeys = 256;
 constexpr int64_t kMaxPieces = 64;
@@ -292,6 +294,8 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
 struct EvictPlan {
   EvictHeader hdr;
   std::vector<EvictReq> reqs;
+  std::vector<EvictShort> shorts;
+  std::vector<EvictSeg> segs;
   std::vector<EvictItem> items;
 };
 
@@ -304,7 +308,7 @@ int build_evict(const ssa_shape* s, const int32_t* kv_len, const int32_t* budget
   if (sink < 0 || recent < 0) return SSA_ERR_ARG;
   EvictHeader& h = p->hdr;
   std::memset(&h, 0, sizeof h);
-  int64_t keys = 0, keep = 0;
+  int64_t keys = 0, keep = 0, cands = 0;
   for (int32_t i = 0; i < n; ++i) {
     const int64_t len = kv_len[i], kept = std::min(kv_len[i], budget[i]);
     if (len < 0 || budget[i] < 0) return SSA_ERR_LENGTH;
@@ -313,12 +317,20 @@ int build_evict(const ssa_shape* s, const int32_t* kv_len, const int32_t* budget
     if (ceil_div(len, SSA_PAGE_SIZE) > s->max_pages_per_req) return SSA_ERR_PAGES;
     if (kept < len && (int64_t)sink + recent > kept) return SSA_ERR_ARG;
     p->reqs.push_back({(int32_t)len, (int32_t)kept, keep});
+    if (kept > 0 && (len <= kShortList || kept == len)) {
+      p->shorts.push_back({i, (int32_t)len, (int32_t)kept, 0, keep});
+    } else if (kept > 0) {
+      const int32_t seg0 = (int32_t)p->segs.size();
+      for (int64_t k = 0; k < len; k += kSegKeys)
+        p->segs.push_back({i, (int32_t)len, (int32_t)kept, (int32_t)k, seg0, h.num_long, keep, cands});
+      ++h.num_long;
+      cands += len;
+    }
     if (kept < len)
       for (int64_t k = 0; k < kept; k += kEvictSlots)
         p->items.push_back({i, (int32_t)k, (int32_t)std::min<int64_t>(kEvictSlots, kept - k),
                             (int32_t)len, (int32_t)kept, 0, keep});
     keep += kept;
-    h.max_len = std::max(h.max_len, (int32_t)len);
   }
   h.magic = kEvictMagic;
   h.sink = sink;
@@ -332,21 +344,31 @@ int build_evict(const ssa_shape* s, const int32_t* kv_len, const int32_t* budget
   h.num_pages = s->num_pages;
   h.softmax_scale = s->softmax_scale;
   h.num_keep = keep;
-  const int64_t items = (int64_t)p->items.size();
-  const int64_t off = sizeof(EvictHeader) + (int64_t)sizeof(EvictReq) * n;
-  h.plan_bytes = off + items * (int64_t)sizeof(EvictItem);
-  if (h.plan_bytes > INT32_MAX || items * h.hkv > INT32_MAX || (int64_t)n * h.hkv > INT32_MAX)
+  const int64_t items = (int64_t)p->items.size(), shorts = (int64_t)p->shorts.size(),
+                segs = (int64_t)p->segs.size();
+  const int64_t off_short = sizeof(EvictHeader) + (int64_t)sizeof(EvictReq) * n;
+  const int64_t off_segs = off_short + (int64_t)sizeof(EvictShort) * shorts;
+  const int64_t off_items = off_segs + (int64_t)sizeof(EvictSeg) * segs;
+  h.plan_bytes = off_items + items * (int64_t)sizeof(EvictItem);
+  if (h.plan_bytes > INT32_MAX || (items + segs + shorts) * h.hkv > INT32_MAX)
     return SSA_ERR_LENGTH;
   h.num_items = (int32_t)items;
-  h.off_items = (int32_t)off;
-  h.ws_bytes = 256;
+  h.num_short = (int32_t)shorts;
+  h.num_segs = (int32_t)segs;
+  h.off_short = (int32_t)off_short;
+  h.off_segs = (int32_t)off_segs;
+  h.off_items = (int32_t)off_items;
+  const int64_t lists = (int64_t)h.num_long * h.hkv;
+  h.ws_counts = lists * (kSegBins * 4 + (int64_t)sizeof(SegState));
+  h.ws_cands = round_up(h.ws_counts + segs * h.hkv * 4, 256);
+  h.ws_bytes = std::max<int64_t>(256, h.ws_cands + cands * h.hkv * 8);
   const int32_t more[2] = {sink, recent};
   uint64_t hv = hash_shape(s, more, 2);
   if (n > 0) {
     hv = fnv1a(hv, kv_len, sizeof(int32_t) * n);
     hv = fnv1a(hv, budget, sizeof(int32_t) * n);
   }
-  const int64_t cut[2] = {items, h.ws_bytes};
+  const int64_t cut[3] = {items, segs, h.ws_bytes};
   h.hash = fnv1a(hv, cut, sizeof cut);
   return SSA_OK;
 }
@@ -448,6 +470,10 @@ int ssa_evict_plan(const ssa_shape* shape, const int32_t* kv_len_host, const int
     std::memcpy(b, &p.hdr, sizeof p.hdr);
     if (!p.reqs.empty())
       std::memcpy(b + sizeof p.hdr, p.reqs.data(), sizeof(ssa::EvictReq) * p.reqs.size());
+    if (!p.shorts.empty())
+      std::memcpy(b + p.hdr.off_short, p.shorts.data(), sizeof(ssa::EvictShort) * p.shorts.size());
+    if (!p.segs.empty())
+      std::memcpy(b + p.hdr.off_segs, p.segs.data(), sizeof(ssa::EvictSeg) * p.segs.size());
     if (!p.items.empty())
       std::memcpy(b + p.hdr.off_items, p.items.data(), sizeof(ssa::EvictItem) * p.items.size());
     return SSA_OK;

@@ -122,7 +122,9 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // Each wave takes every fourth 32-key block (two pages).  S^T = K Q^T in 16x16
 // tiles: the A rows of the two tiles are dealt so that a lane ends up with 8
 // consecutive keys of one column (head), which is also the layout of the B operand
-// of the P V product: no data moves between lanes but the block's maximum.
+// of the P V product: no data moves between lanes but the block's maximum.  Logits are
+// stored as they lie, [32 keys][tile][quarter][G][4 keys]: each store instruction
+// writes one run of 64 G bytes.
 template <int D, bool OUT>
 struct DecodeLds {
   float ml[3][4][16];
@@ -148,27 +150,45 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       v = ld16(a.q + ((size_t)it.q_row * a.hq + kvh * a.g + r16) * D + s * 32 + quad * 8);
     qf[s] = as_bf16x8(v);
   }
-  float* logits = a.ws + it.off0 + ((int64_t)kvh * a.g + r16) * it.cols_pad + 8 * quad;
+  float* logits = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + (quad * a.g + r16) * 4;
   float m = -kInf, l = 0.f, lr = 0.f;
   f32x4 o[OUT ? DT : 1];
 #pragma unroll
   for (int t = 0; t < (OUT ? DT : 1); ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // A block's keys go into registers while the block before is at its softmax, its
+  // values while that one's products run: loads are always in flight.
   const int slot0 = 8 * ((r16 >> 2) & 1) + (r16 & 3);
-  for (int kb = it.key0 + wave * 32; kb < it.key1; kb += 128) {
-    const int p0 = row[kb / 16], p1 = row[min(kb / 16 + 1, last_page)];
+  u32x4 kf[2][KS], vf[OUT ? DT : 1];
+  auto load_keys = [&](int p0, int p1) {
     const uint16_t* kp =
         a.kc + ((size_t)(r16 >> 3 ? p1 : p0) * a.hkv + kvh) * 16 * D + slot0 * D + quad * 8;
-    u32x4 kf[2][KS], vf[OUT ? DT : 1];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int s = 0; s < KS; ++s) kf[t][s] = ld16(kp + t * 4 * D + s * 32);
+  };
+  auto load_values = [&](int p0, int p1) {
     if constexpr (OUT) {
       const uint16_t* vp =
           a.vc + ((size_t)(quad >> 1 ? p1 : p0) * a.hkv + kvh) * 16 * D + r16 * 16 + 8 * (quad & 1);
 #pragma unroll
       for (int t = 0; t < DT; ++t) vf[t] = ld16(vp + t * 256);
+    }
+  };
+  const int first = it.key0 + wave * 32;
+  int p0 = 0, p1 = 0;
+  if (first < it.key1) {
+    p0 = row[first / 16];
+    p1 = row[min(first / 16 + 1, last_page)];
+    load_keys(p0, p1);
+    load_values(p0, p1);
+  }
+  for (int kb = first; kb < it.key1; kb += 128) {
+    const bool more = kb + 128 < it.key1;
+    if (more) {
+      p0 = row[(uint32_t)(kb + 128) / 16];
+      p1 = row[min((kb + 128) / 16 + 1, last_page)];
     }
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
@@ -176,11 +196,13 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       s0 = mfma(as_bf16x8(kf[0][s]), qf[s], s0);
       s1 = mfma(as_bf16x8(kf[1][s]), qf[s], s1);
     }
+    if (more) load_keys(p0, p1);
+    __builtin_amdgcn_sched_barrier(0);
     float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
     if (r16 < a.g) {
-      float* to = logits + kb;
+      float* to = logits + (int64_t)kb * a.g;
       *reinterpret_cast<f32x4*>(to) = s0;
-      *reinterpret_cast<f32x4*>(to + 4) = s1;
+      *reinterpret_cast<f32x4*>(to + 16 * a.g) = s1;
     }
     const int nv = it.key1 - kb - 8 * quad;  // this lane's keys that exist
     if (kb + 32 > it.key1) {
@@ -234,6 +256,8 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       }
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(pk), o[t]);
+      if (more) load_values(p0, p1);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   l += __shfl_xor(l, 16, 64);
@@ -324,10 +348,13 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
   __syncthreads();
   const int k0 = it.key0 + tid * 4;
   if (k0 < it.key1) {
-    const float* lg = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + k0;
+    // keys k0 .. k0 + 3 are quarter k0 / 8 % 4 of tile k0 / 4 % 2 of their 32
+    const float* lg = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad +
+                      ((int64_t)(k0 / 32) * 8 + (k0 / 4 % 2) * 4 + k0 / 8 % 4) * a.g * 4;
     f32x4 w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int g = 0; g < a.g; ++g) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(lg + (int64_t)g * it.cols_pad);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lg + g * 4);
       const float m = s_m[g], inv = s_inv[g];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(x[i], a.c, -m)) * inv;

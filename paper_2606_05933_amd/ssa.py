@@ -933,7 +933,7 @@ def _evict_header(plan_host):
     i, q = np.frombuffer(b, dtype=np.int32), np.frombuffer(b, dtype=np.int64)
     if i[0] == 0x31435353:  # a score plan
         return {"num_reqs": int(i[4]), "num_tokens": int(i[5])}
-    return {"num_reqs": int(i[3]), "num_keep": int(q[8])}
+    return {"num_reqs": int(i[3]), "num_keep": int(q[10])}
 
 
 def _scored_args(name, shape, plan_host, plan_dev, q, k_cache, block_table, scores_in, decay,

@@ -199,12 +199,15 @@ def test_evict_plan_and_its_refusals():
     shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
     plan, ws = ssa.evict_plan(shape, [100, 0, 17, 300], [70, 5, 17, 300], 4, 8)
     i4, i8 = plan[:128].view(np.int32), plan[:128].view(np.int64)
-    assert ws >= 256 and i4[3] == 4 and i8[8] == 70 + 0 + 17 + 300 and i8[9] == plan.nbytes
+    assert ws >= 256 and i4[3] == 4 and i8[10] == 70 + 0 + 17 + 300 and i8[11] == plan.nbytes
     reqs = plan[128:128 + 64].view(np.dtype([("len", "<i4"), ("kept", "<i4"), ("off", "<i8")]))
     assert reqs["len"].tolist() == [100, 0, 17, 300] and reqs["kept"].tolist() == [70, 0, 17, 300]
     assert reqs["off"].tolist() == [0, 70, 70, 87]
-    items = plan[i4[14]:].view(np.int32).reshape(-1, 8)
-    assert len(items) == i4[13] == 2 and items[:, :5].tolist() == [[0, 0, 64, 100, 70],
+    shorts = plan[i4[16]:i4[17]].view(np.int32).reshape(-1, 6)
+    assert len(shorts) == i4[13] == 3 and i4[14] == i4[19] == 0
+    assert shorts[:, :5].tolist() == [[0, 100, 70, 0, 0], [2, 17, 17, 0, 70], [3, 300, 300, 0, 87]]
+    items = plan[i4[18]:].view(np.int32).reshape(-1, 8)
+    assert len(items) == i4[15] == 2 and items[:, :5].tolist() == [[0, 0, 64, 100, 70],
                                                                  [0, 64, 6, 100, 70]]
 
     def code(lens, budget, sink, recent, s=shape):
@@ -222,6 +225,24 @@ def test_evict_plan_and_its_refusals():
     assert code([321], [100], 0, 0) == -6
     with pytest.raises(ValueError):
         ssa.evict_plan(shape, [1, 2], [1], 0, 0)
+
+
+def test_long_lists_are_cut_into_segments():
+    hkv, lens = 3, [8192, 8193, 100000, 9000, 50000]
+    shape = shape_of(3 * hkv, hkv, 64, lens)
+    plan, ws = ssa.evict_plan(shape, lens, [100, 8192, 1, 9000, 0], 0, 0)
+    i4, i8 = plan[:128].view(np.int32), plan[:128].view(np.int64)
+    segs = plan[i4[17]:i4[18]].view(np.dtype([(n, "<i4") for n in (
+        "req", "len", "kept", "key0", "seg0", "long")] + [("keep", "<i8"), ("cand", "<i8")]))
+    assert i4[13] == 2 and i4[19] == 2 and len(segs) == i4[14] == 2 + 13
+    for i, at, long, keep, cand in ((1, 0, 0, 100, 0), (2, 2, 1, 8292, 8193)):
+        x = segs[segs["req"] == i]
+        assert x["key0"].tolist() == list(range(0, lens[i], 8192)) and (x["seg0"] == at).all()
+        for name, v in (("len", lens[i]), ("long", long), ("keep", keep), ("cand", cand)):
+            assert (x[name] == v).all()
+    # histograms and states, counts, candidates
+    assert i8[13] == 2 * hkv * (4096 * 4 + 16) and i8[14] >= i8[13] + 15 * hkv * 4
+    assert i8[14] % 256 == 0 and ws == i8[12] == i8[14] + (8193 + 100000) * hkv * 8
 
 
 def test_evict_calls_refuse_before_they_launch():
