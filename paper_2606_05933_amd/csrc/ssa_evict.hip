@@ -477,71 +477,76 @@ __global__ __launch_bounds__(kSegThreads) void evict_write_kernel(EvictArgs a) {
 // Compaction: one workgroup moves 64 kept keys of a kv head (four new pages).
 // Keys are whole 2 D-byte rows.  Values lie dim-major, so a kept key is one
 // 2-byte element of each of a page's D rows: a thread gathers the 8 elements of one
-// 16-byte piece of a new page's row, neighbours from the same old rows.
+// 16-byte piece of a new page's row, neighbours from the same old rows.  A page with
+// one kept key is read whole (32-byte rows), so that cutting long contexts to a
+// quarter reads most of the values.  Every load is issued before the first store; a
+// slot that is not followed loads from the first page and stores nothing.
 template <int D>
 __global__ __launch_bounds__(256) void evict_compact_kernel(EvictArgs a) {
   constexpr int CPR = D / 8, PER = kEvictSlots * CPR / 256;
   __shared__ int s_page[kEvictSlots], s_slot[kEvictSlots];
+  __shared__ uint64_t s_valid;
   const int wg = workgroup_id();
   if (wg >= a.workgroups || !plan_ok(a)) return;
   const EvictItem it = reinterpret_cast<const EvictItem*>(a.plan + a.off_items)[wg / a.hkv];
   const int kvh = wg % a.hkv, tid = threadIdx.x;
   const int32_t* old_row = a.bt + (size_t)it.req * a.maxp;
   const int32_t* new_row = a.nt + (size_t)it.req * a.maxp + it.slot0 / 16;
-  if (tid < kEvictSlots) {
-    int page = -1, slot = 0;
-    if (tid < it.n) {
-      const int key = a.keep_in[it.keep_off * a.hkv + (int64_t)kvh * it.kept + it.slot0 + tid];
-      if (key >= 0 && key < it.len) {
-        page = old_row[key / 16];
-        slot = key % 16;
-      }
-    }
+  float score = 0.f;
+  if (tid < kEvictSlots) {  // the first wave
+    int key = -1;
+    if (tid < it.n)
+      key = a.keep_in[it.keep_off * a.hkv + (int64_t)kvh * it.kept + it.slot0 + tid];
+    const bool valid = key >= 0 && key < it.len;
+    const int page = valid ? old_row[key / 16] : 0, slot = valid ? key % 16 : 0;
     s_page[tid] = page;
     s_slot[tid] = slot;
-    if (page >= 0 && a.scores_io) {
-      const size_t to = ((size_t)new_row[tid / 16] * a.hkv + kvh) * 16 + tid % 16;
-      a.scores_io[to] = a.scores_io[((size_t)page * a.hkv + kvh) * 16 + slot];
-    }
+    const uint64_t mask = __ballot(valid);
+    if (tid == 0) s_valid = mask;
+    if (valid && a.scores_io) score = a.scores_io[((size_t)page * a.hkv + kvh) * 16 + slot];
   }
   __syncthreads();
-  // keys: all loads, then all stores
-  u32x4 v[PER];
+  const uint64_t valid = s_valid;
+  // keys: 16-byte piece p % CPR of slot p / CPR; values: piece p is dims p / 2 % D,
+  // slots 8 (p & 1) .. + 7 of new page p / (2 D)
+  u32x4 k[PER];
+  uint16_t e[PER][8];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int p = tid + i * 256, s = p / CPR;
-    if (s_page[s] >= 0)
-      v[i] = ld16(a.kc + (((size_t)s_page[s] * a.hkv + kvh) * 16 + s_slot[s]) * D + p % CPR * 8);
+    k[i] = ld16(a.kc + (((size_t)s_page[s] * a.hkv + kvh) * 16 + s_slot[s]) * D + p % CPR * 8);
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int p = tid + i * 256, d = p / 2 % D, s0 = p / (2 * D) * 16 + (p & 1) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      e[i][j] = a.vc[((size_t)s_page[s0 + j] * a.hkv + kvh) * 16 * D + (size_t)d * 16 + s_slot[s0 + j]];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  if (tid < kEvictSlots && (valid >> tid & 1) && a.scores_io)
+    a.scores_io[((size_t)new_row[tid / 16] * a.hkv + kvh) * 16 + tid % 16] = score;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int p = tid + i * 256, s = p / CPR;
-    if (s_page[s] >= 0)
-      st16(a.kc + (((size_t)new_row[s / 16] * a.hkv + kvh) * 16 + s % 16) * D + p % CPR * 8, v[i]);
+    if (valid >> s & 1)
+      st16(a.kc + (((size_t)new_row[s / 16] * a.hkv + kvh) * 16 + s % 16) * D + p % CPR * 8, k[i]);
   }
-  // values: piece p is dims p / 2 % D, slots 8 (p & 1) .. + 7 of new page p / (2 D)
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int p = tid + i * 256, page = p / (2 * D), d = p / 2 % D, s0 = page * 16 + (p & 1) * 8;
-    uint32_t e[8];
-    bool all = true, any = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int old = s_page[s0 + j];
-      e[j] = 0;
-      all &= old >= 0;
-      any |= old >= 0;
-      if (old >= 0)
-        e[j] = a.vc[((size_t)old * a.hkv + kvh) * 16 * D + (size_t)d * 16 + s_slot[s0 + j]];
-    }
-    if (!any) continue;
+    const int p = tid + i * 256, page = p / (2 * D), d = p / 2 % D;
+    const uint32_t here = valid >> (page * 16 + (p & 1) * 8) & 0xFF;
+    if (!here) continue;
     uint16_t* to = a.vc + ((size_t)new_row[page] * a.hkv + kvh) * 16 * D + (size_t)d * 16 + (p & 1) * 8;
-    if (all) {
-      st16(to, u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16});
+    if (here == 0xFF) {
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = e[i][2 * j] | (uint32_t)e[i][2 * j + 1] << 16;
+      st16(to, v);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (s_page[s0 + j] >= 0) to[j] = (uint16_t)e[j];
+        if (here >> j & 1) to[j] = e[i][j];
     }
   }
 }

@@ -18,6 +18,7 @@ constexpr int kScoreWaveCols = 64;             // stationary vectors of a wave (
 constexpr int kSumKeys = 4 * kScoreWaveCols;   // keys of a tile of the second chunk pass
 constexpr int kLseMaxKeys = 32768;             // keys of one item of the first chunk pass
 constexpr int kJoinKeys = 1024;                // keys of one item of the decode join
+constexpr int kWholeLogits = 8192;             // logits of a decode row that one workgroup holds
 constexpr int kColsPad = 256;                  // a chunk request's columns are padded to this
 constexpr int kEvictSlots = 64;                // kept keys of one compaction item
 constexpr int kShortList = 8192;               // keys of a list that one workgroup selects from
@@ -67,11 +68,11 @@ struct ScoreItem {
   int32_t col0;     // first column (row * G + head in group) of the item
   int32_t cols_pad; // columns of the request, padded; decode lists: its padded length
   int32_t key0, key1;
-  int32_t split, nsplit;
+  int32_t split, nsplit;  // kListDecode: split -1, the whole row (no join)
   // float offsets in the workspace for kv head 0:
   //   chunk lists:   off0 = lse [Hkv][cols_pad]; off1 = (m, l) [Hkv][nsplit][cols_pad][2],
   //                  kListSum: sums [pieces][Hkv][len, padded to kSumKeys]
-  //   decode lists:  off0 = logits [Hkv][cols_pad / 32][32 G], off1 = records [Hkv][nsplit][record]
+  //   decode lists:  off0 = logits [Hkv][G][cols_pad], off1 = records [Hkv][nsplit][record]
   int64_t off0, off1;
 };
 static_assert(sizeof(ScoreItem) == 64, "score item size");

@@ -69,7 +69,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   if (n > 0 && (!q_len || !ctx_len)) return SSA_ERR_NULL;
   if (last_rows < 0) return SSA_ERR_ARG;
   const int hkv = s->num_kv_heads, g = s->num_q_heads / hkv, d = s->head_dim;
-  int64_t tokens = 0, keys = 0, decode_keys = 0, max_q = 0;
+  int64_t tokens = 0, keys = 0, decode_keys = 0, decode_rows = 0, max_q = 0;
   struct Chunk {
     int64_t cols, span;
   };
@@ -85,9 +85,10 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     max_q = std::max(max_q, c);
     const int64_t r = last_rows ? std::min<int64_t>(c, last_rows) : c;
     if (r * g > kMaxScoreCols) return SSA_ERR_LENGTH;
-    if (r == 1)
+    if (r == 1) {
       decode_keys += c + u;
-    else
+      ++decode_rows;
+    } else
       chunks.push_back({r * g, c + u});
   }
   ScoreHeader& h = p->hdr;
@@ -158,6 +159,21 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
       std::min(kDecodeMaxKeys, std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
                                                                   kDecodeStepKeys)));
 
+  // Rows that one workgroup does, at once and without a second launch: as long as its
+  // LDS holds the logits where there are enough rows for every compute unit, shorter
+  // ones where there are not.  Attention and scores in us, in pieces and whole (heads
+  // of 128, 32/8): 128 rows of 2048 keys 245 and 206, of 256 42 and 39; 8 rows of 2048 35
+  // and 33, of 512 25 and 17; 1 row of 2048 20 and 26, of 1024 16.5 and 16.9, of 512 15 and
+  // 12.  (8/8 heads of 64: 8 rows of 4096 32 and 38, 32 of 4096 60 and 57.)
+  // Beside chunk rows, which have a second launch anyway, only short ones (64 decodes
+  // of 512 to 4096 keys and a chunk: 98 us with rows of 2048 whole, 92 in pieces).
+  const int64_t decode_groups = decode_rows * hkv;
+  const int64_t whole_keys = std::min<int64_t>(
+      kWholeLogits / g, !chunks.empty()              ? 512
+                        : decode_groups >= kCus      ? kWholeLogits
+                        : decode_groups >= kCus / 4  ? 2048
+                                                     : 1024);
+
   int64_t ws = 0, row = 0;  // floats; token row
   std::vector<ScoreItem> sums;  // a chunk request's fields each
   auto take = [&](int64_t floats) {
@@ -180,6 +196,13 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     if (r == 1) {
       const int64_t padded = round_up(len, 32);
       it.cols_pad = (int32_t)padded;
+      if (padded <= whole_keys) {
+        it.nsplit = 1;
+        it.split = -1;
+        it.key1 = it.len;
+        p->list[kListDecode].push_back(it);
+        continue;
+      }
       it.nsplit = (int32_t)ceil_div(len, decode_piece);
       it.off0 = take(padded * g * hkv);
       it.off1 = take((int64_t)hkv * it.nsplit * score_rec_floats(g, d));

@@ -99,8 +99,10 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
   if (k0 + 4 <= key1) {
     if (a.scores_in && k0 + 4 <= it.ctx_len) {
       const f32x4 old = *reinterpret_cast<const f32x4*>(a.scores_in + at);
-      w += old * a.decay;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] += old[i] * a.decay;
     } else if (a.scores_in) {
+#pragma unroll
       for (int i = 0; i < 4; ++i)
         if (k0 + i < it.ctx_len) w[i] += a.scores_in[at + i] * a.decay;
     }
@@ -123,19 +125,51 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // tiles: the A rows of the two tiles are dealt so that a lane ends up with 8
 // consecutive keys of one column (head), which is also the layout of the B operand
 // of the P V product: no data moves between lanes but the block's maximum.  Logits are
-// stored as they lie, [32 keys][tile][quarter][G][4 keys]: each store instruction
-// writes one run of 64 G bytes.
+// stored as they lie, [G][32 keys][tile][quarter][4 keys]: a store instruction writes
+// 64 bytes of each head, and 8 threads of the join read 128.
+//
+// A row whose logits fit in LDS is one item: the workgroup turns them into scores and
+// writes the output itself.
+struct JoinLds {
+  float m[16], inv[16], inv_r[16];
+  __attribute__((aligned(16))) f32x4 part[kScoreThreads];
+};
 template <int D, bool OUT>
 struct DecodeLds {
+  static constexpr int kO = OUT ? 4 * 16 * D : 0;
   float ml[3][4][16];
-  __attribute__((aligned(16))) float o[OUT ? 4 * 16 * D : 4];
+  float m[16], inv[16], inv_r[16];
+  __attribute__((aligned(16))) float big[kO > kWholeLogits ? kO : kWholeLogits];  // logits, then o
 };
+
+// Four keys' weights from their logits, x[g * stride .. + 3] for head g.
+__device__ __forceinline__ f32x4 weights4(const ScoreArgs& a, const float* x, int stride,
+                                          const float* m, const float* inv) {
+  f32x4 w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int g = 0; g < a.g; ++g) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(x + (int64_t)g * stride);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(v[i], a.c, -m[g])) * inv[g];
+  }
+  return w;
+}
+// Where the logits of keys k0 .. k0 + 3 lie in a head's: quarter k0 / 8 % 4 of tile
+// k0 / 4 % 2 of their 32 keys.
+__device__ __forceinline__ int logits_at(int k0) {
+  return k0 / 32 * 32 + (k0 / 4 % 2) * 16 + k0 / 8 % 4 * 4;
+}
+__device__ __forceinline__ u32x2 pack4(f32x4 v) {
+  return u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
+
 template <int D, bool OUT>
 __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
                                             DecodeLds<D, OUT>& lds) {
   constexpr int KS = D / 32, DT = D / 16;
   auto& s_ml = lds.ml;
-  float* const s_o = lds.o;
+  float* const s_o = lds.big;
+  const bool whole = it.split < 0;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, quad = lane >> 4;
@@ -150,7 +184,8 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       v = ld16(a.q + ((size_t)it.q_row * a.hq + kvh * a.g + r16) * D + s * 32 + quad * 8);
     qf[s] = as_bf16x8(v);
   }
-  float* logits = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + (quad * a.g + r16) * 4;
+  float* logits = a.ws + it.off0 + ((int64_t)kvh * a.g + r16) * it.cols_pad + quad * 4;
+  float* held = lds.big + (whole ? r16 * it.cols_pad : 0) + quad * 4;
   float m = -kInf, l = 0.f, lr = 0.f;
   f32x4 o[OUT ? DT : 1];
 #pragma unroll
@@ -200,9 +235,13 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     __builtin_amdgcn_sched_barrier(0);
     float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
     if (r16 < a.g) {
-      float* to = logits + (int64_t)kb * a.g;
-      *reinterpret_cast<f32x4*>(to) = s0;
-      *reinterpret_cast<f32x4*>(to + 16 * a.g) = s1;
+      if (whole) {
+        *reinterpret_cast<f32x4*>(held + kb) = s0;
+        *reinterpret_cast<f32x4*>(held + kb + 16) = s1;
+      } else {
+        *reinterpret_cast<f32x4*>(logits + kb) = s0;
+        *reinterpret_cast<f32x4*>(logits + kb + 16) = s1;
+      }
     }
     const int nv = it.key1 - kb - 8 * quad;  // this lane's keys that exist
     if (kb + 32 > it.key1) {
@@ -269,11 +308,6 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     s_ml[1][wave][r16] = l;
     s_ml[2][wave][r16] = lr;
   }
-  if constexpr (OUT) {
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-      *reinterpret_cast<f32x4*>(s_o + (wave * 16 + r16) * D + t * 16 + 4 * quad) = o[t];
-  }
   __syncthreads();
   float* rec = a.ws + it.off1 + ((int64_t)kvh * it.nsplit + it.split) * score_rec_floats(a.g, D);
   if (tid < a.g) {
@@ -287,33 +321,46 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       ll += s_ml[1][w][tid] * f;
       rr += s_ml[2][w][tid] * f;
     }
-    rec[tid] = mm;
-    rec[a.g + tid] = ll;
-    rec[2 * a.g + tid] = rr;
+    lds.m[tid] = ms;
+    lds.inv[tid] = 1.f / ll;
+    lds.inv_r[tid] = 1.f / rr;
+    if (!whole) {
+      rec[tid] = mm;
+      rec[a.g + tid] = ll;
+      rec[2 * a.g + tid] = rr;
+    }
+  }
+  if (whole) {
+    __syncthreads();
+    for (int k0 = tid * 4; k0 < it.len; k0 += kScoreThreads * 4)
+      add_scores4(a, it, kvh, k0, it.len, weights4(a, lds.big + logits_at(k0), it.cols_pad, lds.m, lds.inv));
   }
   if constexpr (OUT) {
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      *reinterpret_cast<f32x4*>(s_o + (wave * 16 + r16) * D + t * 16 + 4 * quad) = o[t];
+    __syncthreads();
     float* ro = rec + score_rec_o(a.g);
     for (int e = tid * 4; e < a.g * D; e += kScoreThreads * 4) {
       const int g = e / D, d = e % D;
-      float mm = -kInf;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[0][w][g]);
-      const float ms = mm == -kInf ? 0.f : mm;
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < 4; ++w)
         v += *reinterpret_cast<const f32x4*>(s_o + (w * 16 + g) * D + d) *
-             exp2_fast(s_ml[0][w][g] - ms);
-      *reinterpret_cast<f32x4*>(ro + e) = v;
+             exp2_fast(s_ml[0][w][g] - lds.m[g]);
+      if (whole)
+        *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + d) =
+            pack4(v * lds.inv_r[g]);
+      else
+        *reinterpret_cast<f32x4*>(ro + e) = v;
     }
   }
 }
 
-// One counted row: join the key ranges' sums, turn a range's logits into scores;
-// the first range's workgroup also joins the attention output.
-struct JoinLds {
-  float m[16], inv[16], inv_r[16];
-};
+// One counted row: join the key ranges' sums, turn a range's logits into scores.  The
+// row's items share out its output, a few 4-dim pieces each, whose records all
+// threads read.
 template <int D, bool OUT>
 __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
                                                  JoinLds& lds) {
@@ -348,33 +395,32 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
   __syncthreads();
   const int k0 = it.key0 + tid * 4;
   if (k0 < it.key1) {
-    // keys k0 .. k0 + 3 are quarter k0 / 8 % 4 of tile k0 / 4 % 2 of their 32
-    const float* lg = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad +
-                      ((int64_t)(k0 / 32) * 8 + (k0 / 4 % 2) * 4 + k0 / 8 % 4) * a.g * 4;
-    f32x4 w = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int g = 0; g < a.g; ++g) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(lg + g * 4);
-      const float m = s_m[g], inv = s_inv[g];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] += exp2_fast(__builtin_fmaf(x[i], a.c, -m)) * inv;
-    }
-    add_scores4(a, it, kvh, k0, it.key1, w);
+    const float* lg = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + logits_at(k0);
+    add_scores4(a, it, kvh, k0, it.key1, weights4(a, lg, it.cols_pad, s_m, s_inv));
   }
   if constexpr (OUT) {
-    if (it.key0 == 0) {
-      for (int e = tid * 4; e < a.g * D; e += kScoreThreads * 4) {
-        const int g = e / D, d = e % D;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    const int items = (it.len + kJoinKeys - 1) / kJoinKeys, pieces = a.g * D / 4;
+    const int per = (pieces + items - 1) / items;  // pieces of an item, at most 512
+    const int first = it.key0 / kJoinKeys * per, mine = min(per, pieces - first);
+    for (int p0 = 0; p0 < mine; p0 += kScoreThreads) {
+      const int n = min(kScoreThreads, mine - p0);   // pieces of this round ...
+      const int lanes = kScoreThreads / n;           // ... and the threads of each
+      const int p = tid % n, lane0 = tid / n, e = (first + p0 + p) * 4, g = e / D;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (lane0 < lanes)
 #pragma unroll 4
-        for (int s = 0; s < it.nsplit; ++s) {
+        for (int s = lane0; s < it.nsplit; s += lanes) {
           const float* r = recs + (int64_t)s * stride;
           v += *reinterpret_cast<const f32x4*>(r + score_rec_o(a.g) + e) * exp2_fast(r[g] - s_m[g]);
         }
-        v *= s_inv_r[g];
-        u32x2 b = {pack2(v[0], v[1]), pack2(v[2], v[3])};
-        *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + d) = b;
+      lds.part[tid] = v;
+      __syncthreads();
+      if (tid < n) {
+        for (int x = 1; x < lanes; ++x) v += lds.part[x * n + tid];
+        *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + e % D) =
+            pack4(v * s_inv_r[g]);
       }
+      __syncthreads();
     }
   }
 }

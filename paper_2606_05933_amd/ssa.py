@@ -425,7 +425,7 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -590,33 +590,6 @@ def rope_append(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_cac
                              vp(_stream(stream)))
     if rc != SSA_OK:
         raise SsaError(rc, "ssa_rope_append")
-
-
-def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shift_host, shift_dev,
-                        q_out, k_cache, v_cache, block_table, stream=None):
-    """ssa_rope_append_shifted: rope_append of requests that have lost keys to an
-    eviction; request i's tokens are rotated shift_host[i] (int32 array; shift_dev
-    the same on the device) positions past their cache index."""
-    h = _plan_header(plan_host)
-    T, n = h["num_tokens"], h["num_reqs"]
-    d, hq, hkv = shape.head_dim, shape.num_q_heads, shape.num_kv_heads
-    pool = shape.num_pages * hkv * shape.page_size * d
-    _check_dev("qkv", qkv, T * (hq + 2 * hkv) * d, 2)
-    _check_dev("q_out", q_out, T * hq * d, 2)
-    _check_dev("cos_sin", cos_sin, d, 4)
-    _check_dev("k_cache", k_cache, pool, 2)
-    _check_dev("v_cache", v_cache, pool, 2)
-    _check_dev("block_table", block_table, n * shape.max_pages_per_req, 4)
-    _check_dev("shift_dev", shift_dev, n, 4)
-    shift, shift_ptr = _lens(shift_host)
-    if shift.shape[0] != n:
-        raise ValueError(f"{shift.shape[0]} shifts for {n} requests")
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_rope_append_shifted(
-        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(qkv)),
-        vp(_ptr(cos_sin)), int(cos_sin.numel() // d), vp(shift_ptr), vp(_ptr(shift_dev)),
-        vp(_ptr(q_out)), vp(_ptr(k_cache)), vp(_ptr(v_cache)), vp(_ptr(block_table)),
-        vp(_stream(stream))), "ssa_rope_append_shifted")
 
 
 def linear_workspace_size(m: int, n: int, k: int) -> int:
@@ -884,7 +857,9 @@ def bind_plan(shape: SsaShape, q_len, ctx_len, tuning, out, info: SsaPlanInfo) -
     return call
 
 
-# Eviction from the cache by accumulated attention weight (include/ssa_evict.h).
+# Eviction from the cache by accumulated attention weight (include/ssa_evict.h).  A serving
+# loop makes these calls for every layer: the wrappers do no more per call than check
+# each buffer once.
 
 def _plan_buffer(out, nbytes: int):
     """(buffer, address, bytes) of a plan: `out`, or a new numpy array."""
@@ -926,109 +901,177 @@ def evict_plan(shape: SsaShape, kv_len, budget, sink: int, recent: int, out=None
     return out, wb.value
 
 
-def _evict_header(plan_host):
-    """num_reqs (and tokens of a score plan, kept keys of an eviction plan) of a blob
-    (ssa_evict_format.h)."""
-    b = np.asarray(_as_np(plan_host))[:128].tobytes()
-    i, q = np.frombuffer(b, dtype=np.int32), np.frombuffer(b, dtype=np.int64)
-    if i[0] == 0x31435353:  # a score plan
-        return {"num_reqs": int(i[4]), "num_tokens": int(i[5])}
-    return {"num_reqs": int(i[3]), "num_keep": int(q[10])}
+# The 128-byte plan headers (ssa_evict_format.h, ssa_plan_format.h).
+_SCORE_MAGIC, _EVICT_MAGIC, _PLAN_MAGIC = 0x31435353, 0x31565353, 0x31415353
 
 
-def _scored_args(name, shape, plan_host, plan_dev, q, k_cache, block_table, scores_in, decay,
-                 scores_out, workspace):
-    h = _evict_header(plan_host)
+def _header(plan_host, magic: int, what: str):
+    """Address of a plan and its header as int32 words, checked for its kind."""
+    at = _ptr(plan_host)
+    if at is None:
+        raise SsaError(SSA_ERR_NULL, what)
+    words = (ctypes.c_int32 * 32).from_address(at)
+    if words[0] != magic:
+        raise SsaError(SSA_ERR_PLAN_MISMATCH, what)
+    return at, words
+
+
+class _Buffers:
+    """Checks the buffers of one call, which have to be on the current device (the
+    call's stream is one of it), and gives their addresses."""
+
+    def __init__(self):
+        import torch
+        self.device = torch.cuda.current_device()
+
+    def __call__(self, name, t, numel, itemsize):
+        if t is None:
+            return None
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must be a tensor on the current device")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.element_size() != itemsize:
+            raise ValueError(f"{name} must have {itemsize}-byte elements")
+        if t.numel() < numel:
+            raise ValueError(f"{name} holds {t.numel()} elements, the layout needs {numel}")
+        return t.data_ptr()
+
+    def plan(self, plan_dev, plan_host):
+        """The plan as the kernels read it: on the device, or the pinned host buffer."""
+        if plan_dev is None:
+            return None
+        if isinstance(plan_dev, np.ndarray):
+            raise ValueError("plan_dev must be a device tensor or a pinned host tensor")
+        if plan_dev.get_device() != self.device and not plan_dev.is_pinned():
+            raise ValueError("plan_dev must be on the current device or pinned")
+        need = plan_host.nbytes if isinstance(plan_host, np.ndarray) else (
+            plan_host.numel() * plan_host.element_size())
+        if plan_dev.numel() * plan_dev.element_size() < need or not plan_dev.is_contiguous():
+            raise ValueError(f"plan_dev must hold the plan's {need} bytes")
+        return plan_dev.data_ptr()
+
+    def workspace(self, t):
+        """(address, bytes); the library checks the size."""
+        if t is None:
+            return None, 0
+        return self("workspace", t, 0, t.element_size()), t.numel() * t.element_size()
+
+
+def _scored_args(what, shape, plan_host, plan_dev, q, k_cache, block_table, scores_in, scores_out,
+                 workspace):
+    at, h = _header(plan_host, _SCORE_MAGIC, what)
+    check = _Buffers()
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
-    rows = h.get("num_tokens", 0) * shape.num_q_heads * shape.head_dim
-    _check_dev("q", q, rows, 2)
-    _check_dev("k_cache", k_cache, slots * shape.head_dim, 2)
-    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
-    _check_dev("scores_in", scores_in, slots, 4)
-    _check_dev("scores_out", scores_out, slots, 4)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    return rows, ws_bytes
+    rows = h[5] * shape.num_q_heads * shape.head_dim
+    return (check, rows, at, check.plan(plan_dev, plan_host), check("q", q, rows, 2),
+            check("k_cache", k_cache, slots * shape.head_dim, 2),
+            check("block_table", block_table, h[4] * shape.max_pages_per_req, 4),
+            check("scores_in", scores_in, slots, 4), check("scores_out", scores_out, slots, 4),
+            *check.workspace(workspace))
 
 
 def key_scores(shape: SsaShape, plan_host, plan_dev, q, k_cache, block_table, scores_in,
                decay: float, scores_out, workspace, stream=None):
     """ssa_key_scores: a batch's attention weights, added per cached key and kv head
     (fp32 [num_pages, Hkv, 16]) to decay times scores_in (None: to nothing)."""
-    _, ws_bytes = _scored_args("ssa_key_scores", shape, plan_host, plan_dev, q, k_cache,
-                               block_table, scores_in, decay, scores_out, workspace)
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_key_scores(
-        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(q)),
-        vp(_ptr(k_cache)), vp(_ptr(block_table)), vp(_ptr(scores_in)), float(decay),
-        vp(_ptr(scores_out)), vp(_ptr(workspace)), ctypes.c_size_t(ws_bytes),
-        vp(_stream(stream))), "ssa_key_scores")
+    _, _, at, pd, pq, pk, bt, si, so, ws, n = _scored_args(
+        "ssa_key_scores", shape, plan_host, plan_dev, q, k_cache, block_table, scores_in,
+        scores_out, workspace)
+    rc = LIB.ssa_key_scores(shape, at, pd, pq, pk, bt, si, decay, so, ws, n, _stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_key_scores")
 
 
 def decode_scored(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, block_table,
                   scores_in, decay: float, scores_out, out, workspace, stream=None):
     """ssa_decode_scored: attention of a pure-decode batch (out as
     ssa_mixed_attention's) and its weights (scores_out as key_scores')."""
-    rows, ws_bytes = _scored_args("ssa_decode_scored", shape, plan_host, plan_dev, q, k_cache,
-                                  block_table, scores_in, decay, scores_out, workspace)
-    _check_dev("v_cache", v_cache,
-               shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim, 2)
-    _check_dev("out", out, rows, 2)
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_decode_scored(
-        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(q)),
-        vp(_ptr(k_cache)), vp(_ptr(v_cache)), vp(_ptr(block_table)), vp(_ptr(scores_in)),
-        float(decay), vp(_ptr(scores_out)), vp(_ptr(out)), vp(_ptr(workspace)),
-        ctypes.c_size_t(ws_bytes), vp(_stream(stream))), "ssa_decode_scored")
+    check, rows, at, pd, pq, pk, bt, si, so, ws, n = _scored_args(
+        "ssa_decode_scored", shape, plan_host, plan_dev, q, k_cache, block_table, scores_in,
+        scores_out, workspace)
+    pool = shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim
+    rc = LIB.ssa_decode_scored(shape, at, pd, pq, pk, check("v_cache", v_cache, pool, 2), bt, si,
+                               decay, so, check("out", out, rows, 2), ws, n, _stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_decode_scored")
+
+
+def _num_keep(h, shape) -> int:
+    """Entries of the kept keys' lists, from an eviction plan's header."""
+    return (h[20] & 0xFFFFFFFF | h[21] << 32) * shape.num_kv_heads
 
 
 def evict_select(shape: SsaShape, plan_host, plan_dev, scores, block_table, keep, workspace,
                  stream=None):
     """ssa_evict_select: the kept keys' cache indexes (int32, flat: per request Hkv
     ascending lists) by the plan's sinks, recent keys and highest scores."""
-    h = _evict_header(plan_host)
-    _check_dev("scores", scores, shape.num_pages * shape.num_kv_heads * shape.page_size, 4)
-    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
-    _check_dev("keep", keep, h.get("num_keep", 0) * shape.num_kv_heads, 4)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_evict_select(
-        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(scores)),
-        vp(_ptr(block_table)), vp(_ptr(keep)), vp(_ptr(workspace)), ctypes.c_size_t(ws_bytes),
-        vp(_stream(stream))), "ssa_evict_select")
+    at, h = _header(plan_host, _EVICT_MAGIC, "ssa_evict_select")
+    check = _Buffers()
+    ws, n = check.workspace(workspace)
+    slots = shape.num_pages * shape.num_kv_heads * shape.page_size
+    rc = LIB.ssa_evict_select(
+        shape, at, check.plan(plan_dev, plan_host), check("scores", scores, slots, 4),
+        check("block_table", block_table, h[3] * shape.max_pages_per_req, 4),
+        check("keep", keep, _num_keep(h, shape), 4), ws, n, _stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_evict_select")
 
 
 def evict_compact(shape: SsaShape, plan_host, plan_dev, keep, block_table, new_table, k_cache,
                   v_cache, scores=None, stream=None):
     """ssa_evict_compact: the kept keys, values and scores move to the pages of
     new_table (as check_evict_tables wants them)."""
-    h = _evict_header(plan_host)
+    at, h = _header(plan_host, _EVICT_MAGIC, "ssa_evict_compact")
+    check = _Buffers()
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
-    _check_dev("keep", keep, h.get("num_keep", 0) * shape.num_kv_heads, 4)
-    _check_dev("block_table", block_table, h["num_reqs"] * shape.max_pages_per_req, 4)
-    _check_dev("new_table", new_table, h["num_reqs"] * shape.max_pages_per_req, 4)
-    _check_dev("k_cache", k_cache, slots * shape.head_dim, 2)
-    _check_dev("v_cache", v_cache, slots * shape.head_dim, 2)
-    _check_dev("scores", scores, slots, 4)
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_evict_compact(
-        ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)), vp(_ptr(keep)),
-        vp(_ptr(block_table)), vp(_ptr(new_table)), vp(_ptr(k_cache)), vp(_ptr(v_cache)),
-        vp(_ptr(scores)), vp(_stream(stream))), "ssa_evict_compact")
+    entries = h[3] * shape.max_pages_per_req
+    rc = LIB.ssa_evict_compact(
+        shape, at, check.plan(plan_dev, plan_host), check("keep", keep, _num_keep(h, shape), 4),
+        check("block_table", block_table, entries, 4), check("new_table", new_table, entries, 4),
+        check("k_cache", k_cache, slots * shape.head_dim, 2),
+        check("v_cache", v_cache, slots * shape.head_dim, 2), check("scores", scores, slots, 4),
+        _stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_evict_compact")
 
 
 def check_evict_tables(shape: SsaShape, plan_host, block_table_host, new_table_host=None) -> None:
     """ssa_check_evict_tables on host copies (int32 [num_reqs, max_pages_per_req]);
     raises SsaError on a page outside the pool or a new page that is not free."""
-    n = _evict_header(plan_host)["num_reqs"]
+    at, h = _header(plan_host, _EVICT_MAGIC, "ssa_check_evict_tables")
     tables = []
     for t in (block_table_host, new_table_host):
         if t is not None:
             t = np.ascontiguousarray(t, dtype=np.int32)
-            if t.shape != (n, shape.max_pages_per_req):
+            if t.shape != (h[3], shape.max_pages_per_req):
                 raise ValueError(f"table of shape {t.shape}, the plan needs "
-                                 f"({n}, {shape.max_pages_per_req})")
+                                 f"({h[3]}, {shape.max_pages_per_req})")
         tables.append(t)
-    vp = ctypes.c_void_p
-    _check(LIB.ssa_check_evict_tables(ctypes.byref(shape), vp(_ptr(plan_host)),
-                                      vp(_ptr(tables[0])), vp(_ptr(tables[1]))),
+    _check(LIB.ssa_check_evict_tables(shape, at, _ptr(tables[0]), _ptr(tables[1])),
            "ssa_check_evict_tables")
+
+
+def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shift_host, shift_dev,
+                        q_out, k_cache, v_cache, block_table, stream=None):
+    """ssa_rope_append_shifted: rope_append of requests that have lost keys to an
+    eviction; request i's tokens are rotated shift_host[i] (int32 array; shift_dev
+    the same on the device) positions past their cache index."""
+    at, h = _header(plan_host, _PLAN_MAGIC, "ssa_rope_append_shifted")
+    check = _Buffers()
+    n, tokens, d, hq, hkv = h[4], h[5], shape.head_dim, shape.num_q_heads, shape.num_kv_heads
+    pool = shape.num_pages * hkv * shape.page_size * d
+    if not (isinstance(shift_host, np.ndarray) and shift_host.dtype == np.int32
+            and shift_host.flags.c_contiguous):
+        shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
+    if shift_host.size != n:
+        raise ValueError(f"{shift_host.size} shifts for {n} requests")
+    rc = LIB.ssa_rope_append_shifted(
+        shape, at, check.plan(plan_dev, plan_host),
+        check("qkv", qkv, tokens * (hq + 2 * hkv) * d, 2), check("cos_sin", cos_sin, d, 4),
+        cos_sin.numel() // d, shift_host.ctypes.data, check("shift_dev", shift_dev, n, 4),
+        check("q_out", q_out, tokens * hq * d, 2), check("k_cache", k_cache, pool, 2),
+        check("v_cache", v_cache, pool, 2),
+        check("block_table", block_table, n * shape.max_pages_per_req, 4), _stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_rope_append_shifted")

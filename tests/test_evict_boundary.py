@@ -74,6 +74,10 @@ def test_score_plans_cover_the_batch_once_and_stay_in_the_workspace(seed):
         if rows == 1:
             dec = mine["decode"]
             partition(dec)
+            if dec["split"][0] == -1:  # the whole row in one workgroup, its logits in LDS
+                assert len(dec) == 1 and not len(mine["decode_join"])
+                assert dec["cols_pad"][0] * g <= 8192
+                continue
             partition(mine["decode_join"])
             assert (dec["key0"] % 128 == 0).all() and (mine["decode_join"]["key0"] % 16 == 0).all()
             pad, ns = int(dec["cols_pad"][0]), int(dec["nsplit"][0])

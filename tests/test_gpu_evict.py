@@ -141,8 +141,9 @@ def test_decode_rows_at_every_block_edge(torch_dev, heads, out):
         x.check_out()
 
 
-@pytest.mark.parametrize("heads,u", [((8, 2, 128), [20001, 4097, 9]), ((64, 8, 128), [33000]),
-                                     ((2, 1, 64), [70000, 1])])
+@pytest.mark.parametrize("heads,u", [((8, 2, 128), [20001, 4097, 9, 2047, 2048]), ((64, 8, 128), [33000]),
+                                     ((2, 1, 64), [70000, 1]), ((16, 1, 64), [511, 512, 6000, 1025]),
+                                     ((13, 1, 128), [140000, 3])])
 def test_long_decodes_join_their_pieces(torch_dev, heads, u):
     x = Scored(torch_dev, batch(*heads, [1] * len(u), u, seed=4), q_scale=2)
     x.decode()
