@@ -156,7 +156,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   h.lse_groups = 1 << lse_k;
   h.sum_cols = (int32_t)sum_cols;
   const int64_t decode_piece =
-      std::min(kDecodeMaxKeys, std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
+      std::min(std::min(kDecodeMaxKeys, kWholeLogits / g / kDecodeStepKeys * kDecodeStepKeys), std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
                                                                   kDecodeStepKeys)));
 
   // Rows that one workgroup does, at once and without a second launch: as long as its

@@ -184,8 +184,9 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       v = ld16(a.q + ((size_t)it.q_row * a.hq + kvh * a.g + r16) * D + s * 32 + quad * 8);
     qf[s] = as_bf16x8(v);
   }
-  float* logits = a.ws + it.off0 + ((int64_t)kvh * a.g + r16) * it.cols_pad + quad * 4;
-  float* held = lds.big + (whole ? r16 * it.cols_pad : 0) + quad * 4;
+  // the item's logits, in LDS until it has read its keys
+  const int stride = (it.key1 - it.key0 + 31) / 32 * 32;
+  float* held = lds.big + r16 * stride + quad * 4 - it.key0;
   float m = -kInf, l = 0.f, lr = 0.f;
   f32x4 o[OUT ? DT : 1];
 #pragma unroll
@@ -235,13 +236,8 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     __builtin_amdgcn_sched_barrier(0);
     float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
     if (r16 < a.g) {
-      if (whole) {
-        *reinterpret_cast<f32x4*>(held + kb) = s0;
-        *reinterpret_cast<f32x4*>(held + kb + 16) = s1;
-      } else {
-        *reinterpret_cast<f32x4*>(logits + kb) = s0;
-        *reinterpret_cast<f32x4*>(logits + kb + 16) = s1;
-      }
+      *reinterpret_cast<f32x4*>(held + kb) = s0;
+      *reinterpret_cast<f32x4*>(held + kb + 16) = s1;
     }
     const int nv = it.key1 - kb - 8 * quad;  // this lane's keys that exist
     if (kb + 32 > it.key1) {
@@ -333,7 +329,13 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
   if (whole) {
     __syncthreads();
     for (int k0 = tid * 4; k0 < it.len; k0 += kScoreThreads * 4)
-      add_scores4(a, it, kvh, k0, it.len, weights4(a, lds.big + logits_at(k0), it.cols_pad, lds.m, lds.inv));
+      add_scores4(a, it, kvh, k0, it.len, weights4(a, lds.big + logits_at(k0), stride, lds.m, lds.inv));
+  } else {
+    float* to = a.ws + it.off0 + (int64_t)kvh * a.g * it.cols_pad + it.key0;
+    for (int g = wave; g < a.g; g += 4)
+      for (int k = lane * 4; k < stride; k += 256)
+        *reinterpret_cast<f32x4*>(to + (int64_t)g * it.cols_pad + k) =
+            *reinterpret_cast<const f32x4*>(lds.big + g * stride + k);
   }
   if constexpr (OUT) {
     __syncthreads();
