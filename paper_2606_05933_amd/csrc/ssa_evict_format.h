@@ -77,9 +77,9 @@ struct ScoreItem {
 };
 static_assert(sizeof(ScoreItem) == 64, "score item size");
 
-// One key range's record of a decode row: m, l and the l of the rounded weights for
-// G heads, padded to four floats, then o [G][D].
-constexpr int score_rec_o(int g) { return (3 * g + 3) / 4 * 4; }
+// One key range's record of a decode row: m and l for G heads, padded to four floats,
+// then o [G][D].
+constexpr int score_rec_o(int g) { return (2 * g + 3) / 4 * 4; }
 constexpr int score_rec_floats(int g, int d) { return score_rec_o(g) + g * d; }
 
 struct EvictHeader {

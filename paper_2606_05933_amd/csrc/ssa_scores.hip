@@ -131,14 +131,14 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // A row whose logits fit in LDS is one item: the workgroup turns them into scores and
 // writes the output itself.
 struct JoinLds {
-  float m[16], inv[16], inv_r[16];
+  float m[16], inv[16];
   __attribute__((aligned(16))) f32x4 part[kScoreThreads];
 };
 template <int D, bool OUT>
 struct DecodeLds {
   static constexpr int kO = OUT ? 4 * 16 * D : 0;
-  float ml[3][4][16];
-  float m[16], inv[16], inv_r[16];
+  float ml[2][4][16];
+  float m[16], inv[16];
   __attribute__((aligned(16))) float big[kO > kWholeLogits ? kO : kWholeLogits];  // logits, then o
 };
 
@@ -187,7 +187,7 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
   // the item's logits, in LDS until it has read its keys
   const int stride = (it.key1 - it.key0 + 31) / 32 * 32;
   float* held = lds.big + r16 * stride + quad * 4 - it.key0;
-  float m = -kInf, l = 0.f, lr = 0.f;
+  float m = -kInf, l = 0.f;
   f32x4 o[OUT ? DT : 1];
 #pragma unroll
   for (int t = 0; t < (OUT ? DT : 1); ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -265,16 +265,15 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     l = l * alpha + sum;
     m = mn;
     if constexpr (OUT) {
-      // The weights are rounded to bf16 for the matrix product, and the output is
-      // divided by the sum of the rounded ones: the weights applied add up to 1.
-      u32x4 pk;
-      float rs = 0.f;
+      // A weight enters the matrix product as two bf16 values, the rounded one and
+      // what that misses (16 bits of it together): memory bounds this loop, and one alone
+      // put as much error into the output as its own rounding to bf16.
+      u32x4 hi, lo;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        pk[w] = pack2(p[2 * w], p[2 * w + 1]);
-        rs += bf16_lo(pk[w]) + bf16_hi(pk[w]);
+        hi[w] = pack2(p[2 * w], p[2 * w + 1]);
+        lo[w] = pack2(p[2 * w] - bf16_lo(hi[w]), p[2 * w + 1] - bf16_hi(hi[w]));
       }
-      lr = lr * alpha + rs;
       if (__any(alpha != 1.f)) {
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= alpha;
@@ -290,40 +289,34 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
           }
       }
 #pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(pk), o[t]);
+      for (int t = 0; t < DT; ++t) {
+        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(hi), o[t]);
+        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(lo), o[t]);
+      }
       if (more) load_values(p0, p1);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  lr += __shfl_xor(lr, 16, 64);
-  lr += __shfl_xor(lr, 32, 64);
   if (quad == 0) {
     s_ml[0][wave][r16] = m;
     s_ml[1][wave][r16] = l;
-    s_ml[2][wave][r16] = lr;
   }
   __syncthreads();
   float* rec = a.ws + it.off1 + ((int64_t)kvh * it.nsplit + it.split) * score_rec_floats(a.g, D);
   if (tid < a.g) {
-    float mm = -kInf, ll = 0.f, rr = 0.f;
+    float mm = -kInf, ll = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[0][w][tid]);
     const float ms = mm == -kInf ? 0.f : mm;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = exp2_fast(s_ml[0][w][tid] - ms);
-      ll += s_ml[1][w][tid] * f;
-      rr += s_ml[2][w][tid] * f;
-    }
+    for (int w = 0; w < 4; ++w) ll += s_ml[1][w][tid] * exp2_fast(s_ml[0][w][tid] - ms);
     lds.m[tid] = ms;
     lds.inv[tid] = 1.f / ll;
-    lds.inv_r[tid] = 1.f / rr;
     if (!whole) {
       rec[tid] = mm;
       rec[a.g + tid] = ll;
-      rec[2 * a.g + tid] = rr;
     }
   }
   if (whole) {
@@ -353,7 +346,7 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
              exp2_fast(s_ml[0][w][g] - lds.m[g]);
       if (whole)
         *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + d) =
-            pack4(v * lds.inv_r[g]);
+            pack4(v * lds.inv[g]);
       else
         *reinterpret_cast<f32x4*>(ro + e) = v;
     }
@@ -366,7 +359,7 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
 template <int D, bool OUT>
 __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
                                                  JoinLds& lds) {
-  auto &s_m = lds.m, &s_inv = lds.inv, &s_inv_r = lds.inv_r;
+  auto &s_m = lds.m, &s_inv = lds.inv;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int stride = score_rec_floats(a.g, D);
   const float* recs = a.ws + it.off1 + (int64_t)kvh * it.nsplit * stride;
@@ -376,22 +369,16 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
     const float ms = m == -kInf ? 0.f : m;
-    float l = 0.f, lr = 0.f;
+    float l = 0.f;
     for (int s = lane; s < it.nsplit; s += 64) {
       const float* r = recs + (int64_t)s * stride;
-      const float f = exp2_fast(r[g] - ms);
-      l += r[a.g + g] * f;
-      lr += r[2 * a.g + g] * f;
+      l += r[a.g + g] * exp2_fast(r[g] - ms);
     }
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) {
-      l += __shfl_xor(l, x, 64);
-      lr += __shfl_xor(lr, x, 64);
-    }
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
     if (lane == 0) {
       s_m[g] = ms;
       s_inv[g] = 1.f / l;
-      s_inv_r[g] = 1.f / lr;
     }
   }
   __syncthreads();
@@ -420,7 +407,7 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
       if (tid < n) {
         for (int x = 1; x < lanes; ++x) v += lds.part[x * n + tid];
         *reinterpret_cast<u32x2*>(a.out + ((size_t)it.q_row * a.hq + kvh * a.g + g) * D + e % D) =
-            pack4(v * s_inv_r[g]);
+            pack4(v * s_inv[g]);
       }
       __syncthreads();
     }

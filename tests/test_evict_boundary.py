@@ -84,7 +84,7 @@ def test_score_plans_cover_the_batch_once_and_stay_in_the_workspace(seed):
             assert pad % 32 == 0 and pad >= length and ns == len(dec)
             assert sorted(dec["split"]) == list(range(ns))
             taken.append((int(dec["off0"][0]), hkv * g * pad))
-            taken.append((int(dec["off1"][0]), hkv * ns * ((3 * g + 3) // 4 * 4 + g * d)))
+            taken.append((int(dec["off1"][0]), hkv * ns * ((2 * g + 3) // 4 * 4 + g * d)))
             continue
         lse, cols = mine["lse"], rows * g
         pad, ns = int(lse["cols_pad"][0]), int(lse["nsplit"][0])

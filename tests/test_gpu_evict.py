@@ -9,9 +9,9 @@ Bars, from the arithmetic:
   2^-24 each along the longest chain (here under L / 32 + 128, L keys, for a
   sum over keys, and under R / 32 + 128 for one over R columns).  So
       |err| <= ref 2^-24 (2 D A + 8 A + 2 (L + R) / 32 + 512).
-* attention outputs: that relative error and two roundings to bf16 (the weight's and
-  the sum's of rounded weights) of every |w v|, and the result's own rounding:
-      |err| <= 2^-8 |ref| + (2^-7 + 2 rel) sum |w v|.
+* attention outputs: that relative error, a weight's rounding to two bf16 values (2^-16),
+  fp32 sums (in the bar above) of every |w v|, and the result's own rounding to bf16:
+      |err| <= 2^-8 |ref| + (2^-16 + 2 rel) sum |w v|.
 * keys, values, indexes: bit for bit.
 """
 import sys
@@ -112,7 +112,7 @@ class Scored:
         _, size = evict.key_scores(b, self.kc, self.window)
         rel = self.rel(np.nanmax(size))
         got = self.out.float().cpu().numpy().astype(np.float64)
-        err, tol = np.abs(got - ref), 2.0 ** -8 * np.abs(ref) + (2.0 ** -7 + 2 * rel) * mass
+        err, tol = np.abs(got - ref), 2.0 ** -8 * np.abs(ref) + (2.0 ** -16 + 2 * rel) * mass
         assert (err <= tol).all(), (float(np.nanmax(err)), np.argwhere(~(err <= tol))[:5])
 
 
