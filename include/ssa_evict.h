@@ -26,6 +26,7 @@
  * plans are position-independent but not interchangeable with ssa_plan's.
  * Workspaces need no clearing: a call reads nothing of them that it has not
  * written itself.  Calls that share a workspace must be ordered on one stream.
+ * Pointers to queries, pools, scores, outputs and workspaces are 16-byte aligned.
  * Results do not depend on the order in which workgroups run (no atomics on
  * outputs).  All calls can be captured into a HIP graph; the plan at plan_dev
  * must then stay as it is for the replays.
@@ -50,8 +51,9 @@ extern "C" {
  *              0: all of them
  *   ws_bytes   the workspace of the calls with this plan.  The attention logits
  *              of requests with one counted row take 4 Hq bytes per key of it.
- * Errors: those of ssa_plan_size (without TUNING); SSA_ERR_ARG (last_rows < 0);
- * SSA_ERR_PLAN_SIZE (plan_bytes too small).
+ * Errors: those of ssa_plan_size (without TUNING); SHAPE also for Hq D > 2^24;
+ * LENGTH also for more than 2^28 counted rows times heads of a group, and where the
+ * plan would pass 2 GiB; ARG (last_rows < 0); PLAN_SIZE (plan_bytes too small).
  */
 int ssa_score_plan_size(const ssa_shape* shape, const int32_t* q_len_host,
                         const int32_t* ctx_len_host, int32_t num_reqs, int32_t last_rows,
@@ -75,7 +77,8 @@ int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int3
  *   decay       finite, >= 0
  *   Requests with c_i = 0, slots past a request's last key and other pages are
  *   left as they are.  Pages must not be shared between requests with c_i > 0.
- * Errors: NULL, the shape errors, PLAN_MISMATCH, ARG (decay), WORKSPACE, HIP.
+ * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, ARG (decay; a
+ * misaligned pointer), HIP.
  */
 int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                    const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
@@ -85,7 +88,8 @@ int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* pl
 /*
  * Attention of a pure-decode batch (every c_i <= 1) that also gives its weights:
  * out as ssa_mixed_attention, scores_out as ssa_key_scores, with keys and values
- * read once.  The new tokens' keys and values must be in the cache.
+ * read once.  The new tokens' keys and values must be in the cache.  (An infinite
+ * value of a key that is seen makes its dim of the output NaN, whatever its weight.)
  * Errors: those of ssa_key_scores; ARG also where the plan has a c_i > 1.
  */
 int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
@@ -116,7 +120,8 @@ int ssa_evict_plan(const ssa_shape* shape, const int32_t* kv_len_host, const int
  * lists start at Hkv * (n_0 + ... + n_{i-1})).  Of equal scores the lowest index
  * stays first; a NaN counts as -infinity; -0 equals +0.  A request that keeps all
  * its keys lists 0 .. n_i - 1.
- * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, HIP.
+ * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, ARG (a misaligned
+ * pointer), HIP.
  */
 int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                      const float* scores, const int32_t* block_table, int32_t* keep,
@@ -133,7 +138,7 @@ int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* 
  * (ssa_check_evict_tables).  An index of keep outside [0, kv_len[i]) is not
  * followed: its slot is left as it is.
  *   scores may be NULL (none are kept).
- * Errors: NULL, the shape errors, PLAN_MISMATCH, HIP.
+ * Errors: NULL, the shape errors, PLAN_MISMATCH, ARG (a misaligned pool), HIP.
  */
 int ssa_evict_compact(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                       const int32_t* keep, const int32_t* block_table, const int32_t* new_table,

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "../../include/ssa_evict.h"
 #include "ssa_device.h"
@@ -563,6 +564,13 @@ int launch(K kernel, const EvictArgs& a, int threads, hipStream_t stream) {
   return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
 }
 
+// Pages are read and written 16 bytes at a time.
+bool misaligned(std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return true;
+  return false;
+}
+
 EvictArgs evict_args(const EvictHeader* h, const void* plan_dev, const int32_t* block_table) {
   EvictArgs a{};
   a.plan = static_cast<const uint8_t*>(plan_dev);
@@ -589,6 +597,7 @@ int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* 
   if (!plan_dev) return SSA_ERR_NULL;
   if (h->num_keep > 0 && (!scores || !block_table || !keep)) return SSA_ERR_NULL;
   if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
+  if (misaligned({scores, workspace})) return SSA_ERR_ARG;
   if (h->num_keep == 0) return SSA_OK;
   EvictArgs a = evict_args(h, plan_dev, block_table);
   a.scores = scores;
@@ -621,6 +630,7 @@ int ssa_evict_compact(const ssa_shape* shape, const void* plan_host, const void*
   if (!plan_dev) return SSA_ERR_NULL;
   if (h->num_items == 0) return SSA_OK;
   if (!keep || !block_table || !new_table || !k_cache || !v_cache) return SSA_ERR_NULL;
+  if (misaligned({k_cache, v_cache})) return SSA_ERR_ARG;
   EvictArgs a = evict_args(h, plan_dev, block_table);
   a.workgroups = h->num_items * h->hkv;
   a.keep_in = keep;

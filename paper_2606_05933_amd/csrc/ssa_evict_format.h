@@ -1,8 +1,9 @@
 // Plan blobs of include/ssa_evict.h: written by the host planner
 // (ssa_evict_plan.cpp), read unchanged by the kernels.
 //
-//   score plan  [ScoreHeader][ScoreReq x num_reqs][ScoreItem x (the five lists)]
-//   evict plan  [EvictHeader][EvictReq x num_reqs][EvictItem x num_items]
+//   score plan  [ScoreHeader][ScoreItem x (the five lists)]
+//   evict plan  [EvictHeader][EvictReq x num_reqs][EvictShort x num_short]
+//               [EvictSeg x num_segs][EvictItem x num_items]
 //
 // A workgroup runs one item for one kv head; a request's fields are copied into
 // its items, so that a workgroup reads one record before it starts.
@@ -16,7 +17,6 @@ constexpr uint32_t kEvictMagic = 0x31565353u;  // "SSV1"
 constexpr int kScoreThreads = 256;             // four waves
 constexpr int kScoreWaveCols = 64;             // stationary vectors of a wave (chunk kernels)
 constexpr int kSumKeys = 4 * kScoreWaveCols;   // keys of a tile of the second chunk pass
-constexpr int kLseMaxKeys = 32768;             // keys of one item of the first chunk pass
 constexpr int kJoinKeys = 1024;                // keys of one item of the decode join
 constexpr int kWholeLogits = 8192;             // logits of a decode row that one workgroup holds
 constexpr int kColsPad = 256;                  // a chunk request's columns are padded to this
@@ -53,10 +53,6 @@ struct ScoreHeader {
   int64_t plan_bytes, ws_bytes;
 };
 static_assert(sizeof(ScoreHeader) == 128, "score header size");
-
-struct ScoreReq {
-  int32_t q_len, ctx_len;
-};
 
 struct ScoreItem {
   int32_t req;

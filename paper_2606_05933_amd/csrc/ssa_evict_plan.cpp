@@ -16,9 +16,13 @@ int validate_shape(const ssa_shape* s);
 namespace {
 
 constexpr int64_t kMaxLen = 1 << 30;
-// Workgroups a launch should have at least: two of four waves run on each of 256
-// compute units, and twice that evens out ranges of different cost.
+// Workgroups that the decode rows are cut into, at least: four on each of 256 compute
+// units.
 constexpr int64_t kFillGroups = 1024;
+// Records of all lists: the blob's size stays within its 32-bit offsets.
+constexpr int64_t kMaxScoreItems = (INT32_MAX - 4096) / (int64_t)sizeof(ScoreItem);
+// A token's queries: 32-bit byte offsets within a few rows of them.
+constexpr int64_t kMaxQueryRow = 1 << 24;
 // A decode row's key range is cut into pieces of a multiple of 128 keys (one
 // 32-key block for each of four waves), at most kDecodeMaxKeys: a piece costs a
 // record of G (D + 3) floats, and long ones leave compute units idle at the end (32
@@ -57,7 +61,6 @@ uint64_t hash_shape(const ssa_shape* s, const int32_t* more, int n_more) {
 
 struct ScorePlan {
   ScoreHeader hdr;
-  std::vector<ScoreReq> reqs;
   std::vector<ScoreItem> list[kNumScoreLists];
 };
 
@@ -69,6 +72,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   if (n > 0 && (!q_len || !ctx_len)) return SSA_ERR_NULL;
   if (last_rows < 0) return SSA_ERR_ARG;
   const int hkv = s->num_kv_heads, g = s->num_q_heads / hkv, d = s->head_dim;
+  if ((int64_t)s->num_q_heads * d > kMaxQueryRow) return SSA_ERR_SHAPE;
   int64_t tokens = 0, keys = 0, decode_keys = 0, decode_rows = 0, max_q = 0;
   struct Chunk {
     int64_t cols, span;
@@ -115,11 +119,10 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     const int64_t per_cu = std::max<int64_t>(1, ceil_div(wgs, kCus));
     return (double)per_cu * (tiles + kItemTiles) * (per_cu == 1 ? kAlone : 1.0);
   };
-  int64_t piece = kLseMaxKeys;
+  int64_t piece = 0;
   double best = 0;
   for (int64_t n = 1; n <= kMaxPieces && !chunks.empty(); ++n) {
     const int64_t p = std::max(kLseMinKeys, round_up(ceil_div(longest, n), 128));
-    if (p > kLseMaxKeys) continue;
     int64_t wgs = 0;
     double tiles = 0;
     for (const Chunk& c : chunks) {
@@ -155,9 +158,18 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   }
   h.lse_groups = 1 << lse_k;
   h.sum_cols = (int32_t)sum_cols;
+  // nothing is built that would not fit
+  int64_t records = ceil_div(decode_keys, kDecodeStepKeys) * 2 + 2 * decode_rows;
+  for (const Chunk& c : chunks) {
+    const int64_t pieces = ceil_div(c.span, piece), tiles = ceil_div(c.span, kSumKeys);
+    records += ceil_div(c.cols, lse_cols) * pieces + ceil_div(c.cols, kScoreThreads) + 1 +
+               tiles * ceil_div(c.cols, sum_cols);
+    if (records > kMaxScoreItems) return SSA_ERR_LENGTH;
+  }
   const int64_t decode_piece =
-      std::min(std::min(kDecodeMaxKeys, kWholeLogits / g / kDecodeStepKeys * kDecodeStepKeys), std::max(kDecodeStepKeys, round_up(ceil_div(decode_keys * hkv, kFillGroups),
-                                                                  kDecodeStepKeys)));
+      std::min(std::min(kDecodeMaxKeys, kWholeLogits / g / kDecodeStepKeys * kDecodeStepKeys),
+               std::max(kDecodeStepKeys,
+                        round_up(ceil_div(decode_keys * hkv, kFillGroups), kDecodeStepKeys)));
 
   // Rows that one workgroup does, at once and without a second launch: as long as its
   // LDS holds the logits where there are enough rows for every compute unit, shorter
@@ -183,7 +195,6 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   };
   for (int32_t i = 0; i < n; ++i) {
     const int64_t c = q_len[i], u = ctx_len[i], len = c + u;
-    p->reqs.push_back({q_len[i], ctx_len[i]});
     if (c == 0) continue;
     const int64_t r = last_rows ? std::min<int64_t>(c, last_rows) : c;
     ScoreItem it{};
@@ -289,9 +300,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   h.num_pages = s->num_pages;
   h.softmax_scale = s->softmax_scale;
   h.max_q_len = (int32_t)max_q;
-  int64_t off = sizeof(ScoreHeader) + (int64_t)sizeof(ScoreReq) * n;
-  off = round_up(off, 64);
-  h.off_items = (int32_t)std::min<int64_t>(off, INT32_MAX);
+  h.off_items = sizeof(ScoreHeader);
   int64_t items = 0;
   for (int l = 0; l < kNumScoreLists; ++l) {
     const int64_t count = (int64_t)p->list[l].size();
@@ -300,7 +309,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     h.count[l] = (int32_t)count;
     items += count;
   }
-  h.plan_bytes = off + items * (int64_t)sizeof(ScoreItem);
+  h.plan_bytes = h.off_items + items * (int64_t)sizeof(ScoreItem);
   if (h.plan_bytes > INT32_MAX) return SSA_ERR_LENGTH;
   h.ws_bytes = std::max<int64_t>(256, ws * 4);
   uint64_t hv = hash_shape(s, &last_rows, 1);
@@ -451,8 +460,6 @@ int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int3
     if (plan_bytes < (size_t)p.hdr.plan_bytes) return SSA_ERR_PLAN_SIZE;
     char* b = static_cast<char*>(plan_host);
     std::memcpy(b, &p.hdr, sizeof p.hdr);
-    if (!p.reqs.empty())
-      std::memcpy(b + sizeof p.hdr, p.reqs.data(), sizeof(ssa::ScoreReq) * p.reqs.size());
     char* at = b + p.hdr.off_items;
     for (const auto& l : p.list) {
       if (!l.empty()) std::memcpy(at, l.data(), sizeof(ssa::ScoreItem) * l.size());

@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "../../include/ssa_evict.h"
@@ -937,6 +938,13 @@ int launch_scores(const ScoreArgs& a, const ScoreHeader* h, hipStream_t s) {
   return launch(score_second_kernel<D>, a, h, kListSum, kListDecodeJoin, s);
 }
 
+// Rows, pages and records are read and written 16 bytes at a time.
+bool misaligned(std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return true;
+  return false;
+}
+
 int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_dev,
                const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
                const float* scores_in, float decay, float* scores_out, void* workspace,
@@ -945,6 +953,7 @@ int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_de
   if (!plan_dev) return SSA_ERR_NULL;
   if (h->max_q_len > 0 && (!q || !k_cache || !block_table || !scores_out)) return SSA_ERR_NULL;
   if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
+  if (misaligned({q, k_cache, scores_in, scores_out, workspace})) return SSA_ERR_ARG;
   *a = ScoreArgs{};
   a->plan = static_cast<const uint8_t*>(plan_dev);
   a->hash = h->hash;
@@ -1001,6 +1010,7 @@ int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void*
                        workspace, ws_bytes, &a)))
     return rc;
   if (h->max_q_len > 0 && (!v_cache || !out)) return SSA_ERR_NULL;
+  if (misaligned({v_cache, out})) return SSA_ERR_ARG;
   a.vc = v_cache;
   a.out = out;
   (void)hipGetLastError();

@@ -95,7 +95,6 @@ def test_score_plans_cover_the_batch_once_and_stay_in_the_workspace(seed):
             x = lse[lse["col0"] == col]
             partition(x)
             assert len(x) == ns and (x["key0"] % 128 == 0).all()
-            assert (x["key1"] - x["key0"] <= 32768).all()
         sums, per = mine["sum"], int(h["sum_cols"])
         assert per % 32 == 0 and (sums["key0"] % 256 == 0).all()
         partition(sums[sums["col0"] == sums["col0"].max()])  # the last rows see every key
@@ -154,6 +153,7 @@ def test_score_plan_refusals():
     big = ssa.make_shape(16, 1, 64, 1 << 27, 1 << 26, 0.1)
     assert raw_score_plan(big, [1 << 29, 1 << 29, 1], [0, 0, 0], 1) == -5
     assert raw_score_plan(big, [(1 << 24) + 1], [0], 0) == -5  # more than 2^28 columns
+    assert raw_score_plan(ssa.make_shape(1 << 18, 1 << 18, 128, 9, 9, 0.1), [1], [1], 0) == -2
     pb = ctypes.c_size_t()
     assert LIB.ssa_score_plan_size(ctypes.byref(shape), None, None, 1, 0, ctypes.byref(pb),
                                    ctypes.byref(pb)) == ssa.SSA_ERR_NULL
@@ -161,7 +161,7 @@ def test_score_plan_refusals():
                                    None) == ssa.SSA_ERR_NULL
 
 
-def call_scores(shape, plan, decay=1.0, ws=1 << 30, fill=1, dev=1, fn="ssa_key_scores", n_ptr=0):
+def call_scores(shape, plan, decay=1.0, ws=1 << 30, fill=16, dev=1, fn="ssa_key_scores", n_ptr=0):
     """Raw call with made-up pointers: it has to be refused before they are used."""
     vp = ctypes.c_void_p
     ptr = plan.ctypes.data if plan is not None else None
@@ -186,6 +186,7 @@ def test_scored_calls_refuse_before_they_launch():
         assert call_scores(shape, plan, decay) == ssa.SSA_ERR_ARG
     assert call_scores(shape, plan, ws=ws - 1) == ssa.SSA_ERR_WORKSPACE
     assert call_scores(shape, plan, fill=0) == ssa.SSA_ERR_NULL
+    assert call_scores(shape, plan, fill=24) == ssa.SSA_ERR_ARG  # 8-byte aligned
     assert call_scores(shape, plan, dev=0) == ssa.SSA_ERR_NULL
     # a chunk has no place in the decode call
     assert call_scores(shape, plan, fn="ssa_decode_scored", n_ptr=1) == ssa.SSA_ERR_ARG
@@ -264,6 +265,7 @@ def test_evict_calls_refuse_before_they_launch():
     for name in ("scores", "table", "keep"):
         assert select(**{name: 0}) == ssa.SSA_ERR_NULL
     assert select(w=0) == select(n=ws - 1) == ssa.SSA_ERR_WORKSPACE
+    assert select(scores=24, w=16) == select(scores=16, w=8) == ssa.SSA_ERR_ARG
 
     def compact(p=ptr, dev=1, keep=1, table=1, new=1, k=1, v=1):
         return LIB.ssa_evict_compact(s, p, vp(dev), vp(keep), vp(table), vp(new), vp(k), vp(v),
@@ -272,6 +274,7 @@ def test_evict_calls_refuse_before_they_launch():
     assert compact(p=score.ctypes.data) == ssa.SSA_ERR_PLAN_MISMATCH
     for name in ("p", "dev", "keep", "table", "new", "k", "v"):
         assert compact(**{name: None if name == "p" else 0}) == ssa.SSA_ERR_NULL
+    assert compact(k=8, v=16) == compact(k=16, v=8) == ssa.SSA_ERR_ARG
     whole, _ = ssa.evict_plan(shape, [100], [100], 0, 0)
     assert LIB.ssa_evict_compact(s, whole.ctypes.data, vp(1), None, None, None, None, None, None,
                                  None) == ssa.SSA_OK  # nothing moves

@@ -289,6 +289,35 @@ def test_scored_calls_are_deterministic_on_a_side_stream_and_in_a_graph(torch_de
         assert same()
 
 
+def test_buffers_that_do_not_fit_are_refused(torch_dev):
+    torch = torch_dev
+    from paper_2606_05933_amd import ssa
+    x = Scored(torch, batch(8, 2, 64, [1, 1], [100, 60], seed=13))
+    good = dict(q=x.q, k=x.k, table=x.table, old_dev=x.old_dev, ws=x.ws)
+
+    def refused(error, **change):
+        for n, t in {**good, **change}.items():
+            setattr(x, n, t)
+        with pytest.raises(error):
+            x.decode()
+        with pytest.raises(error):
+            x.scores()
+
+    refused(ValueError, q=x.q.cpu())
+    refused(ValueError, q=x.q[:1])
+    refused(ValueError, k=x.k[:-1])
+    refused(ValueError, k=x.k.transpose(2, 3))
+    refused(ValueError, old_dev=x.old_dev.double())
+    refused(ValueError, table=x.table[:1])
+    refused(ssa.SsaError, ws=x.ws[:-1])
+    refused(ssa.SsaError, ws=torch.empty(x.ws.numel() + 8, dtype=torch.uint8, device="cuda")[8:])
+    refused(ssa.SsaError, q=torch.empty(x.q.numel() + 4, dtype=torch.bfloat16, device="cuda")[4:])
+    refused(ssa.SsaError, ws=None)
+    x.plan_dev = x.plan_dev[:-1]
+    refused(ValueError)
+    assert bool((x.out_scores == -7.0).all())
+
+
 def test_a_stale_device_plan_writes_nothing(torch_dev):
     torch = torch_dev
     x = Scored(torch, batch(8, 2, 64, [1, 30], [100, 60], seed=13))
@@ -389,7 +418,8 @@ def test_select_and_compact(torch_dev, budget, sink, recent):
 
 
 @pytest.mark.parametrize("lens,budget", [([4097, 5], 4096), ([33000, 20000], 1000), ([70001], 69999),
-                                         ([40000], 17), ([131072, 9000, 1], 8192)])
+                                         ([40000], 17), ([131072, 9000, 1], 8192),
+                                         ([20000, 100, 9000], 30000), ([8192, 8193, 16384, 16385], 8000)])
 def test_long_lists(torch_dev, lens, budget):
     x = Evicted(torch_dev, lens, budget, 4, 5, hkv=2, d=128, seed=2)
     x.select()
