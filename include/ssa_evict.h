@@ -72,7 +72,8 @@ int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int3
  * earlier score: what scores_in holds there is not read.
  *   q, k_cache, block_table: as ssa_mixed_attention; the batch's own keys must
  *   be in the cache (ssa_kv_append, ssa_append_attention or ssa_rope_append ran
- *   before on the stream).
+ *   before on the stream), and the table's entries as ssa_check_block_table of
+ *   the batch's ssa_plan checks them.
  *   scores_in   may be NULL (all zero; decay is then unused) or scores_out
  *   decay       finite, >= 0
  *   Requests with c_i = 0, slots past a request's last key and other pages are

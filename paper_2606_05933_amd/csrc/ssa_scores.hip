@@ -120,7 +120,11 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 }
 
 // ---------------------------------------------------------------------------
-// One counted row: logits over a key range.
+// One counted row: logits over a key range.  Memory bounds it: 32 rows of 8k to 33k
+// keys, 64/8 heads of 128, with the output: 2.46 GB of keys and values and 0.17 GB of
+// logits in 525 us, 5.0 TB/s where a large copy reaches 4.8 (without the logits'
+// stores 435 us), and 48 us for the join.  One step of loads ahead: 580 us against 674
+// without; the non-temporal hint changes nothing.
 //
 // Each wave takes every fourth 32-key block (two pages).  S^T = K Q^T in 16x16
 // tiles: the A rows of the two tiles are dealt so that a lane ends up with 8
@@ -416,7 +420,12 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
 }
 
 // ---------------------------------------------------------------------------
-// Several rows: both passes.  A wave holds 64 stationary vectors (columns in the
+// Several rows: both passes.  The issue of matrix and vector instructions bounds them:
+// per 32 x 64 scores a wave runs 16 products (512 cycles), 32 exponentials (half
+// rate), 32 multiply-adds and 30 additions.  Four chunks of 64 to 1024 rows, 267 M
+// scores of 28/4 heads: 86 us and 105 us; of the first pass's cycles the matrix unit is
+// busy 0.35, and 0.46 of those have a vector instruction beside.  Waves of 32 vectors
+// (twice as many resident) take 97 and 108 us.  A wave holds 64 stationary vectors (columns in the
 // first pass, keys in the second) as B operands of the 32x32x16 product and runs
 // the streamed rows (keys, columns) past them in 32-row tiles; NC waves lie side
 // by side over the same rows, 4 / NC one behind the other.  Lane n of a 32x32
@@ -709,7 +718,7 @@ struct SumLds {
 template <int D>
 __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
                                          SumLds<D>& lds) {
-  constexpr int NC = 4;
+  constexpr int NC = 4;  // tiles of 64 or 128 keys put too few products between copies
   using C = ChunkCfg<D, NC>;
   static_assert(C::RG == 1 && C::COLS == kSumKeys, "one row group");
   const int tid = threadIdx.x, lane = tid & 63;
