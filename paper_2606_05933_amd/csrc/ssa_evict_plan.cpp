@@ -35,7 +35,8 @@ constexpr int64_t kLseMinKeys = 256;
 constexpr int64_t kMaxPieces = 64;
 // The chunk passes' estimate.
 constexpr int64_t kCus = 256;
-constexpr double kItemTiles = 3;
+constexpr double kItemTiles = 3;     // of 2, 3, 5 and 8 for the second pass, 5 chose best:
+constexpr double kSumItemTiles = 5;  // (31, 28, 27, 28) us of a mixed batch, (105, 106, 104, 116) of four chunks
 constexpr double kAlone = 1.2;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -149,8 +150,8 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
       wgs += k * ceil_div(c.cols, p);
       tiles += k * c.cols / 32;
     }
-    const double cost = std::max(1.0, std::ceil(wgs / kCus) * kCus / wgs) * (tiles + wgs * kItemTiles) / kCus +
-                        p / 32 + kItemTiles;
+    const double cost = std::max(1.0, std::ceil(wgs / kCus) * kCus / wgs) * (tiles + wgs * kSumItemTiles) / kCus +
+                        p / 32 + kSumItemTiles;
     if (best == 0 || cost < best) {
       best = cost;
       sum_cols = p;

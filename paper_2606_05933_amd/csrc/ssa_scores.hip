@@ -437,10 +437,11 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
 
 constexpr int kTiles = kScoreWaveCols / 32;
 
-template <int D, int NC>
+template <int D, int NC, int TILES = 1>
 struct ChunkCfg {
   static constexpr int RG = 4 / NC;             // row groups
-  static constexpr int ROWS = 32 * RG;          // streamed rows of a stage
+  static constexpr int TPS = TILES;             // 32-row tiles of a wave in a stage
+  static constexpr int ROWS = 32 * RG * TPS;    // streamed rows of a stage
   static constexpr int ROWB = D * 2;
   static constexpr int CPR = D / 8;             // 16-byte pieces of a row
   static constexpr int RPD = 64 / CPR;          // rows of one copy instruction
@@ -467,13 +468,12 @@ __device__ __forceinline__ uint32_t copy_offset(int lane, int row0) {
 }
 
 // Where a lane reads the fragments of its row of the first stage.
-template <int D, int NC>
+template <class C, int D>
 __device__ __forceinline__ void fragment_addresses(const char* buf, int rg, int lane,
                                                    const char* (&at)[D / 16]) {
-  using C = ChunkCfg<D, NC>;
 #pragma unroll
   for (int s = 0; s < C::KS; ++s)
-    at[s] = buf + (rg * 32 + (lane & 31)) * C::ROWB +
+    at[s] = buf + (rg * 32 * C::TPS + (lane & 31)) * C::ROWB +
             ((2 * s + (lane >> 5)) ^ (lane & (C::CPR - 1))) * 16;
 }
 
@@ -494,10 +494,9 @@ __device__ __forceinline__ void for_stages(int stages, F stage) {
 
 // One 32-row tile's products with the wave's 64 vectors.  All of the tile's
 // fragments are on their way before the first product.
-template <int D, int NC>
+template <class C, int D>
 __device__ __forceinline__ void tile_products(const char* const (&at)[D / 16], int offset,
                                               const bf16x8 (*st)[D / 16], f32x16* acc) {
-  using C = ChunkCfg<D, NC>;
   bf16x8 x[C::KS];
 #pragma unroll
   for (int s = 0; s < C::KS; ++s) x[s] = as_bf16x8(ld16(at[s] + offset));
@@ -570,16 +569,20 @@ __device__ __forceinline__ void lse_update(const f32x16& x, float c, int limit, 
   *m = mn;
 }
 
+// Two tiles a stage where four waves share them (half the barriers; 85.7 us of the
+// chunks above, 82.5 with).  The second pass is slower with two (105 us, 111 with).
+template <int D, int NC>
+using LseCfg = ChunkCfg<D, NC, NC == 4 ? 2 : 1>;
 template <int D, int NC>
 struct LseLds {
-  using C = ChunkCfg<D, NC>;
+  using C = LseCfg<D, NC>;
   __attribute__((aligned(16))) char buf[C::NB * C::STAGE];
   float m[C::RG][C::COLS], l[C::RG][C::COLS];
 };
 template <int D, int NC>
 __device__ __forceinline__ void lse_item(const ScoreArgs& a, const ScoreItem& it, int kvh,
                                          LseLds<D, NC>& lds) {
-  using C = ChunkCfg<D, NC>;
+  using C = LseCfg<D, NC>;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cg = wave % NC, rg = wave / NC, half = lane >> 5;
@@ -635,7 +638,7 @@ __device__ __forceinline__ void lse_item(const ScoreArgs& a, const ScoreItem& it
   for (int k = 0; k < C::NB - 1; ++k)
     if (k < stages) issue(k);
   const char* at[C::KS];
-  fragment_addresses<D, NC>(lds.buf, rg, lane, at);
+  fragment_addresses<C, D>(lds.buf, rg, lane, at);
   for_stages<C::NB>(stages, [&](int k, auto buffer) {
     if (C::NB == 3 && k + 1 < stages)
       vm_wait<C::LOADS>();
@@ -643,15 +646,19 @@ __device__ __forceinline__ void lse_item(const ScoreArgs& a, const ScoreItem& it
       vm_wait<0>();
     __syncthreads();
     if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
-    f32x16 acc[kTiles];
-    tile_products<D, NC>(at, buffer() * C::STAGE, st, acc);
-    const int kb = it.key0 + k * C::ROWS + rg * 32;
-    if (k > 0 && kb + 31 <= first_limit && kb + 32 <= kend) {
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) lse_add(acc[t], a.c, &m[t], &l[t]);
-    } else {
+    for (int tile = 0; tile < C::TPS; ++tile) {
+      const int kb = it.key0 + k * C::ROWS + (rg * C::TPS + tile) * 32;
+      if (tile > 0 && kb >= kend) break;
+      f32x16 acc[kTiles];
+      tile_products<C, D>(at, buffer() * C::STAGE + tile * 32 * C::ROWB, st, acc);
+      if (k > 0 && kb + 31 <= first_limit && kb + 32 <= kend) {
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) lse_update(acc[t], a.c, limit[t] - kb, &m[t], &l[t]);
+        for (int t = 0; t < kTiles; ++t) lse_add(acc[t], a.c, &m[t], &l[t]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) lse_update(acc[t], a.c, limit[t] - kb, &m[t], &l[t]);
+      }
     }
   });
 #pragma unroll
@@ -711,7 +718,7 @@ template <int D>
 struct SumLds {
   using C = ChunkCfg<D, 4>;
   __attribute__((aligned(16))) char buf[C::NB * C::STAGE];
-  __attribute__((aligned(16))) float lse[C::NB][4][32];  // one copy a wave
+  __attribute__((aligned(16))) float lse[C::NB][4][C::ROWS];  // one copy a wave
   __attribute__((aligned(16))) float sum[C::COLS];
   int last;
 };
@@ -729,27 +736,48 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
   const int n0 = max(it.col0, max(0, it.key0 - limit0) * a.g / C::ROWS * C::ROWS);
   const int stages = (ncols - n0 + C::ROWS - 1) / C::ROWS;
 
+  // columns from here on see the whole tile
+  const int64_t n_whole = (int64_t)(it.key0 + C::COLS - 1 - limit0) * a.g;
   // sums of 16 tiles, then the sums of those: few terms that differ much in size
   float sum[kTiles] = {}, total[kTiles] = {};
   const float* lse = a.ws + it.off0 + (int64_t)kvh * it.cols_pad;
+  // Copy i of a stage starts at column n[i], head at[i] of its group, row from[i]:
+  // stepped from stage to stage, since dividing by G for each would cost a wave more
+  // scalar instructions than its products.
+  const uint16_t* from[C::LOADS];
+  int head[C::LOADS];
+#pragma unroll
+  for (int i = 0; i < C::LOADS; ++i) {
+    const int n = min(n0 + copy_row<C>(wave, i), ncols - 1), j = div_g(a, n);
+    head[i] = n - j * a.g;
+    from[i] = a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + head[i]) * D;
+  }
+  const int step_rows = div_g(a, C::ROWS), step_heads = C::ROWS - step_rows * a.g;
+  const int64_t step = ((int64_t)step_rows * a.hq + step_heads) * D, wrap_step = (int64_t)(a.hq - a.g) * D;
+  const uint16_t* row0 = a.q + ((size_t)it.q_row * a.hq + kvh * a.g) * D;
   auto issue = [&](int k) {
     const int nb = n0 + k * C::ROWS;
     char* buf = lds.buf + (k % C::NB) * C::STAGE;
 #pragma unroll
     for (int i = 0; i < C::LOADS; ++i) {
-      const int row0 = copy_row<C>(wave, i), n = nb + row0, j = div_g(a, n);
-      const uint16_t* p = a.q + ((size_t)(it.q_row + j) * a.hq + kvh * a.g + (n - j * a.g)) * D;
-      // a lane's row is `more` heads on, or in a later token
-      const int more = min(lane / C::CPR, max(0, ncols - 1 - n));
-      const int wrap = ((n - j * a.g + more) * a.g_magic12) >> 12;
-      if (n < ncols)
-        dma16_base(p, copy_offset<C>(lane, row0) + (more - lane / C::CPR + wrap * (a.hq - a.g)) * C::ROWB,
-                   buf + row0 * C::ROWB);
-      else  // past the last column: any row of the request
-        dma16_base(a.q + ((size_t)it.q_row * a.hq + kvh * a.g) * D, copy_offset<C>(lane, row0) % C::ROWB,
-                   buf + row0 * C::ROWB);
+      const int at = copy_row<C>(wave, i), left = ncols - 1 - (nb + at);
+      if (left >= 0) {
+        // a lane's row is `more` heads on, or in a later token
+        const int more = min(lane / C::CPR, left);
+        const int wrap = ((head[i] + more) * a.g_magic12) >> 12;
+        dma16_base(from[i], copy_offset<C>(lane, at) + (more - lane / C::CPR + wrap * (a.hq - a.g)) * C::ROWB,
+                   buf + at * C::ROWB);
+      } else {  // past the last column: any row of the request
+        dma16_base(row0, copy_offset<C>(lane, at) % C::ROWB, buf + at * C::ROWB);
+      }
+      from[i] += step;
+      head[i] += step_heads;
+      if (head[i] >= a.g) {
+        head[i] -= a.g;
+        from[i] += wrap_step;
+      }
     }
-    if (lane < 8)
+    if (lane < C::ROWS / 4)
       dma16(lse + nb + lane * 4,
             reinterpret_cast<const char*>(&lds.lse[k % C::NB][wave][0]));
   };
@@ -769,7 +797,7 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
   }
   vm_wait<0>();  // all of it has landed: the waits below count later copies only
   const char* at[C::KS];
-  fragment_addresses<D, NC>(lds.buf, 0, lane, at);
+  fragment_addresses<C, D>(lds.buf, 0, lane, at);
   const float* lse_at = &lds.lse[0][wave][4 * half];
   for_stages<C::NB>(stages, [&](int k, auto buffer) {
     if (C::NB == 3 && k + 1 < stages)
@@ -778,19 +806,19 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
       vm_wait<0>();
     __syncthreads();
     if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
+    const int nb = n0 + k * C::ROWS;
     f32x16 acc[kTiles];
     f32x4 lv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      lv[i] = *reinterpret_cast<const f32x4*>(lse_at + buffer() * 128 + 8 * i);
-    tile_products<D, NC>(at, buffer() * C::STAGE, st, acc);
-    const int nb = n0 + k * C::ROWS;
+      lv[i] = *reinterpret_cast<const f32x4*>(lse_at + buffer() * 4 * C::ROWS + 8 * i);
+    tile_products<C, D>(at, buffer() * C::STAGE, st, acc);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         acc[t][i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -lv[i >> 2][i & 3]));
-    if (limit0 + div_g(a, nb) < it.key0 + C::COLS - 1) {  // some row does not see some key
+    if (nb < n_whole) {  // some row does not see some key
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int limit = limit0 + div_g(a, nb + tile_row(i) + 4 * half);
