@@ -38,6 +38,7 @@
 #include <stdint.h>
 
 #include "ssa.h"
+#include "ssa_layer.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -170,6 +171,42 @@ int ssa_rope_append_shifted(const ssa_shape* shape, const void* plan_host, const
                             const int32_t* shift_host, const int32_t* shift_dev, uint16_t* q_out,
                             uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
                             void* stream);
+
+/*
+ * What a decoder layer does beside ssa_layer_forward for requests that are evicted
+ * from.  Either part may be left out (NULL).
+ *   score_plan_host, score_plan_dev   ssa_score_plan of the same batch as the layer's
+ *            plan; after RoPE and append, the layer's rows add their weights as
+ *            ssa_key_scores (scores_in, decay, scores_out: as there)
+ *   score_workspace   of the score plan; not the layer's
+ *   shift_host, shift_dev   as ssa_rope_append_shifted
+ */
+typedef struct ssa_layer_eviction {
+  const void* score_plan_host;
+  const void* score_plan_dev;
+  const float* scores_in;
+  float* scores_out;
+  void* score_workspace;
+  size_t score_ws_bytes;
+  const int32_t* shift_host;
+  const int32_t* shift_dev;
+  float decay;
+} ssa_layer_eviction;
+
+/*
+ * ssa_layer_forward with `eviction`'s parts: the same launches with the shifted
+ * positions, and ssa_key_scores of the rotated queries before attention.  Without
+ * shifts, out and the caches are bit for bit those of ssa_layer_forward.
+ * Everything is validated before the first launch.
+ * Errors: those of ssa_layer_forward, ssa_key_scores and ssa_rope_append_shifted;
+ * NULL (eviction); PLAN_MISMATCH also where the two plans differ in requests, tokens
+ * or their longest request's new tokens.
+ */
+int ssa_layer_forward_evicting(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                               const ssa_layer_weights* w, const ssa_layer_eviction* eviction,
+                               const uint16_t* x, uint16_t* out, uint16_t* k_cache,
+                               uint16_t* v_cache, const int32_t* block_table, void* workspace,
+                               size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,9 @@
 #include <algorithm>
 #include <cmath>
 
+#include "../../include/ssa_evict.h"
 #include "../../include/ssa_layer.h"
+#include "ssa_evict_format.h"
 #include "ssa_layer_internal.h"
 #include "ssa_plan_format.h"
 
@@ -73,6 +75,87 @@ int layer_ws(const ssa_shape* shape, const void* plan_host, const ssa_layer_weig
   return SSA_OK;
 }
 
+// e: the parts of ssa_layer_forward_evicting, or null.
+int layer_forward(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                  const ssa_layer_weights* w, const ssa_layer_eviction* e, const uint16_t* x,
+                  uint16_t* out, uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
+                  void* workspace, size_t ws_bytes, void* stream) {
+  const PlanHeader* h = nullptr;
+  LayerWs l;
+  int rc = layer_ws(shape, plan_host, w, &h, &l);
+  if (rc) return rc;
+  if (!plan_dev) return SSA_ERR_NULL;
+  const ReqEntry* reqs =
+      reinterpret_cast<const ReqEntry*>(static_cast<const uint8_t*>(plan_host) + h->off_reqs);
+  const int32_t* shift = e ? e->shift_host : nullptr;
+  const void* const score_plan = e ? e->score_plan_host : nullptr;
+  if (e && (!e->shift_host != !e->shift_dev)) return SSA_ERR_NULL;
+  for (int32_t i = 0; i < h->num_reqs; ++i) {
+    if (reqs[i].q_len <= 0) continue;
+    const int64_t s = shift ? shift[i] : 0;
+    if (s < 0 || s + reqs[i].ctx_len + reqs[i].q_len > w->max_position) return SSA_ERR_ARG;
+  }
+  const int32_t t = h->num_tokens;
+  if (score_plan) {
+    const ScoreHeader* sh = nullptr;
+    if ((rc = check_score_plan(shape, score_plan, &sh))) return rc;
+    int32_t longest = 0;
+    for (int32_t i = 0; i < h->num_reqs; ++i) longest = std::max(longest, reqs[i].q_len);
+    if (sh->num_reqs != h->num_reqs || sh->num_tokens != t || sh->max_q_len != longest)
+      return SSA_ERR_PLAN_MISMATCH;
+  }
+  if (t == 0) return SSA_OK;
+  if (!x || !out || !k_cache || !v_cache || !block_table || !w->attn_norm || !w->w_qkv ||
+      !w->w_o || !w->mlp_norm || !w->w_gate_up || !w->w_down || !w->cos_sin)
+    return SSA_ERR_NULL;
+  if (!workspace || ws_bytes < l.total) return SSA_ERR_WORKSPACE;
+  if (score_plan &&
+      (rc = check_key_scores(shape, score_plan, e->score_plan_dev,
+                             reinterpret_cast<const uint16_t*>(static_cast<char*>(workspace) + l.q),
+                             k_cache, block_table, e->scores_in, e->decay, e->scores_out,
+                             e->score_workspace, e->score_ws_bytes)))
+    return rc;
+  char* ws = static_cast<char*>(workspace);
+  auto at = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
+  uint16_t *xn = at(l.xn), *qkv = at(l.qkv), *q = at(l.q), *a = at(l.a), *hb = at(l.h),
+           *act = at(l.act);
+  void* gws = ws + l.gemm;
+  const int32_t hid = w->hidden, qd = h->hq * h->head_dim;
+  const int32_t nqkv = (h->hq + 2 * h->hkv) * h->head_dim;
+
+  const size_t counters = kLaunchCounters * sizeof(uint32_t);
+  const ClearWords tickets = {
+      {reinterpret_cast<uint32_t*>(ws + l.attn + counters), static_cast<uint32_t*>(gws)},
+      {((int64_t)h->ws_partials_off - (int64_t)counters) / 4,
+       l.gemm_bytes > 0 ? (int64_t)(kLinearTicketBytes / 4) : 0}};
+  if ((rc = rms_norm(t, hid, x, w->attn_norm, w->eps, xn, tickets, stream))) return rc;
+  if ((rc = ssa_linear(t, nqkv, hid, SSA_EPILOGUE_NONE, xn, w->w_qkv, nullptr, qkv, gws,
+                       l.gemm_bytes, stream)))
+    return rc;
+  rc = shift ? ssa_rope_append_shifted(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position,
+                                       shift, e->shift_dev, q, k_cache, v_cache, block_table, stream)
+             : ssa_rope_append(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position, q,
+                               k_cache, v_cache, block_table, stream);
+  if (rc) return rc;
+  if (score_plan &&
+      (rc = ssa_key_scores(shape, score_plan, e->score_plan_dev, q, k_cache, block_table,
+                           e->scores_in, e->decay, e->scores_out, e->score_workspace,
+                           e->score_ws_bytes, stream)))
+    return rc;
+  if ((rc = ssa_mixed_attention(shape, plan_host, plan_dev, q, k_cache, v_cache, block_table, a,
+                                ws + l.attn, l.attn_bytes, stream)))
+    return rc;
+  if ((rc = ssa_linear(t, hid, qd, SSA_EPILOGUE_RESIDUAL, a, w->w_o, x, hb, gws, l.gemm_bytes,
+                       stream)))
+    return rc;
+  if ((rc = ssa_rms_norm(t, hid, hb, w->mlp_norm, w->eps, xn, stream))) return rc;
+  if ((rc = ssa_linear(t, 2 * w->inter, hid, SSA_EPILOGUE_SWIGLU, xn, w->w_gate_up, nullptr, act,
+                       gws, l.gemm_bytes, stream)))
+    return rc;
+  return ssa_linear(t, hid, w->inter, SSA_EPILOGUE_RESIDUAL, act, w->w_down, hb, out, gws,
+                    l.gemm_bytes, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -107,54 +190,18 @@ int ssa_layer_forward(const ssa_shape* shape, const void* plan_host, const void*
                       const ssa_layer_weights* w, const uint16_t* x, uint16_t* out,
                       uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
                       void* workspace, size_t ws_bytes, void* stream) {
-  const PlanHeader* h = nullptr;
-  LayerWs l;
-  int rc = layer_ws(shape, plan_host, w, &h, &l);
-  if (rc) return rc;
-  if (!plan_dev) return SSA_ERR_NULL;
-  const ReqEntry* reqs =
-      reinterpret_cast<const ReqEntry*>(static_cast<const uint8_t*>(plan_host) + h->off_reqs);
-  for (int32_t i = 0; i < h->num_reqs; ++i)
-    if (reqs[i].q_len > 0 && (int64_t)reqs[i].ctx_len + reqs[i].q_len > w->max_position)
-      return SSA_ERR_ARG;
-  const int32_t t = h->num_tokens;
-  if (t == 0) return SSA_OK;
-  if (!x || !out || !k_cache || !v_cache || !block_table || !w->attn_norm || !w->w_qkv ||
-      !w->w_o || !w->mlp_norm || !w->w_gate_up || !w->w_down || !w->cos_sin)
-    return SSA_ERR_NULL;
-  if (!workspace || ws_bytes < l.total) return SSA_ERR_WORKSPACE;
-  char* ws = static_cast<char*>(workspace);
-  auto at = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
-  uint16_t *xn = at(l.xn), *qkv = at(l.qkv), *q = at(l.q), *a = at(l.a), *hb = at(l.h),
-           *act = at(l.act);
-  void* gws = ws + l.gemm;
-  const int32_t hid = w->hidden, qd = h->hq * h->head_dim;
-  const int32_t nqkv = (h->hq + 2 * h->hkv) * h->head_dim;
+  return layer_forward(shape, plan_host, plan_dev, w, nullptr, x, out, k_cache, v_cache,
+                       block_table, workspace, ws_bytes, stream);
+}
 
-  const size_t counters = kLaunchCounters * sizeof(uint32_t);
-  const ClearWords tickets = {
-      {reinterpret_cast<uint32_t*>(ws + l.attn + counters), static_cast<uint32_t*>(gws)},
-      {((int64_t)h->ws_partials_off - (int64_t)counters) / 4,
-       l.gemm_bytes > 0 ? (int64_t)(kLinearTicketBytes / 4) : 0}};
-  if ((rc = rms_norm(t, hid, x, w->attn_norm, w->eps, xn, tickets, stream))) return rc;
-  if ((rc = ssa_linear(t, nqkv, hid, SSA_EPILOGUE_NONE, xn, w->w_qkv, nullptr, qkv, gws,
-                       l.gemm_bytes, stream)))
-    return rc;
-  if ((rc = ssa_rope_append(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position, q,
-                            k_cache, v_cache, block_table, stream)))
-    return rc;
-  if ((rc = ssa_mixed_attention(shape, plan_host, plan_dev, q, k_cache, v_cache, block_table, a,
-                                ws + l.attn, l.attn_bytes, stream)))
-    return rc;
-  if ((rc = ssa_linear(t, hid, qd, SSA_EPILOGUE_RESIDUAL, a, w->w_o, x, hb, gws, l.gemm_bytes,
-                       stream)))
-    return rc;
-  if ((rc = ssa_rms_norm(t, hid, hb, w->mlp_norm, w->eps, xn, stream))) return rc;
-  if ((rc = ssa_linear(t, 2 * w->inter, hid, SSA_EPILOGUE_SWIGLU, xn, w->w_gate_up, nullptr, act,
-                       gws, l.gemm_bytes, stream)))
-    return rc;
-  return ssa_linear(t, hid, w->inter, SSA_EPILOGUE_RESIDUAL, act, w->w_down, hb, out, gws,
-                    l.gemm_bytes, stream);
+int ssa_layer_forward_evicting(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                               const ssa_layer_weights* w, const ssa_layer_eviction* eviction,
+                               const uint16_t* x, uint16_t* out, uint16_t* k_cache,
+                               uint16_t* v_cache, const int32_t* block_table, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  if (!eviction) return SSA_ERR_NULL;
+  return layer_forward(shape, plan_host, plan_dev, w, eviction, x, out, k_cache, v_cache,
+                       block_table, workspace, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -1015,6 +1015,21 @@ int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_de
 
 }  // namespace
 
+namespace ssa {
+
+int check_key_scores(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                     const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
+                     const float* scores_in, float decay, float* scores_out, void* workspace,
+                     size_t ws_bytes) {
+  const ScoreHeader* h = nullptr;
+  const int rc = check_score_plan(shape, plan_host, &h);
+  ScoreArgs a;
+  return rc ? rc : score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay,
+                              scores_out, workspace, ws_bytes, &a);
+}
+
+}  // namespace ssa
+
 extern "C" {
 
 int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* plan_dev,

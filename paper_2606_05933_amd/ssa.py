@@ -87,6 +87,13 @@ class SsaLayerWeights(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
+class SsaLayerEviction(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("score_plan_host", "score_plan_dev", "scores_in",
+                                               "scores_out", "score_workspace")] + [
+        ("score_ws_bytes", ctypes.c_size_t), ("shift_host", ctypes.c_void_p),
+        ("shift_dev", ctypes.c_void_p), ("decay", ctypes.c_float)]
+
+
 class SsaLinearPlanInfo(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_m", "tile_n", "threads", "tiles_m", "tiles_n",
                                               "splits")]
@@ -204,6 +211,8 @@ def _load():
     lib.ssa_evict_select.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ssa_evict_compact.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ssa_check_evict_tables.argtypes = [P(SsaShape), vp, vp, vp]
+    lib.ssa_layer_forward_evicting.argtypes = [P(SsaShape), vp, vp, P(SsaLayerWeights),
+                                               P(SsaLayerEviction), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ssa_rope_append_shifted.argtypes = [P(SsaShape), vp, vp, vp, vp, i32, vp, vp, vp, vp, vp,
                                             vp, vp]
     lib.ssa_priority_sort.argtypes = [P(SsaCandidate), i32, ctypes.c_double, ctypes.c_double,
@@ -233,7 +242,7 @@ EXPORTED = ("ssa_status_string", "ssa_plan_size", "ssa_plan", "ssa_check_block_t
             "ssa_probe_hbm_gather", "ssa_probe_mfma_bf16", "ssa_score_plan_size",
             "ssa_score_plan", "ssa_key_scores", "ssa_decode_scored", "ssa_evict_plan_size",
             "ssa_evict_plan", "ssa_evict_select", "ssa_evict_compact", "ssa_check_evict_tables",
-            "ssa_rope_append_shifted")
+            "ssa_rope_append_shifted", "ssa_layer_forward_evicting")
 
 EPILOGUE_NONE, EPILOGUE_RESIDUAL, EPILOGUE_SWIGLU = 0, 1, 2
 
@@ -1075,3 +1084,41 @@ def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shif
         check("block_table", block_table, n * shape.max_pages_per_req, 4), _stream(stream))
     if rc:
         raise SsaError(rc, "ssa_rope_append_shifted")
+
+
+def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerWeights, x, out,
+                           k_cache, v_cache, block_table, workspace, score_plan_host=None,
+                           score_plan_dev=None, scores_in=None, decay: float = 1.0,
+                           scores_out=None, score_workspace=None, shift_host=None, shift_dev=None,
+                           stream=None):
+    """ssa_layer_forward_evicting: layer_forward whose rows also add their attention
+    weights to the scores (with a score plan) and whose tokens are rotated at shifted
+    positions (with shifts)."""
+    what = "ssa_layer_forward_evicting"
+    at, h = _header(plan_host, _PLAN_MAGIC, what)
+    check = _Buffers()
+    n, tokens = h[4], h[5]
+    slots = shape.num_pages * shape.num_kv_heads * shape.page_size
+    e = SsaLayerEviction(decay=decay)
+    if score_plan_host is not None:
+        e.score_plan_host, _ = _header(score_plan_host, _SCORE_MAGIC, what)
+        e.score_plan_dev = check.plan(score_plan_dev, score_plan_host)
+        e.scores_in = check("scores_in", scores_in, slots, 4)
+        e.scores_out = check("scores_out", scores_out, slots, 4)
+        e.score_workspace, e.score_ws_bytes = check.workspace(score_workspace)
+    if shift_host is not None:
+        shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
+        if shift_host.size != n:
+            raise ValueError(f"{shift_host.size} shifts for {n} requests")
+        e.shift_host = shift_host.ctypes.data
+        e.shift_dev = check("shift_dev", shift_dev, n, 4)
+    ws, ws_bytes = check.workspace(workspace)
+    rc = LIB.ssa_layer_forward_evicting(
+        shape, at, check.plan(plan_dev, plan_host), weights.c, e,
+        check("x", x, tokens * weights.hidden, 2), check("out", out, tokens * weights.hidden, 2),
+        check("k_cache", k_cache, slots * shape.head_dim, 2),
+        check("v_cache", v_cache, slots * shape.head_dim, 2),
+        check("block_table", block_table, n * shape.max_pages_per_req, 4), ws, ws_bytes,
+        _stream(stream))
+    if rc:
+        raise SsaError(rc, what)

@@ -325,6 +325,46 @@ def test_rope_append_shifted_refuses_bad_shifts():
     assert call([0, 0, 0], 1000, dev=0) == ssa.SSA_ERR_NULL
 
 
+def test_an_evicting_layer_refuses_before_it_launches():
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    c, u = [1, 3], [10, 20]
+    plan, _ = ssa.ssa_plan(shape, c, u)
+    vp = ctypes.c_void_p
+    w = ssa.SsaLayerWeights(16, 16, 16, 16, 16, 16, 16, 256, 128, 64, 1e-5)
+
+    def call(e, position=64, ws=1 << 30):
+        w.max_position = position
+        return LIB.ssa_layer_forward_evicting(
+            ctypes.byref(shape), plan.ctypes.data, vp(16), ctypes.byref(w),
+            None if e is None else ctypes.byref(e), vp(16), vp(16), vp(16), vp(16), vp(16), vp(16),
+            ws, None)
+
+    def scored(plan, **more):
+        return ssa.SsaLayerEviction(**{**dict(
+            score_plan_host=plan.ctypes.data, score_plan_dev=16, scores_out=16, score_workspace=16,
+            score_ws_bytes=1 << 20, decay=1.0), **more})
+
+    assert call(None) == ssa.SSA_ERR_NULL
+    good, ws = ssa.score_plan(shape, c, u)
+    for other in ([1, 3, 0], [20, 10, 5]), ([1, 2], [10, 20]), ([2, 2], [10, 20]):
+        bad, _ = ssa.score_plan(shape, *other)
+        assert call(scored(bad)) == ssa.SSA_ERR_PLAN_MISMATCH
+    assert call(scored(plan)) == ssa.SSA_ERR_PLAN_MISMATCH
+    assert call(scored(good, score_ws_bytes=ws - 1)) == ssa.SSA_ERR_WORKSPACE
+    assert call(scored(good, score_plan_dev=None)) == ssa.SSA_ERR_NULL
+    assert call(scored(good, scores_out=None)) == ssa.SSA_ERR_NULL
+    assert call(scored(good, scores_out=8)) == ssa.SSA_ERR_ARG
+    assert call(scored(good, decay=-1.0)) == ssa.SSA_ERR_ARG
+    assert call(scored(good), ws=256) == ssa.SSA_ERR_WORKSPACE
+    shift = np.array([0, 41], np.int32)
+    e = ssa.SsaLayerEviction(shift_host=shift.ctypes.data, shift_dev=16)
+    assert call(e, position=63) == ssa.SSA_ERR_ARG  # position 63
+    assert call(ssa.SsaLayerEviction(shift_host=shift.ctypes.data)) == ssa.SSA_ERR_NULL
+    assert call(ssa.SsaLayerEviction(shift_dev=16)) == ssa.SSA_ERR_NULL
+    shift[0] = -1
+    assert call(e) == ssa.SSA_ERR_ARG
+
+
 def test_oracle_scores_against_one_weight_at_a_time():
     """The oracle's scores of a small batch, weight by weight with Python floats."""
     import math

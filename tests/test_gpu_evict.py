@@ -124,7 +124,7 @@ def batch(hq, hkv, d, c, u, seed=0, scale=None):
     return b
 
 
-HEADS = [(8, 8, 64), (4, 2, 128), (28, 4, 128), (16, 1, 64), (64, 8, 128), (5, 5, 64), (13, 1, 128)]
+HEADS = [(8, 8, 64), (4, 2, 128), (28, 4, 128), (16, 1, 64), (64, 8, 128), (5, 5, 64), (13, 1, 128), (6, 2, 128), (5, 1, 64)]
 EDGES = [0, 1, 14, 15, 16, 30, 31, 32, 33, 126, 127, 128, 129, 255, 256, 500]
 
 
@@ -198,6 +198,103 @@ def test_every_width_and_cut_runs(torch_dev):
             seen |= {("lse", d, int(h[14])), ("cut", d, bool(h[17]))}
     assert seen == {(k, d, n) for d in (64, 128) for k, n in
                     (("lse", 1), ("lse", 2), ("lse", 4), ("cut", False), ("cut", True))}, seen
+
+
+def test_pools_past_32_bit_offsets(torch_dev):
+    """Pages beyond 2^31 elements and 2^32 bytes of the pools: the same bits as in a
+    small pool."""
+    torch = torch_dev
+    base, hkv, d = 140000, 8, 128
+    for c in ([1, 1], [40, 1]):
+        b = batch(16, hkv, d, c, [300, 5000], seed=31)
+        x = Scored(torch, b)
+        x.decode() if max(c) == 1 else x.scores()
+        torch.cuda.synchronize()
+        x.check_scores()
+        n = b.num_pages
+        pool = torch.empty((base + n, hkv, 16, d), dtype=torch.bfloat16, device="cuda")
+        pool[base:] = x.k
+        values = torch.empty((base + n, hkv, d, 16), dtype=torch.bfloat16, device="cuda")
+        values[base:] = x.v
+        assert pool.numel() > 2 ** 31
+        out, scores = x.out.clone(), x.out_scores.clone()
+        big = torch.full((base + n, hkv, 16), -7.0, device="cuda")
+        old = torch.empty_like(big)
+        old[base:] = x.old_dev
+        x.shape = x.ssa.make_shape(16, hkv, d, base + n, b.max_pages_per_req, b.shape.softmax_scale)
+        x.plan, ws = x.ssa.score_plan(x.shape, b.q_len, b.ctx_len)
+        x.plan_dev, x.k, x.v, x.old_dev, x.out_scores = dev(torch, x.plan), pool, values, old, big
+        x.table = (x.table + base).int()
+        x.out.zero_()
+        x.decode() if max(c) == 1 else x.scores()
+        torch.cuda.synchronize()
+        assert torch.equal(big[base:], scores) and bool((big[:base] == -7.0).all())
+        assert torch.equal(x.out.view(torch.int16), out.view(torch.int16))
+    # the last request's keys cut and moved up there
+    lens, kept = [5001], 400
+    plan, ws = x.ssa.evict_plan(x.shape, lens, [kept], 4, 16)
+    free = np.setdiff1d(np.arange(n), b.block_table[1])[:25] + base
+    table, new = b.block_table[1:] + base, np.full_like(b.block_table[1:], -1)
+    new[0, :25] = free
+    x.ssa.check_evict_tables(x.shape, plan, table, new)
+    keep = torch.empty(kept * hkv, dtype=torch.int32, device="cuda")
+    pd, td, nd = dev(torch, plan), dev(torch, table), dev(torch, new)
+    ws = torch.empty(ws, dtype=torch.uint8, device="cuda")
+    x.ssa.evict_select(x.shape, plan, pd, big, td, keep, ws)
+    x.ssa.evict_compact(x.shape, plan, pd, keep, td, nd, pool, values, big)
+    torch.cuda.synchronize()
+    from oracle import evict
+    from paper_2606_05933_amd.device import bits_of
+    t = np.arange(5001)
+    sc = big[base:].cpu().numpy()
+    at = (b.block_table[1, t // 16], t % 16)
+    for h in range(hkv):
+        want = evict.select(sc[at[0], h, at[1]], kept, 4, 16)
+        got = keep[h * kept:(h + 1) * kept].cpu().numpy()
+        assert np.array_equal(got, want)
+        r = np.arange(kept)
+        assert np.array_equal(bits_of(pool[free[r // 16], h, r % 16]), x.kc[at[0][want], h, at[1][want]])
+        assert np.array_equal(bits_of(values[free[r // 16], h, :, r % 16]),
+                              x.vc[at[0][want], h, :, at[1][want]])
+
+
+def test_more_workgroups_than_a_grid_row(torch_dev):
+    """70000 requests in one call: the bits of calls of 20000."""
+    torch = torch_dev
+    from paper_2606_05933_amd import ssa
+    n, d = 70000, 64
+    say(f"[gpu evict grid rows] requests={n}")
+    g = torch.Generator(device="cuda").manual_seed(0)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    q, k, v = normal(n, 1, d), normal(n, 1, 16, d), normal(n, 1, d, 16)
+    u = np.random.default_rng(0).integers(0, 15, n).astype(np.int32)
+
+    def call(at, m):
+        # request i's keys in page i, what stays of them in page m + i
+        shape = ssa.make_shape(1, 1, d, 2 * m, 1, 0.125)
+        table = torch.arange(m, dtype=torch.int32, device="cuda").view(m, 1)
+        kk, vv = torch.cat([k[at:at + m]] * 2), torch.cat([v[at:at + m]] * 2)
+        scores = torch.zeros((2 * m, 1, 16), device="cuda")
+        out = torch.zeros((m, 1, d), dtype=torch.bfloat16, device="cuda")
+        plan, ws = ssa.score_plan(shape, np.ones(m, np.int32), u[at:at + m])
+        ssa.decode_scored(shape, plan, dev(torch, plan), q[at:at + m], kk, vv, table, None, 1.0, scores,
+                          out, torch.empty(ws, dtype=torch.uint8, device="cuda"))
+        lens = u[at:at + m] + 1
+        plan, ws = ssa.evict_plan(shape, lens, np.full(m, 4), 1, 1)
+        keep = torch.empty(int(np.minimum(lens, 4).sum()), dtype=torch.int32, device="cuda")
+        pd = dev(torch, plan)
+        ssa.evict_select(shape, plan, pd, scores, table, keep,
+                         torch.empty(ws, dtype=torch.uint8, device="cuda"))
+        ssa.evict_compact(shape, plan, pd, keep, table, table + m, kk, vv, scores)
+        torch.cuda.synchronize()
+        return out, keep, scores[:m], scores[m:], kk[m:], vv[m:]
+
+    whole = call(0, n)
+    parts = [call(at, min(20000, n - at)) for at in range(0, n, 20000)]
+    for i in range(len(whole)):
+        assert torch.equal(whole[i], torch.cat([p[i] for p in parts]))
+    # every row's weights add up to 1
+    assert torch.allclose(whole[2].sum(dim=2), torch.ones((n, 1), device="cuda"), rtol=1e-5)
 
 
 @pytest.mark.parametrize("chunk", [1, 50])
@@ -559,6 +656,63 @@ def test_rope_append_shifted(torch_dev, heads, cu, shift):
     none = call(ssa.rope_append_shifted, 0 * shift, dev(torch, 0 * shift))
     assert all(np.array_equal(x, y) for x, y in zip(plain, none))
     assert np.array_equal(plain[2], got[2])
+
+
+@pytest.mark.parametrize("c,u,shift", [([5, 1, 40], [20, 300, 0], [0, 0, 0]),
+                                       ([1, 1, 0, 1], [600, 15, 9, 0], [77, 0, 5, 3]),
+                                       ([30, 1], [100, 64], [500, 900])])
+def test_an_evicting_layer_is_its_steps(torch_dev, c, u, shift):
+    """ssa_layer_forward_evicting: out and caches bit for bit those of ssa_layer_forward
+    without shifts; with them, queries, caches and scores those of the separate calls."""
+    torch = torch_dev
+    from paper_2606_05933_amd import ssa, workload
+    hq, hkv, d, hidden, inter = 8, 2, 64, 256, 128
+    b = batch(hq, hkv, d, c, u, seed=30)
+    shape = ssa.make_shape(hq, hkv, d, b.num_pages, b.max_pages_per_req, d ** -0.5)
+    T = b.num_tokens
+    w = ssa.LayerWeights(workload.layer_weights(1, hidden, inter, hq, hkv, d), hq, hkv, d, 2048)
+    x = dev(torch, workload.normal_bf16((T, hidden), 5))
+    plan, _ = ssa.ssa_plan(shape, c, u)
+    sp, sws = ssa.score_plan(shape, c, u)
+    pd, spd, table = dev(torch, plan), dev(torch, sp), dev(torch, b.block_table)
+    old = torch.rand((b.num_pages, hkv, 16), device="cuda")
+    shift = np.asarray(shift, np.int32)
+    ws = torch.zeros(ssa.layer_workspace_size(shape, plan, w), dtype=torch.uint8, device="cuda")
+
+    def pools():
+        return dev(torch, b.k_cache), dev(torch, b.v_cache)
+
+    k, v = pools()
+    out = torch.zeros((T, hidden), dtype=torch.bfloat16, device="cuda")
+    scores = torch.full_like(old, -7.0)
+    score_ws = torch.full((sws,), 0xFF, dtype=torch.uint8, device="cuda")
+    ssa.layer_forward_evicting(shape, plan, pd, w, x, out, k, v, table, ws, sp, spd, old, 0.5, scores,
+                               score_ws, shift, dev(torch, shift))
+    # the steps
+    k2, v2 = pools()
+    xn, qkv = torch.empty_like(x), torch.empty((T, (hq + 2 * hkv) * d), dtype=torch.bfloat16, device="cuda")
+    q = torch.empty((T, hq, d), dtype=torch.bfloat16, device="cuda")
+    ssa.rms_norm(x, w.attn_norm, xn)
+    lw = torch.zeros(ssa.linear_workspace_size(T, qkv.shape[1], hidden) + 256, dtype=torch.uint8,
+                     device="cuda")
+    ssa.linear(xn, w.w_qkv, qkv, workspace=lw)
+    ssa.rope_append_shifted(shape, plan, pd, qkv, w.cos_sin, shift, dev(torch, shift), q, k2, v2, table)
+    scores2 = torch.full_like(old, -7.0)
+    ssa.key_scores(shape, sp, spd, q, k2, table, old, 0.5, scores2, score_ws)
+    torch.cuda.synchronize()
+    bits = lambda t: t.view(torch.int16)  # noqa: E731
+    assert torch.equal(bits(k), bits(k2)) and torch.equal(bits(v), bits(v2))
+    assert torch.equal(scores, scores2) and bool((scores != -7.0).any())
+    # without scores and shifts: the plain layer; shifts of zero as well
+    k3, v3 = pools()
+    plain, same = torch.zeros_like(out), torch.zeros_like(out)
+    ssa.layer_forward(shape, plan, pd, w, x, plain, k3, v3, table, ws)
+    k4, v4 = pools()
+    ssa.layer_forward_evicting(shape, plan, pd, w, x, same, k4, v4, table, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(bits(plain), bits(same)) and torch.equal(bits(k3), bits(k4))
+    assert torch.equal(bits(out), bits(plain)) == bool((shift == 0).all())
+    assert bool(torch.isfinite(out.float()).all())
 
 
 def test_a_request_decodes_over_its_budget_and_goes_on(torch_dev):
