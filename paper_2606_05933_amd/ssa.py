@@ -434,7 +434,7 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -870,6 +870,9 @@ def bind_plan(shape: SsaShape, q_len, ctx_len, tuning, out, info: SsaPlanInfo) -
 # loop makes these calls for every layer: the wrappers do no more per call than check
 # each buffer once.
 
+import torch as _torch  # noqa: E402 (the library above needs it loaded)
+
+
 def _plan_buffer(out, nbytes: int):
     """(buffer, address, bytes) of a plan: `out`, or a new numpy array."""
     if out is None:
@@ -914,12 +917,22 @@ def evict_plan(shape: SsaShape, kv_len, budget, sink: int, recent: int, out=None
 _SCORE_MAGIC, _EVICT_MAGIC, _PLAN_MAGIC = 0x31435353, 0x31565353, 0x31415353
 
 
+_HeaderWords = ctypes.c_int32 * 32
+
+
+def _address(a):
+    """Address of a numpy array (a third of the time of its .ctypes.data) or a tensor."""
+    if isinstance(a, np.ndarray):
+        return a.__array_interface__["data"][0]
+    return None if a is None else a.data_ptr()
+
+
 def _header(plan_host, magic: int, what: str):
     """Address of a plan and its header as int32 words, checked for its kind."""
-    at = _ptr(plan_host)
+    at = _address(plan_host)
     if at is None:
         raise SsaError(SSA_ERR_NULL, what)
-    words = (ctypes.c_int32 * 32).from_address(at)
+    words = _HeaderWords.from_address(at)
     if words[0] != magic:
         raise SsaError(SSA_ERR_PLAN_MISMATCH, what)
     return at, words
@@ -928,23 +941,30 @@ def _header(plan_host, magic: int, what: str):
 class _Buffers:
     """Checks the buffers of one call, which have to be on the current device (the
     call's stream is one of it), and gives their addresses."""
+    __slots__ = ("device",)
 
     def __init__(self):
-        import torch
-        self.device = torch.cuda.current_device()
+        self.device = _torch.cuda.current_device()
 
     def __call__(self, name, t, numel, itemsize):
         if t is None:
             return None
+        if (t.get_device() == self.device and t.is_contiguous() and t.element_size() == itemsize
+                and t.numel() >= numel):
+            return t.data_ptr()
         if t.get_device() != self.device:
             raise ValueError(f"{name} must be a tensor on the current device")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.element_size() != itemsize:
             raise ValueError(f"{name} must have {itemsize}-byte elements")
-        if t.numel() < numel:
-            raise ValueError(f"{name} holds {t.numel()} elements, the layout needs {numel}")
-        return t.data_ptr()
+        raise ValueError(f"{name} holds {t.numel()} elements, the layout needs {numel}")
+
+    def stream(self, stream):
+        """The stream's handle; None: the current one."""
+        if stream is None:
+            return _torch._C._cuda_getCurrentRawStream(self.device)
+        return getattr(stream, "cuda_stream", stream)
 
     def plan(self, plan_dev, plan_host):
         """The plan as the kernels read it: on the device, or the pinned host buffer."""
@@ -984,10 +1004,10 @@ def key_scores(shape: SsaShape, plan_host, plan_dev, q, k_cache, block_table, sc
                decay: float, scores_out, workspace, stream=None):
     """ssa_key_scores: a batch's attention weights, added per cached key and kv head
     (fp32 [num_pages, Hkv, 16]) to decay times scores_in (None: to nothing)."""
-    _, _, at, pd, pq, pk, bt, si, so, ws, n = _scored_args(
+    check, _, at, pd, pq, pk, bt, si, so, ws, n = _scored_args(
         "ssa_key_scores", shape, plan_host, plan_dev, q, k_cache, block_table, scores_in,
         scores_out, workspace)
-    rc = LIB.ssa_key_scores(shape, at, pd, pq, pk, bt, si, decay, so, ws, n, _stream(stream))
+    rc = LIB.ssa_key_scores(shape, at, pd, pq, pk, bt, si, decay, so, ws, n, check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_key_scores")
 
@@ -1001,7 +1021,7 @@ def decode_scored(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, blo
         scores_out, workspace)
     pool = shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim
     rc = LIB.ssa_decode_scored(shape, at, pd, pq, pk, check("v_cache", v_cache, pool, 2), bt, si,
-                               decay, so, check("out", out, rows, 2), ws, n, _stream(stream))
+                               decay, so, check("out", out, rows, 2), ws, n, check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_decode_scored")
 
@@ -1022,7 +1042,7 @@ def evict_select(shape: SsaShape, plan_host, plan_dev, scores, block_table, keep
     rc = LIB.ssa_evict_select(
         shape, at, check.plan(plan_dev, plan_host), check("scores", scores, slots, 4),
         check("block_table", block_table, h[3] * shape.max_pages_per_req, 4),
-        check("keep", keep, _num_keep(h, shape), 4), ws, n, _stream(stream))
+        check("keep", keep, _num_keep(h, shape), 4), ws, n, check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_evict_select")
 
@@ -1040,7 +1060,7 @@ def evict_compact(shape: SsaShape, plan_host, plan_dev, keep, block_table, new_t
         check("block_table", block_table, entries, 4), check("new_table", new_table, entries, 4),
         check("k_cache", k_cache, slots * shape.head_dim, 2),
         check("v_cache", v_cache, slots * shape.head_dim, 2), check("scores", scores, slots, 4),
-        _stream(stream))
+        check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_evict_compact")
 
@@ -1078,10 +1098,10 @@ def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shif
     rc = LIB.ssa_rope_append_shifted(
         shape, at, check.plan(plan_dev, plan_host),
         check("qkv", qkv, tokens * (hq + 2 * hkv) * d, 2), check("cos_sin", cos_sin, d, 4),
-        cos_sin.numel() // d, shift_host.ctypes.data, check("shift_dev", shift_dev, n, 4),
+        cos_sin.numel() // d, _address(shift_host), check("shift_dev", shift_dev, n, 4),
         check("q_out", q_out, tokens * hq * d, 2), check("k_cache", k_cache, pool, 2),
         check("v_cache", v_cache, pool, 2),
-        check("block_table", block_table, n * shape.max_pages_per_req, 4), _stream(stream))
+        check("block_table", block_table, n * shape.max_pages_per_req, 4), check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_rope_append_shifted")
 
@@ -1110,7 +1130,7 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
         shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
         if shift_host.size != n:
             raise ValueError(f"{shift_host.size} shifts for {n} requests")
-        e.shift_host = shift_host.ctypes.data
+        e.shift_host = _address(shift_host)
         e.shift_dev = check("shift_dev", shift_dev, n, 4)
     ws, ws_bytes = check.workspace(workspace)
     rc = LIB.ssa_layer_forward_evicting(
@@ -1119,6 +1139,6 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
         check("k_cache", k_cache, slots * shape.head_dim, 2),
         check("v_cache", v_cache, slots * shape.head_dim, 2),
         check("block_table", block_table, n * shape.max_pages_per_req, 4), ws, ws_bytes,
-        _stream(stream))
+        check.stream(stream))
     if rc:
         raise SsaError(rc, what)
