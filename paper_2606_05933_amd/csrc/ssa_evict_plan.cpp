@@ -25,7 +25,7 @@ constexpr int64_t kMaxScoreItems = (INT32_MAX - 4096) / (int64_t)sizeof(ScoreIte
 constexpr int64_t kMaxQueryRow = 1 << 24;
 // A decode row's key range is cut into pieces of a multiple of 128 keys (one
 // 32-key block for each of four waves), at most kDecodeMaxKeys: a piece costs a
-// record of G (D + 3) floats, and long ones leave compute units idle at the end (32
+// record of G (D + 2) floats, and long ones leave compute units idle at the end (32
 // rows of 8k to 33k keys, 64/8 heads: 596 us in pieces of 2048, 585 of 1024, 592 of
 // 512).
 constexpr int64_t kDecodeStepKeys = 128;
@@ -33,10 +33,13 @@ constexpr int64_t kDecodeMaxKeys = 1024;
 // A piece of a chunk column tile's key range, at least, and pieces of one, at most.
 constexpr int64_t kLseMinKeys = 256;
 constexpr int64_t kMaxPieces = 64;
-// The chunk passes' estimate.
+// The chunk passes' estimate, in 32-row tiles: starting an item of the first and of the
+// second pass, and a compute unit with one workgroup.  (Of 2, 3, 5 and 8 for the second,
+// 5 chose best: 31, 28, 27 and 28 us of a mixed batch, 105, 106, 104 and 116 of four
+// chunks.)
 constexpr int64_t kCus = 256;
-constexpr double kItemTiles = 3;     // of 2, 3, 5 and 8 for the second pass, 5 chose best:
-constexpr double kSumItemTiles = 5;  // (31, 28, 27, 28) us of a mixed batch, (105, 106, 104, 116) of four chunks
+constexpr double kItemTiles = 3;
+constexpr double kSumItemTiles = 5;
 constexpr double kAlone = 1.2;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -52,9 +52,9 @@ struct ScoreArgs {
   int32_t chunk_groups, workgroups;
   int32_t sum_cols, num_tickets;
   int32_t hq, hkv, g, maxp;
-  uint32_t g_magic;    // ceil(2^32 / g)
-  int32_t g_magic12;   // ceil(2^12 / g): exact for x < 32
-  float c;           // softmax scale times log2(e)
+  uint32_t g_magic;   // ceil(2^32 / g)
+  int32_t g_magic12;  // ceil(2^12 / g): exact for x < 32
+  float c;            // softmax scale times log2(e)
   float decay;
   const uint16_t* q;
   const uint16_t* kc;
@@ -123,8 +123,9 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // One counted row: logits over a key range.  Memory bounds it: 32 rows of 8k to 33k
 // keys, 64/8 heads of 128, with the output: 2.46 GB of keys and values and 0.17 GB of
 // logits in 525 us, 5.0 TB/s where a large copy reaches 4.8 (without the logits'
-// stores 435 us), and 48 us for the join.  One step of loads ahead: 580 us against 674
-// without; the non-temporal hint changes nothing.
+// stores 435 us), and 48 us for the join; 622 us together before a block's loads were
+// issued a step ahead and the pieces cut to 1024 keys.  The non-temporal hint changes
+// nothing.
 //
 // Each wave takes every fourth 32-key block (two pages).  S^T = K Q^T in 16x16
 // tiles: the A rows of the two tiles are dealt so that a lane ends up with 8
@@ -423,7 +424,7 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
 // Several rows: both passes.  The issue of matrix and vector instructions bounds them:
 // per 32 x 64 scores a wave runs 16 products (512 cycles), 32 exponentials (half
 // rate), 32 multiply-adds and 30 additions.  Four chunks of 64 to 1024 rows, 267 M
-// scores of 28/4 heads: 86 us and 105 us; of the first pass's cycles the matrix unit is
+// scores of 28/4 heads: 84 us and 101 us; of the first pass's cycles the matrix unit is
 // busy 0.35, and 0.46 of those have a vector instruction beside.  Waves of 32 vectors
 // (twice as many resident) take 97 and 108 us.  A wave holds 64 stationary vectors (columns in the
 // first pass, keys in the second) as B operands of the 32x32x16 product and runs
