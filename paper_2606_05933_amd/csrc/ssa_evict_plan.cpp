@@ -41,6 +41,7 @@ constexpr int64_t kCus = 256;
 constexpr double kItemTiles = 3;
 constexpr double kSumItemTiles = 5;
 constexpr double kAlone = 1.2;
+constexpr double kGroupCost[3] = {1.3, 1.15, 1.0};  // a tile's, in 1, 2 and 4 column groups
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
@@ -102,44 +103,46 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   ScoreHeader& h = p->hdr;
   std::memset(&h, 0, sizeof h);
 
-  // Column groups of the first chunk pass: waves side by side share the keys that
-  // go through LDS, waves one behind the other take different ones.  Four groups
-  // read LDS and cache least; narrow requests fill fewer columns.
-  int64_t waste[3] = {0, 0, 0}, longest = 0, widest = 0;
-  for (const Chunk& c : chunks) {
-    for (int k = 0; k < 3; ++k)
-      waste[k] += round_up(c.cols, (int64_t)kScoreWaveCols << k) * c.span * (12 - k) / 10;
-    longest = std::max(longest, c.span);
-    widest = std::max(widest, c.cols);
-  }
-  int lse_k = 2;
-  for (int k = 1; k >= 0; --k)
-    if (waste[k] < waste[lse_k]) lse_k = k;
-  const int64_t lse_cols = (int64_t)kScoreWaveCols << lse_k;
-  // Its pieces of the key ranges are cut for the shortest estimate: the workgroups of the busiest compute unit times their 32-row
-  // tiles, kItemTiles for starting one, and kAlone more where there are not two to a
-  // unit to fill each other's waits.
+  // The first chunk pass's column groups and pieces of the key ranges.  Waves side by
+  // side (column groups) share the keys that go through LDS, waves one behind the other
+  // take different ones: four groups read LDS and cache least (kGroupCost), fewer fill
+  // narrow requests better and are done sooner where there are few workgroups.  Both
+  // are cut for the shortest estimate: the workgroups of the busiest compute unit times
+  // their 32-row tiles, kItemTiles for starting one, and kAlone more where there are not
+  // two to a unit to fill each other's waits.  (200 rows on 200 to 4000 keys, 8/8 heads of
+  // 64: 18 to 21 us with the groups that pad the fewest columns, 15 to 19 so; 32 rows on
+  // 200 keys, 64/8 of 128: 19 and 15.)
   auto estimate = [&](int64_t wgs, double tiles) {
     const int64_t per_cu = std::max<int64_t>(1, ceil_div(wgs, kCus));
     return (double)per_cu * (tiles + kItemTiles) * (per_cu == 1 ? kAlone : 1.0);
   };
+  int64_t longest = 0, widest = 0;
+  for (const Chunk& c : chunks) {
+    longest = std::max(longest, c.span);
+    widest = std::max(widest, c.cols);
+  }
+  int lse_k = 2;
   int64_t piece = 0;
   double best = 0;
-  for (int64_t n = 1; n <= kMaxPieces && !chunks.empty(); ++n) {
-    const int64_t p = std::max(kLseMinKeys, round_up(ceil_div(longest, n), 128));
-    int64_t wgs = 0;
-    double tiles = 0;
-    for (const Chunk& c : chunks) {
-      const int64_t w = ceil_div(c.cols, lse_cols) * ceil_div(c.span, p) * hkv;
-      wgs += w;
-      tiles += (double)w * std::min(p, c.span) / (32 * (4 >> lse_k));
+  for (int k = 2; k >= 0 && !chunks.empty(); --k)
+    for (int64_t n = 1; n <= kMaxPieces; ++n) {
+      const int64_t p = std::max(kLseMinKeys, round_up(ceil_div(longest, n), 128));
+      int64_t wgs = 0;
+      double tiles = 0;
+      for (const Chunk& c : chunks) {
+        const int64_t w = ceil_div(c.cols, (int64_t)kScoreWaveCols << k) * ceil_div(c.span, p) * hkv;
+        wgs += w;
+        tiles += (double)w * std::min(p, c.span) / (32 * (4 >> k));
+      }
+      const double cost = estimate(wgs, tiles / wgs * kGroupCost[k]);
+      if (best == 0 || cost < best) {
+        best = cost;
+        piece = p;
+        lse_k = k;
+      }
+      if (p == kLseMinKeys) break;
     }
-    const double cost = estimate(wgs, tiles / wgs);
-    if (best == 0 || cost < best) {
-      best = cost;
-      piece = p;
-    }
-  }
+  const int64_t lse_cols = (int64_t)kScoreWaveCols << lse_k;
   // The second pass: 256 keys stay in registers, columns go through LDS.  Its column
   // ranges, by the same estimate over tiles of equal length and one item's time for
   // the end.

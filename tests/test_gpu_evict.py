@@ -188,8 +188,8 @@ def test_every_width_and_cut_runs(torch_dev):
     cut column ranges, D 64 and 128: batches for which the planner chooses each."""
     seen = set()
     for d in (64, 128):
-        for hq, hkv, c, u in ((2, 2, 20, 100), (4, 2, 60, 2000), (8, 8, 100, 4000), (8, 4, 512, 200),
-                              (16, 16, 130, 4500), (7, 1, 700, 300)):
+        for hq, hkv, c, u in ((2, 2, 20, 100), (8, 4, 512, 200), (4, 4, 1117, 2685), (7, 1, 700, 300),
+                              (32, 8, 262, 4744), (32, 16, 900, 2000)):
             x = Scored(torch_dev, batch(hq, hkv, d, [c], [u], seed=7), old=False)
             x.scores()
             torch_dev.cuda.synchronize()
