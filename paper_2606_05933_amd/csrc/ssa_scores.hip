@@ -16,7 +16,9 @@
 //                     running maximum and sum of its two columns.  Second pass:
 //                     64 keys a wave stay in registers, the columns and their L
 //                     stream through LDS, and every lane sums the weights of its
-//                     two keys.  A key belongs to one workgroup: no atomics.
+//                     two keys.  Where there are few keys the columns are cut into
+//                     ranges too, whose sums the last workgroup of a key tile adds
+//                     in their order.
 //
 // Rows stream into LDS with their 16-byte pieces permuted within the row (piece c
 // of row r lies at c ^ r), so that the 32 rows of a fragment read hit all banks.
@@ -539,10 +541,10 @@ __device__ __forceinline__ void lse_add(const f32x16& x, float c, float* m, floa
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
-    const float mn = fmaxf(*m, mx * c);
+    const float mn = fmaxf(*m, mx * c), ms = mn == -kInf ? 0.f : mn;  // -inf: all logits so far
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = exp2_fast(__builtin_fmaf(x[i], c, -mn));
-    *l = *l * exp2_fast(*m - mn) + sum16(v);
+    for (int i = 0; i < 16; ++i) v[i] = exp2_fast(__builtin_fmaf(x[i], c, -ms));
+    *l = *l * exp2_fast(*m - ms) + sum16(v);
     *m = mn;
   } else {
     *l += sum;

@@ -341,6 +341,32 @@ def test_one_key_takes_all_and_extreme_logits(torch_dev):
         assert np.allclose(got.sum(axis=0), 2 * c, rtol=1e-4)
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 64), (28, 4, 128), (2, 2, 128)])
+@pytest.mark.parametrize("far", [1, 40, 700])
+def test_keys_at_minus_infinity_weigh_nothing(torch_dev, heads, far):
+    """The first `far` cached keys have the logit -inf for every row: whole tiles and
+    pieces of them, before the first finite one."""
+    from oracle import evict
+    b = batch(*heads, [1, 2, 70, 300, 1], [800, 5000, 901, 3500, 9000], seed=16)
+    x = Scored(torch_dev, b, old=False)
+    b.q[..., 0] = 0x3F80  # 1
+    finite = x.kc.copy()
+    t = np.arange(far)
+    for i in range(b.num_reqs):
+        x.kc[b.block_table[i, t // 16], :, t % 16, 0] = 0xFF80
+        finite[b.block_table[i, t // 16], :, t % 16, 0] = 0
+    x.q, x.k = dev(torch_dev, b.q), dev(torch_dev, x.kc)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    ref, _ = evict.key_scores(b, x.kc)
+    _, size = evict.key_scores(b, finite)
+    got = x.out_scores.cpu().numpy().astype(np.float64)
+    known = ~np.isnan(ref)
+    assert (ref[known] == 0).sum() >= far * b.num_reqs * heads[1]
+    assert (got[~known] == -7.0).all()
+    assert (np.abs(got - ref) <= x.rel(size) * ref)[known].all(), int(np.isnan(got).sum())
+
+
 def test_scored_calls_are_deterministic_on_a_side_stream_and_in_a_graph(torch_dev):
     torch = torch_dev
     x = Scored(torch, batch(8, 2, 128, [1, 1, 1], [5000, 77, 16], seed=11))
