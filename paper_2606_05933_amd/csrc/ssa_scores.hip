@@ -273,14 +273,20 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     l = l * alpha + sum;
     m = mn;
     if constexpr (OUT) {
-      // A weight enters the matrix product as two bf16 values, the rounded one and
-      // what that misses (16 bits of it together): memory bounds this loop, and one alone
-      // put as much error into the output as its own rounding to bf16.
-      u32x4 hi, lo;
+      // A weight enters the matrix product as three bf16 values, the rounded one and what
+      // that misses twice over: all of its 24 bits.  Memory bounds this loop.  (One
+      // alone put as much error into the output as its own rounding to bf16, two moved
+      // 1 in 500 of the rounded outputs.)
+      u32x4 part[3];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        hi[w] = pack2(p[2 * w], p[2 * w + 1]);
-        lo[w] = pack2(p[2 * w] - bf16_lo(hi[w]), p[2 * w + 1] - bf16_hi(hi[w]));
+        float x0 = p[2 * w], x1 = p[2 * w + 1];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          part[i][w] = pack2(x0, x1);
+          x0 -= bf16_lo(part[i][w]);
+          x1 -= bf16_hi(part[i][w]);
+        }
       }
       if (__any(alpha != 1.f)) {
 #pragma unroll
@@ -298,8 +304,8 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
       }
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
-        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(hi), o[t]);
-        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(lo), o[t]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[i]), o[t]);
       }
       if (more) load_values(p0, p1);
       __builtin_amdgcn_sched_barrier(0);

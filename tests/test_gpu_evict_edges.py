@@ -1,0 +1,88 @@
+"""GPU tests of the eviction calls at the edges of their arithmetic and their masks.
+
+The bar of each test is derived beside it from the roundings of its own inputs
+(half a step: fp32 2^-24, bf16 2^-8 of the value).
+"""
+import numpy as np
+import pytest
+
+from test_gpu_evict import Scored, batch, dev, say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch_dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def bf16(x):
+    """float64 of the bf16 values nearest to x."""
+    from paper_2606_05933_amd import workload
+    x = np.asarray(x, np.float32)
+    return workload.bf16_bits_to_f32(workload.f32_to_bf16_bits(x)).astype(np.float64).reshape(x.shape)
+
+
+def put_keys(b, cache, i, head, at, rows, values=False):
+    """rows [n, D] (bf16 values) into the slots `at` of request i's pages."""
+    from paper_2606_05933_amd import workload
+    at = np.asarray(at)
+    bits = workload.f32_to_bf16_bits(np.asarray(rows, np.float32))
+    if values:
+        cache[b.block_table[i, at // 16], head, :, at % 16] = bits
+    else:
+        cache[b.block_table[i, at // 16], head, at % 16] = bits
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 64), (4, 1, 128)])
+@pytest.mark.parametrize("u", [2, 40, 4500])
+def test_scored_decode_weighs_values_in_full(torch_dev, heads, u):
+    """Two keys of weight 1 hold the first two bf16 parts of a third key's weight p, and
+    that one the value -1: what is left of the output is p's bits past the 16th.
+
+    Logits are single products (exact).  p = 2^(x c) is off by the rounding of c and of
+    x c (2^-24 |x c| ln 2 each, |x c| < 1) and the exponential's (one step, 2^-23): under
+    4 2^-24 p.  Three terms add with at most three roundings of sums under 2, and 1 / l
+    and its product take 2^-23 of a value under 2^-8.  So, mass being sum |w v| l < 3:
+    |err| <= 2^-8 |ref| + (4 + 3 * 2 + 1) 2^-24 mass / l."""
+    from paper_2606_05933_amd import workload
+    hq, hkv, d = heads
+    g = hq // hkv
+    n = 6
+    b = batch(hq, hkv, d, [1] * n, [u] * n, seed=40, scale=0.125)
+    x = Scored(torch_dev, b, old=False)
+    scale = float(np.float32(0.125))
+    rng = np.random.default_rng(41)
+    q = np.zeros((n, hq, d), np.float32)
+    q[:, :, 0] = 1
+    want = np.zeros((n, hq, d))
+    bar = np.zeros_like(want)
+    for i in range(n):
+        for h in range(hkv):
+            keys = np.zeros((u + 1, d))
+            keys[:, 0] = -1e6  # weight 0
+            values = bf16(rng.standard_normal((u + 1, d)))
+            one, two, third = rng.choice(u + 1, 3, replace=False)
+            logit = bf16(-rng.uniform(0.5, 5.0, 100))
+            p = np.exp(scale * logit)
+            hi = bf16(p)
+            mid = bf16(p - hi)
+            best = np.argmax(np.abs(hi + mid - p))  # much to miss
+            p, hi, mid = p[best], hi[best], mid[best]
+            keys[[one, two], 0], keys[third, 0] = 0, logit[best]
+            values[one], values[two], values[third] = hi, mid, -1
+            put_keys(b, x.kc, i, h, np.arange(u + 1), keys)
+            put_keys(b, x.vc, i, h, np.arange(u + 1), values, values=True)
+            want[i, h * g:(h + 1) * g] = (hi + mid - p) / (2 + p)
+            bar[i, h * g:(h + 1) * g] = 11 * 2.0 ** -24 * (hi + abs(mid) + p) / (2 + p)
+    b.q = workload.f32_to_bf16_bits(q)
+    x.q, x.k, x.v = dev(torch_dev, b.q), dev(torch_dev, x.kc), dev(torch_dev, x.vc)
+    x.decode()
+    torch_dev.cuda.synchronize()
+    got = x.out.float().cpu().numpy().astype(np.float64)
+    err = np.abs(got - want)
+    assert (np.abs(want) > 2 * bar).all(), "the inputs do not show the last bits"
+    assert (err <= 2.0 ** -8 * np.abs(want) + bar).all(), float((err / bar).max())
