@@ -90,8 +90,7 @@ int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* pl
 /*
  * Attention of a pure-decode batch (every c_i <= 1) that also gives its weights:
  * out as ssa_mixed_attention, scores_out as ssa_key_scores, with keys and values
- * read once.  The new tokens' keys and values must be in the cache.  (An infinite
- * value of a key that is seen makes its dim of the output NaN, whatever its weight.)
+ * read once.  The new tokens' keys and values must be in the cache.
  * Errors: those of ssa_key_scores; ARG also where the plan has a c_i > 1.
  */
 int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void* plan_dev,

@@ -167,6 +167,13 @@ __device__ __forceinline__ f32x4 weights4(const ScoreArgs& a, const float* x, in
 __device__ __forceinline__ int logits_at(int k0) {
   return k0 / 32 * 32 + (k0 / 4 % 2) * 16 + k0 / 8 % 4 * 4;
 }
+// Two bf16 values without their signs, and the larger of each of two such pairs.
+constexpr uint32_t kMagnitudes = 0x7FFF7FFFu, kInfBits = 0x7F80u;  // above it: NaN
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
+}
 __device__ __forceinline__ u32x2 pack4(f32x4 v) {
   return u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
@@ -303,9 +310,28 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
           }
       }
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
+      for (int t = 0; t < DT; ++t) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[0]), o[t]);
+      // An infinite value times a part that is zero or negative is not what it is times
+      // the weight: the rounded weight alone has it.
+      uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[i]), o[t]);
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = max_halves(most, vf[t][w] & kMagnitudes);
+      if (__any((most & 0xFFFFu) >= kInfBits || most >> 16 >= kInfBits)) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t v = vf[t][w] & kMagnitudes;
+            if ((v & 0xFFFFu) >= kInfBits) vf[t][w] &= 0xFFFF0000u;
+            if (v >> 16 >= kInfBits) vf[t][w] &= 0xFFFFu;
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[1]), o[t]);
+        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[2]), o[t]);
       }
       if (more) load_values(p0, p1);
       __builtin_amdgcn_sched_barrier(0);

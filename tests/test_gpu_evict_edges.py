@@ -86,3 +86,39 @@ def test_scored_decode_weighs_values_in_full(torch_dev, heads, u):
     err = np.abs(got - want)
     assert (np.abs(want) > 2 * bar).all(), "the inputs do not show the last bits"
     assert (err <= 2.0 ** -8 * np.abs(want) + bar).all(), float((err / bar).max())
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 64), (28, 4, 128)])
+@pytest.mark.parametrize("u", [3, 700, 5000])
+def test_infinite_values_of_seen_keys_stay_infinite(torch_dev, heads, u):
+    """Weights are far from underflow (logits within 20 of each other): a dim with an
+    infinite value is infinite, with both signs NaN, and the others are as they were, bit
+    for bit."""
+    hq, hkv, d = heads
+    b = batch(*heads, [1] * 3, [u, u // 2, u], seed=43)
+    x = Scored(torch_dev, b, old=False)
+    x.decode()
+    torch_dev.cuda.synchronize()
+    plain = x.out.clone()
+    rng = np.random.default_rng(44)
+    kind = np.zeros((3, hkv, d), int)  # 0: finite, 1: +inf, 2: -inf, 3: both
+    for i in range(3):
+        n = int(b.ctx_len[i]) + 1
+        for h in range(hkv):
+            dims = rng.choice(d, 9, replace=False)
+            for dim, what in zip(dims, [1, 1, 1, 2, 2, 2, 3, 3, 3]):
+                kind[i, h, dim] = what
+                at = rng.choice(n, 2, replace=False)
+                for t, bits in zip(at, {1: (0x7F80,), 2: (0xFF80,), 3: (0x7F80, 0xFF80)}[what]):
+                    x.vc[b.block_table[i, t // 16], h, dim, t % 16] = bits
+    x.v = dev(torch_dev, x.vc)
+    x.out.zero_()
+    x.decode()
+    torch_dev.cuda.synchronize()
+    x.check_scores()
+    got = x.out.float().cpu().numpy()
+    kind = np.repeat(kind, hq // hkv, axis=1)
+    assert (got[kind == 1] == np.inf).all() and (got[kind == 2] == -np.inf).all()
+    assert np.isnan(got[kind == 3]).all()
+    same = kind == 0
+    assert np.array_equal(got[same], plain.float().cpu().numpy()[same])
