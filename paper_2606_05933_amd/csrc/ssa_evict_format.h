@@ -66,7 +66,8 @@ struct ScoreItem {
   int32_t key0, key1;
   int32_t split, nsplit;  // kListDecode: split -1, the whole row (no join)
   // float offsets in the workspace for kv head 0:
-  //   chunk lists:   off0 = lse [Hkv][cols_pad]; off1 = (m, l) [Hkv][nsplit][cols_pad][2],
+  //   chunk lists:   off0 = (m 32 times, 1 / l 32 times) [Hkv][cols_pad / 32][2][32],
+  //                  off1 = (m, l) [Hkv][nsplit][cols_pad][2],
   //                  kListSum: sums [pieces][Hkv][len, padded to kSumKeys]
   //   decode lists:  off0 = logits [Hkv][G][cols_pad], off1 = records [Hkv][nsplit][record]
   int64_t off0, off1;

@@ -242,7 +242,7 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     const int64_t cols = r * g, padded = round_up(cols, kColsPad);
     it.cols_pad = (int32_t)padded;
     it.nsplit = (int32_t)ceil_div(len, piece);
-    it.off0 = take(padded * hkv);
+    it.off0 = take(padded * hkv * 2);
     it.off1 = it.nsplit > 1 ? take(padded * hkv * it.nsplit * 2) : 0;
     for (int64_t col = 0; col < cols; col += lse_cols)
       for (int32_t k = 0; k < it.nsplit; ++k) {

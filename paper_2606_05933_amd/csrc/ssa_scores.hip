@@ -1,9 +1,9 @@
 // HIP kernels for gfx950 of ssa_key_scores and ssa_decode_scored
 // (include/ssa_evict.h): the attention weights of a batch, summed per key.
 //
-// With t = scale log2(e) <q, k>, row j's weight on key t is 2^(t - L_j), L_j the
-// log2 of the sum of 2^t over the keys that it sees.  A key's score is a sum over
-// rows, and L_j a sum over keys, so the weights need L first:
+// With t = scale log2(e) <q, k>, row j's weight on key t is 2^(t - m_j) / l_j, m_j a
+// maximum and l_j the sum of 2^(t - m_j) over the keys that it sees.  A key's score is a
+// sum over rows, and l_j a sum over keys, so the weights need m and l first:
 //
 //   one counted row   The logits are few (Hq per key, against 2 D bytes of K per
 //                     kv head): a first pass reads K, writes the logits (fp32)
@@ -14,8 +14,8 @@
 //                     twice.  First pass: 64 columns (row, head) a wave stay in
 //                     registers, keys stream through LDS, and every lane keeps a
 //                     running maximum and sum of its two columns.  Second pass:
-//                     64 keys a wave stay in registers, the columns and their L
-//                     stream through LDS, and every lane sums the weights of its
+//                     64 keys a wave stay in registers, the columns with their m
+//                     and 1 / l stream through LDS, and every lane sums the weights of its
 //                     two keys.  Where there are few keys the columns are cut into
 //                     ranges too, whose sums the last workgroup of a key tile adds
 //                     in their order.
@@ -553,6 +553,23 @@ __device__ __forceinline__ float sum16(float* p) {
     for (int i = 0; i < w; ++i) p[i] += p[i + w];
   return p[0];
 }
+// A column's m and 1 / l for the second pass, in blocks of 32 columns: 32 of the one,
+// then 32 of the other.  They stay apart, so that a row's weights add up to 1: as one
+// number, m + log2(l), they were off by half a step of it, 1e-5 for logits of deviation
+// 64.  Where no weight is a number (l is 0 or NaN), m is NaN and 1 / l is 1: keys that the
+// row does not see then still get nothing.
+__device__ __forceinline__ int norm_at(int n) { return (n & ~31) * 2 + (n & 31); }
+__device__ __forceinline__ void put_norm(float* norms, int n, float m, float l) {
+  const bool weighs = l > 0.f;
+  norms[norm_at(n)] = weighs ? m : __builtin_nanf("");
+  norms[norm_at(n) + 32] = weighs ? 1.f / l : 1.f;
+}
+// a column that only pads
+__device__ __forceinline__ void put_no_norm(float* norms, int n) {
+  norms[norm_at(n)] = kInf;
+  norms[norm_at(n) + 32] = 0.f;
+}
+
 // row of a tile that register i of a lane holds, less 4 (lane / 32)
 __device__ __forceinline__ constexpr int tile_row(int i) { return (i & 3) + 8 * (i >> 2); }
 
@@ -563,7 +580,7 @@ constexpr float kRaise = 0x1p40f;
 // A column's reference m and the sum l of 2^(t - m) over one more tile.  m is a
 // maximum over some of the keys, not all: exponentials are formed against it as it
 // is, which saves the maximum over the tile, and only a tile that has one of over
-// 2^40 raises it.  L = m + log2(l) does not depend on m.
+// 2^40 raises it.  2^(t - m) / l does not depend on m.
 __device__ __forceinline__ void lse_add(const f32x16& x, float c, float* m, float* l) {
   float v[16];
 #pragma unroll
@@ -714,27 +731,28 @@ __device__ __forceinline__ void lse_item(const ScoreArgs& a, const ScoreItem& it
 #pragma unroll
     for (int r = 0; r < C::RG; ++r) ll += lds.l[r][tid] * exp2_fast(lds.m[r][tid] - ms);
     const int n = it.col0 + tid;
+    float* norms = a.ws + it.off0 + (int64_t)kvh * it.cols_pad * 2;
     if (it.nsplit > 1) {
       if (n < it.cols_pad) {
         float* to = a.ws + it.off1 + (((int64_t)kvh * it.nsplit + it.split) * it.cols_pad + n) * 2;
         *reinterpret_cast<f32x2*>(to) = f32x2{mm, ll};
       }
     } else if (n < ncols) {
-      a.ws[it.off0 + (int64_t)kvh * it.cols_pad + n] = mm + __builtin_amdgcn_logf(ll);
+      put_norm(norms, n, ms, ll);
     }
   }
   // columns that only pad: their weights are zero
   if (it.nsplit == 1 && it.col0 + C::COLS >= ncols)
     for (int n = ncols + tid; n < it.cols_pad; n += kScoreThreads)
-      a.ws[it.off0 + (int64_t)kvh * it.cols_pad + n] = kInf;
+      put_no_norm(a.ws + it.off0 + (int64_t)kvh * it.cols_pad * 2, n);
 }
 
-// L of 256 columns from the pieces of a cut key range.
+// m and l of 256 columns from the pieces of a cut key range.
 __device__ __forceinline__ void lse_join_item(const ScoreArgs& a, const ScoreItem& it, int kvh) {
   const int n = it.col0 + (int)threadIdx.x;  // < cols_pad, a multiple of 256
-  float* to = a.ws + it.off0 + (int64_t)kvh * it.cols_pad + n;
+  float* norms = a.ws + it.off0 + (int64_t)kvh * it.cols_pad * 2;
   if (n >= it.rows * a.g) {
-    *to = kInf;
+    put_no_norm(norms, n);
     return;
   }
   const float* r = a.ws + it.off1 + ((int64_t)kvh * it.nsplit * it.cols_pad + n) * 2;
@@ -746,14 +764,14 @@ __device__ __forceinline__ void lse_join_item(const ScoreArgs& a, const ScoreIte
     l = l * exp2_fast(m - ms) + v[1] * exp2_fast(v[0] - ms);
     m = mn;
   }
-  *to = m + __builtin_amdgcn_logf(l);
+  put_norm(norms, n, m, l);
 }
 
 template <int D>
 struct SumLds {
   using C = ChunkCfg<D, 4>;
   __attribute__((aligned(16))) char buf[C::NB * C::STAGE];
-  __attribute__((aligned(16))) float lse[C::NB][4][C::ROWS];  // one copy a wave
+  __attribute__((aligned(16))) float norm[C::NB][4][2 * C::ROWS];  // m, 1 / l: one copy a wave
   __attribute__((aligned(16))) float sum[C::COLS];
   int last;
 };
@@ -762,7 +780,7 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
                                          SumLds<D>& lds) {
   constexpr int NC = 4;  // tiles of 64 or 128 keys put too few products between copies
   using C = ChunkCfg<D, NC>;
-  static_assert(C::RG == 1 && C::COLS == kSumKeys, "one row group");
+  static_assert(C::RG == 1 && C::COLS == kSumKeys && C::ROWS == 32, "one row group of 32");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
@@ -775,7 +793,7 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
   const int64_t n_whole = (int64_t)(it.key0 + C::COLS - 1 - limit0) * a.g;
   // sums of 16 tiles, then the sums of those: few terms that differ much in size
   float sum[kTiles] = {}, total[kTiles] = {};
-  const float* lse = a.ws + it.off0 + (int64_t)kvh * it.cols_pad;
+  const float* norms = a.ws + it.off0 + (int64_t)kvh * it.cols_pad * 2;
   // Copy i of a stage starts at column n[i], head at[i] of its group, row from[i]:
   // stepped from stage to stage, since dividing by G for each would cost a wave more
   // scalar instructions than its products.
@@ -812,9 +830,9 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
         from[i] += wrap_step;
       }
     }
-    if (lane < C::ROWS / 4)
-      dma16(lse + nb + lane * 4,
-            reinterpret_cast<const char*>(&lds.lse[k % C::NB][wave][0]));
+    if (lane < C::ROWS / 2)
+      dma16(norms + norm_at(nb) + lane * 4,
+            reinterpret_cast<const char*>(&lds.norm[k % C::NB][wave][0]));
   };
 #pragma unroll
   for (int k = 0; k < C::NB - 1; ++k)
@@ -833,7 +851,7 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
   vm_wait<0>();  // all of it has landed: the waits below count later copies only
   const char* at[C::KS];
   fragment_addresses<C, D>(lds.buf, 0, lane, at);
-  const float* lse_at = &lds.lse[0][wave][4 * half];
+  const float* norm = &lds.norm[0][wave][4 * half];
   for_stages<C::NB>(stages, [&](int k, auto buffer) {
     if (C::NB == 3 && k + 1 < stages)
       vm_wait<C::LOADS + 1>();
@@ -843,16 +861,19 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
     if (k + C::NB - 1 < stages) issue(k + C::NB - 1);
     const int nb = n0 + k * C::ROWS;
     f32x16 acc[kTiles];
-    f32x4 lv[4];
+    f32x4 mv[4], rv[4];  // m and 1 / l of the lane's 16 columns
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      lv[i] = *reinterpret_cast<const f32x4*>(lse_at + buffer() * 4 * C::ROWS + 8 * i);
+      mv[i] = *reinterpret_cast<const f32x4*>(norm + buffer() * 8 * C::ROWS + 8 * i);
     tile_products<C, D>(at, buffer() * C::STAGE, st, acc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      rv[i] = *reinterpret_cast<const f32x4*>(norm + buffer() * 8 * C::ROWS + C::ROWS + 8 * i);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        acc[t][i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -lv[i >> 2][i & 3]));
+        acc[t][i] = exp2_fast(__builtin_fmaf(acc[t][i], a.c, -mv[i >> 2][i & 3]));
     if (nb < n_whole) {  // some row does not see some key
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -864,10 +885,14 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
     }
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      float p[16];
+      float p[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = acc[t][i];
-      sum[t] += sum16(p);
+      for (int j = 0; j < 4; ++j) {
+        p[j] = acc[t][j] * rv[0][j];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) p[j] = __builtin_fmaf(acc[t][4 * i + j], rv[i][j], p[j]);
+      }
+      sum[t] += (p[0] + p[1]) + (p[2] + p[3]);
     }
     if ((k & 15) == 15) {
 #pragma unroll

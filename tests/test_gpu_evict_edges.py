@@ -122,3 +122,31 @@ def test_infinite_values_of_seen_keys_stay_infinite(torch_dev, heads, u):
     assert np.isnan(got[kind == 3]).all()
     same = kind == 0
     assert np.array_equal(got[same], plain.float().cpu().numpy()[same])
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 64), (8, 4, 128)])
+@pytest.mark.parametrize("c,u", [([2, 2, 3], [500, 40, 300]), ([2], [9000])])
+@pytest.mark.parametrize("q_scale", [1, 16, 256])
+def test_weights_of_chunk_rows_add_up_to_one(torch_dev, heads, c, u, q_scale):
+    """A kv head's new scores of a request add up to its c G rows, however far from zero
+    the logits are: both passes form the same logits (the same products in the same
+    order), so a weight is 2^r / l with the r of l's own terms, r within 40 of zero
+    where it counts.  Per weight, in either pass: r's rounding 2^-24 64 ln 2, the
+    exponential one step; 1 / l and its product one and a half, sums over a tile's
+    rows under 8 additions; in l additions along at most (u + c) / 32 + 40 terms."""
+    b = batch(*heads, c, u, seed=45)
+    x = Scored(torch_dev, b, old=False, q_scale=q_scale)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    got = x.out_scores.cpu().numpy().astype(np.float64)
+    worst = 0.0
+    for i in range(b.num_reqs):
+        n = int(b.q_len[i] + b.ctx_len[i])
+        t = np.arange(n)
+        sums = got[b.block_table[i, t // 16], :, t % 16].sum(axis=0)
+        rows = int(b.q_len[i]) * b.shape.group
+        bar = 2.0 ** -24 * (2 * 64 * np.log(2) + 2 * 2 + 3 + 8 + n / 32 + 40)
+        off = np.abs(sums / rows - 1)
+        worst = max(worst, float(off.max() / bar))
+    say(f"    of the bar: {worst:.3f}")
+    assert worst <= 1
