@@ -25,12 +25,13 @@ def _f64(bits):
 
 
 def weights(q, k, u, scale):
-    """q [c, G, D], k [u + c, D] (float64): softmax weights [c, G, u + c]."""
+    """q [c, G, D], k [u + c, D] (float64): softmax weights [c, G, u + c], zero for the
+    keys that a row does not see (also where its others are NaN)."""
     s = np.einsum("cgd,td->cgt", q, k) * float(np.float32(scale))
     seen = np.arange(k.shape[0])[None, :] <= u + np.arange(q.shape[0])[:, None]
     s = np.where(seen[:, None, :], s, -np.inf)
     w = np.exp(s - s.max(axis=2, keepdims=True))
-    return w / w.sum(axis=2, keepdims=True)
+    return np.where(seen[:, None, :], w / w.sum(axis=2, keepdims=True), 0.0)
 
 
 def key_scores(b, k_cache, window=0, old=None, decay=1.0):

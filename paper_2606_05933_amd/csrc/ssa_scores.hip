@@ -807,7 +807,10 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
   }
   const int step_rows = div_g(a, C::ROWS), step_heads = C::ROWS - step_rows * a.g;
   const int64_t step = ((int64_t)step_rows * a.hq + step_heads) * D, wrap_step = (int64_t)(a.hq - a.g) * D;
-  const uint16_t* row0 = a.q + ((size_t)it.q_row * a.hq + kvh * a.g) * D;
+  // The request's last column, which sees every key, stands in for columns past it: what
+  // of it is not a number is so in every key's score already.
+  const uint16_t* last_col =
+      a.q + ((size_t)(it.q_row + it.rows - 1) * a.hq + kvh * a.g + a.g - 1) * D;
   auto issue = [&](int k) {
     const int nb = n0 + k * C::ROWS;
     char* buf = lds.buf + (k % C::NB) * C::STAGE;
@@ -820,8 +823,8 @@ __device__ __forceinline__ void sum_item(const ScoreArgs& a, const ScoreItem& it
         const int wrap = ((head[i] + more) * a.g_magic12) >> 12;
         dma16_base(from[i], copy_offset<C>(lane, at) + (more - lane / C::CPR + wrap * (a.hq - a.g)) * C::ROWB,
                    buf + at * C::ROWB);
-      } else {  // past the last column: any row of the request
-        dma16_base(row0, copy_offset<C>(lane, at) % C::ROWB, buf + at * C::ROWB);
+      } else {
+        dma16_base(last_col, copy_offset<C>(lane, at) % C::ROWB, buf + at * C::ROWB);
       }
       from[i] += step;
       head[i] += step_heads;

@@ -150,3 +150,35 @@ def test_weights_of_chunk_rows_add_up_to_one(torch_dev, heads, c, u, q_scale):
         worst = max(worst, float(off.max() / bar))
     say(f"    of the bar: {worst:.3f}")
     assert worst <= 1
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 64), (4, 4, 128), (28, 4, 128)])
+@pytest.mark.parametrize("row", [0, 5, -1])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_rows_that_are_not_finite_reach_only_the_keys_they_see(torch_dev, heads, row, value):
+    """One row of each chunk is not finite: the keys that it sees score NaN, later ones
+    what the other rows give them, also where padded columns stand beside."""
+    from oracle import evict
+    from paper_2606_05933_amd import workload
+    c, u = [20, 33, 7, 300], [0, 50, 700, 9]
+    b = batch(*heads, c, u, seed=46)
+    x = Scored(torch_dev, b, old=False)
+    _, size = evict.key_scores(b, x.kc)
+    start = np.cumsum(c) - c
+    bits = workload.f32_to_bf16_bits(np.asarray([value], np.float32)).ravel()[0]
+    for i in range(len(c)):
+        b.q[start[i] + row % c[i], :, 3] = bits
+    x.q = dev(torch_dev, b.q)
+    x.scores()
+    torch_dev.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        ref, _ = evict.key_scores(b, x.kc)
+    got = x.out_scores.cpu().numpy().astype(np.float64)
+    for i in range(len(c)):
+        t = np.arange(c[i] + u[i])
+        at = b.block_table[i, t // 16], slice(None), t % 16
+        seen = t <= u[i] + row % c[i]
+        assert np.isnan(ref[at][seen]).all() and np.isfinite(ref[at][~seen]).all()
+        assert np.isnan(got[at][seen]).all()
+        err, tol = np.abs(got[at] - ref[at])[~seen], (x.rel(size)[at] * ref[at])[~seen]
+        assert (err <= tol).all(), (i, int(np.isnan(err).sum()), err.size)
