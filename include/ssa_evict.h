@@ -198,8 +198,8 @@ typedef struct ssa_layer_eviction {
  * shifts, out and the caches are bit for bit those of ssa_layer_forward.
  * Everything is validated before the first launch.
  * Errors: those of ssa_layer_forward, ssa_key_scores and ssa_rope_append_shifted;
- * NULL (eviction); PLAN_MISMATCH also where the two plans differ in requests, tokens
- * or their longest request's new tokens.
+ * NULL (eviction); PLAN_MISMATCH also where the two plans are not of the same batch
+ * (q_len and ctx_len of every request).
  */
 int ssa_layer_forward_evicting(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                                const ssa_layer_weights* w, const ssa_layer_eviction* eviction,

@@ -1,7 +1,7 @@
 // Plan blobs of include/ssa_evict.h: written by the host planner
 // (ssa_evict_plan.cpp), read unchanged by the kernels.
 //
-//   score plan  [ScoreHeader][ScoreItem x (the five lists)]
+//   score plan  [ScoreHeader][ScoreReq x num_reqs][ScoreItem x (the five lists)]
 //   evict plan  [EvictHeader][EvictReq x num_reqs][EvictShort x num_short]
 //               [EvictSeg x num_segs][EvictItem x num_items]
 //
@@ -12,7 +12,8 @@
 
 namespace ssa {
 
-constexpr uint32_t kScoreMagic = 0x31435353u;  // "SSC1"
+// Kind and, in the last character, version of the layout.
+constexpr uint32_t kScoreMagic = 0x32435353u;  // "SSC2"
 constexpr uint32_t kEvictMagic = 0x31565353u;  // "SSV1"
 constexpr int kScoreThreads = 256;             // four waves
 constexpr int kScoreWaveCols = 64;             // stationary vectors of a wave (chunk kernels)
@@ -53,6 +54,11 @@ struct ScoreHeader {
   int64_t plan_bytes, ws_bytes;
 };
 static_assert(sizeof(ScoreHeader) == 128, "score header size");
+
+// The batch that the plan is of; host side only.
+struct ScoreReq {
+  int32_t q_len, ctx_len;
+};
 
 struct ScoreItem {
   int32_t req;

@@ -66,6 +66,7 @@ uint64_t hash_shape(const ssa_shape* s, const int32_t* more, int n_more) {
 
 struct ScorePlan {
   ScoreHeader hdr;
+  std::vector<ScoreReq> reqs;
   std::vector<ScoreItem> list[kNumScoreLists];
 };
 
@@ -307,7 +308,8 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
   h.num_pages = s->num_pages;
   h.softmax_scale = s->softmax_scale;
   h.max_q_len = (int32_t)max_q;
-  h.off_items = sizeof(ScoreHeader);
+  const int64_t off_items =
+      round_up((int64_t)sizeof(ScoreHeader) + (int64_t)sizeof(ScoreReq) * n, sizeof(ScoreItem));
   int64_t items = 0;
   for (int l = 0; l < kNumScoreLists; ++l) {
     const int64_t count = (int64_t)p->list[l].size();
@@ -316,8 +318,11 @@ int build_score(const ssa_shape* s, const int32_t* q_len, const int32_t* ctx_len
     h.count[l] = (int32_t)count;
     items += count;
   }
-  h.plan_bytes = h.off_items + items * (int64_t)sizeof(ScoreItem);
+  h.plan_bytes = off_items + items * (int64_t)sizeof(ScoreItem);
   if (h.plan_bytes > INT32_MAX) return SSA_ERR_LENGTH;
+  h.off_items = (int32_t)off_items;
+  p->reqs.reserve(n);
+  for (int32_t i = 0; i < n; ++i) p->reqs.push_back({q_len[i], ctx_len[i]});
   h.ws_bytes = std::max<int64_t>(256, ws * 4);
   uint64_t hv = hash_shape(s, &last_rows, 1);
   if (n > 0) {
@@ -467,6 +472,9 @@ int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int3
     if (plan_bytes < (size_t)p.hdr.plan_bytes) return SSA_ERR_PLAN_SIZE;
     char* b = static_cast<char*>(plan_host);
     std::memcpy(b, &p.hdr, sizeof p.hdr);
+    std::memset(b + sizeof p.hdr, 0, p.hdr.off_items - sizeof p.hdr);
+    if (!p.reqs.empty())
+      std::memcpy(b + sizeof p.hdr, p.reqs.data(), sizeof(ssa::ScoreReq) * p.reqs.size());
     char* at = b + p.hdr.off_items;
     for (const auto& l : p.list) {
       if (!l.empty()) std::memcpy(at, l.data(), sizeof(ssa::ScoreItem) * l.size());

@@ -99,10 +99,12 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
   if (score_plan) {
     const ScoreHeader* sh = nullptr;
     if ((rc = check_score_plan(shape, score_plan, &sh))) return rc;
-    int32_t longest = 0;
-    for (int32_t i = 0; i < h->num_reqs; ++i) longest = std::max(longest, reqs[i].q_len);
-    if (sh->num_reqs != h->num_reqs || sh->num_tokens != t || sh->max_q_len != longest)
-      return SSA_ERR_PLAN_MISMATCH;
+    if (sh->num_reqs != h->num_reqs) return SSA_ERR_PLAN_MISMATCH;
+    const ScoreReq* scored = reinterpret_cast<const ScoreReq*>(
+        static_cast<const uint8_t*>(score_plan) + sizeof(ScoreHeader));
+    for (int32_t i = 0; i < h->num_reqs; ++i)
+      if (scored[i].q_len != reqs[i].q_len || scored[i].ctx_len != reqs[i].ctx_len)
+        return SSA_ERR_PLAN_MISMATCH;
   }
   if (t == 0) return SSA_OK;
   if (!x || !out || !k_cache || !v_cache || !block_table || !w->attn_norm || !w->w_qkv ||

@@ -914,7 +914,7 @@ def evict_plan(shape: SsaShape, kv_len, budget, sink: int, recent: int, out=None
 
 
 # The 128-byte plan headers (ssa_evict_format.h, ssa_plan_format.h).
-_SCORE_MAGIC, _EVICT_MAGIC, _PLAN_MAGIC = 0x31435353, 0x31565353, 0x31415353
+_SCORE_MAGIC, _EVICT_MAGIC, _PLAN_MAGIC = 0x32435353, 0x31565353, 0x31415353
 
 
 _HeaderWords = ctypes.c_int32 * 32

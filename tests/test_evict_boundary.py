@@ -398,3 +398,48 @@ def test_oracle_selection_by_hand():
     assert oev.select(x, 9, 0, 1).tolist() == [0, 1, 2, 3, 4, 5, 7, 8, 9]  # NaN before -inf by index
     assert oev.select(x, 2, 2, 0).tolist() == [0, 1]
     assert oev.select(x, 10, 0, 0).tolist() == list(range(10))
+
+
+def test_an_evicting_layer_takes_a_score_plan_of_its_own_batch_only():
+    """Lengths of every request count: a plan of an earlier iteration, or with two
+    requests' lengths exchanged, names other pages and other keys."""
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    vp = ctypes.c_void_p
+    w = ssa.SsaLayerWeights(16, 16, 16, 16, 16, 16, 16, 256, 128, 64, 1e-5)
+
+    def call(c, u, scored_c, scored_u):
+        """Past the plans' check it ends at the layer's workspace, which is too small."""
+        plan, _ = ssa.ssa_plan(shape, c, u)
+        score, _ = ssa.score_plan(shape, scored_c, scored_u)
+        e = ssa.SsaLayerEviction(score_plan_host=score.ctypes.data, score_plan_dev=16,
+                                 scores_out=16, score_workspace=16, score_ws_bytes=1 << 20,
+                                 decay=1.0)
+        return LIB.ssa_layer_forward_evicting(
+            ctypes.byref(shape), plan.ctypes.data, vp(16), ctypes.byref(w), ctypes.byref(e), vp(16),
+            vp(16), vp(16), vp(16), vp(16), vp(16), 256, None)
+
+    def refused(*a):
+        return call(*a) == ssa.SSA_ERR_PLAN_MISMATCH
+
+    assert call([1, 1], [10, 20], [1, 1], [10, 20]) == ssa.SSA_ERR_WORKSPACE
+    assert call([3, 0, 1], [9, 30, 20], [3, 0, 1], [9, 30, 20]) == ssa.SSA_ERR_WORKSPACE
+    assert refused([1, 1], [10, 20], [1, 1], [9, 19])       # the iteration before
+    assert refused([1, 1], [10, 20], [1, 1], [30, 20])      # before an eviction
+    assert refused([1, 1], [10, 20], [1, 1], [20, 10])
+    assert refused([3, 1], [10, 20], [1, 3], [10, 20])
+    assert refused([3, 1], [10, 20], [1, 3], [20, 10])
+    assert refused([1, 0, 1], [10, 5, 20], [1, 1, 0], [10, 5, 20])
+
+
+@pytest.mark.parametrize("n", [0, 1, 7, 8, 9, 200])
+def test_a_score_plan_names_its_batch(n):
+    rng = np.random.default_rng(n)
+    c, u = rng.integers(0, 3, n).astype(np.int32), rng.integers(0, 300, n).astype(np.int32)
+    shape = shape_of(8, 2, 64, c + u if n else [])
+    plan = np.full(ssa.score_plan(shape, c, u)[0].nbytes, 0xA5, np.uint8)
+    ssa.score_plan(shape, c, u, out=plan)
+    h, _ = parse(plan)
+    assert h["off_items"] % 64 == 0 and h["off_items"] >= 128 + 8 * n
+    reqs = plan[128:128 + 8 * n].view(np.int32).reshape(n, 2)
+    assert np.array_equal(reqs[:, 0], c) and np.array_equal(reqs[:, 1], u)
+    assert not plan[128 + 8 * n:h["off_items"]].any()
