@@ -1113,7 +1113,8 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
                            stream=None):
     """ssa_layer_forward_evicting: layer_forward whose rows also add their attention
     weights to the scores (with a score plan) and whose tokens are rotated at shifted
-    positions (with shifts)."""
+    positions (with shifts).  Buffers of the scores without a score plan are refused, and
+    so is one of the two shift arrays without the other."""
     what = "ssa_layer_forward_evicting"
     at, h = _header(plan_host, _PLAN_MAGIC, what)
     check = _Buffers()
@@ -1126,12 +1127,14 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
         e.scores_in = check("scores_in", scores_in, slots, 4)
         e.scores_out = check("scores_out", scores_out, slots, 4)
         e.score_workspace, e.score_ws_bytes = check.workspace(score_workspace)
+    elif not (score_plan_dev is scores_in is scores_out is score_workspace is None):
+        raise ValueError("buffers of the scores are given, but no score_plan_host")
+    e.shift_dev = check("shift_dev", shift_dev, n, 4)
     if shift_host is not None:
         shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
         if shift_host.size != n:
             raise ValueError(f"{shift_host.size} shifts for {n} requests")
         e.shift_host = _address(shift_host)
-        e.shift_dev = check("shift_dev", shift_dev, n, 4)
     ws, ws_bytes = check.workspace(workspace)
     rc = LIB.ssa_layer_forward_evicting(
         shape, at, check.plan(plan_dev, plan_host), weights.c, e,

@@ -182,3 +182,36 @@ def test_rows_that_are_not_finite_reach_only_the_keys_they_see(torch_dev, heads,
         assert np.isnan(got[at][seen]).all()
         err, tol = np.abs(got[at] - ref[at])[~seen], (x.rel(size)[at] * ref[at])[~seen]
         assert (err <= tol).all(), (i, int(np.isnan(err).sum()), err.size)
+
+
+def test_an_evicting_layer_refuses_half_given_parts(torch_dev):
+    """Shifts of which only one copy is given, and buffers of the scores without their
+    plan: nothing is written to the caches."""
+    torch = torch_dev
+    from paper_2606_05933_amd import ssa, workload
+    hq, hkv, d, hidden, inter = 8, 2, 64, 256, 128
+    b = batch(hq, hkv, d, [2, 1], [30, 5], seed=47)
+    shape = ssa.make_shape(hq, hkv, d, b.num_pages, b.max_pages_per_req, d ** -0.5)
+    w = ssa.LayerWeights(workload.layer_weights(1, hidden, inter, hq, hkv, d), hq, hkv, d, 2048)
+    x = dev(torch, workload.normal_bf16((3, hidden), 5))
+    plan, _ = ssa.ssa_plan(shape, b.q_len, b.ctx_len)
+    k, v = dev(torch, b.k_cache), dev(torch, b.v_cache)
+    before = k.clone(), v.clone()
+    ws = torch.zeros(ssa.layer_workspace_size(shape, plan, w), dtype=torch.uint8, device="cuda")
+    scores = torch.zeros((b.num_pages, hkv, 16), device="cuda")
+    shift = np.array([7, 9], np.int32)
+
+    def call(**parts):
+        ssa.layer_forward_evicting(shape, plan, dev(torch, plan), w, x, torch.empty_like(x), k, v,
+                                   dev(torch, b.block_table), ws, **parts)
+
+    for parts in (dict(shift_dev=dev(torch, shift)), dict(shift_host=shift)):
+        with pytest.raises(ssa.SsaError) as e:
+            call(**parts)
+        assert e.value.code == ssa.SSA_ERR_NULL
+    for name in ("scores_in", "scores_out", "score_workspace", "score_plan_dev"):
+        with pytest.raises(ValueError):
+            call(**{name: scores})
+    torch.cuda.synchronize()
+    assert torch.equal(k.view(torch.int16), before[0].view(torch.int16))
+    assert torch.equal(v.view(torch.int16), before[1].view(torch.int16))
