@@ -26,7 +26,8 @@
  * plans are position-independent but not interchangeable with ssa_plan's.
  * Workspaces need no clearing: a call reads nothing of them that it has not
  * written itself.  Calls that share a workspace must be ordered on one stream.
- * Pointers to queries, pools, scores, outputs and workspaces are 16-byte aligned.
+ * Pointers to queries, pools, scores, outputs and workspaces are 16-byte aligned,
+ * plan_dev is 8-byte aligned.
  * Results do not depend on the order in which workgroups run (no atomics on
  * outputs).  All calls can be captured into a HIP graph; the plan at plan_dev
  * must then stay as it is for the replays.
@@ -80,7 +81,7 @@ int ssa_score_plan(const ssa_shape* shape, const int32_t* q_len_host, const int3
  *   Requests with c_i = 0, slots past a request's last key and other pages are
  *   left as they are.  Pages must not be shared between requests with c_i > 0.
  * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, ARG (decay; a
- * misaligned pointer), HIP.
+ * misaligned pointer or plan), HIP.
  */
 int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                    const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
@@ -122,7 +123,7 @@ int ssa_evict_plan(const ssa_shape* shape, const int32_t* kv_len_host, const int
  * stays first; a NaN counts as -infinity; -0 equals +0.  A request that keeps all
  * its keys lists 0 .. n_i - 1.
  * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, ARG (a misaligned
- * pointer), HIP.
+ * pointer or plan), HIP.
  */
 int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                      const float* scores, const int32_t* block_table, int32_t* keep,
@@ -139,7 +140,7 @@ int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* 
  * (ssa_check_evict_tables).  An index of keep outside [0, kv_len[i]) is not
  * followed: its slot is left as it is.
  *   scores may be NULL (none are kept).
- * Errors: NULL, the shape errors, PLAN_MISMATCH, ARG (a misaligned pool), HIP.
+ * Errors: NULL, the shape errors, PLAN_MISMATCH, ARG (a misaligned pool or plan), HIP.
  */
 int ssa_evict_compact(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                       const int32_t* keep, const int32_t* block_table, const int32_t* new_table,

@@ -573,6 +573,11 @@ bool misaligned(std::initializer_list<const void*> pointers) {
   return false;
 }
 
+// Items hold 64-bit fields.
+bool misaligned_plan(const void* plan_dev) {
+  return reinterpret_cast<uintptr_t>(plan_dev) % 8 != 0;
+}
+
 EvictArgs evict_args(const EvictHeader* h, const void* plan_dev, const int32_t* block_table) {
   EvictArgs a{};
   a.plan = static_cast<const uint8_t*>(plan_dev);
@@ -601,6 +606,7 @@ int ssa_evict_select(const ssa_shape* shape, const void* plan_host, const void* 
   if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
   if (misaligned({scores, workspace})) return SSA_ERR_ARG;
   if (h->num_keep == 0) return SSA_OK;
+  if (misaligned_plan(plan_dev)) return SSA_ERR_ARG;
   EvictArgs a = evict_args(h, plan_dev, block_table);
   a.scores = scores;
   a.keep = keep;
@@ -632,7 +638,7 @@ int ssa_evict_compact(const ssa_shape* shape, const void* plan_host, const void*
   if (!plan_dev) return SSA_ERR_NULL;
   if (h->num_items == 0) return SSA_OK;
   if (!keep || !block_table || !new_table || !k_cache || !v_cache) return SSA_ERR_NULL;
-  if (misaligned({k_cache, v_cache})) return SSA_ERR_ARG;
+  if (misaligned({k_cache, v_cache}) || misaligned_plan(plan_dev)) return SSA_ERR_ARG;
   EvictArgs a = evict_args(h, plan_dev, block_table);
   a.workgroups = h->num_items * h->hkv;
   a.keep_in = keep;

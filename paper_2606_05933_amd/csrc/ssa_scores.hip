@@ -1045,6 +1045,12 @@ bool misaligned(std::initializer_list<const void*> pointers) {
   return false;
 }
 
+// The scalar loads of the plan's header drop the low bits of its address: the kernel would
+// find another plan there and do nothing.
+bool misaligned_plan(const ScoreHeader* h, const void* plan_dev) {
+  return h->max_q_len > 0 && reinterpret_cast<uintptr_t>(plan_dev) % 8;
+}
+
 int score_args(const ssa_shape* shape, const ScoreHeader* h, const void* plan_dev,
                const uint16_t* q, const uint16_t* k_cache, const int32_t* block_table,
                const float* scores_in, float decay, float* scores_out, void* workspace,
@@ -1086,9 +1092,11 @@ int check_key_scores(const ssa_shape* shape, const void* plan_host, const void* 
                      size_t ws_bytes) {
   const ScoreHeader* h = nullptr;
   const int rc = check_score_plan(shape, plan_host, &h);
+  if (rc) return rc;
   ScoreArgs a;
-  return rc ? rc : score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay,
+  const int args = score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay,
                               scores_out, workspace, ws_bytes, &a);
+  return args ? args : misaligned_plan(h, plan_dev) ? SSA_ERR_ARG : SSA_OK;
 }
 
 }  // namespace ssa
@@ -1106,6 +1114,7 @@ int ssa_key_scores(const ssa_shape* shape, const void* plan_host, const void* pl
   if ((rc = score_args(shape, h, plan_dev, q, k_cache, block_table, scores_in, decay, scores_out,
                        workspace, ws_bytes, &a)))
     return rc;
+  if (misaligned_plan(h, plan_dev)) return SSA_ERR_ARG;
   (void)hipGetLastError();
   hipStream_t s = static_cast<hipStream_t>(stream);
   return h->head_dim == 128 ? launch_scores<128>(a, h, s) : launch_scores<64>(a, h, s);
@@ -1125,7 +1134,7 @@ int ssa_decode_scored(const ssa_shape* shape, const void* plan_host, const void*
                        workspace, ws_bytes, &a)))
     return rc;
   if (h->max_q_len > 0 && (!v_cache || !out)) return SSA_ERR_NULL;
-  if (misaligned({v_cache, out})) return SSA_ERR_ARG;
+  if (misaligned({v_cache, out}) || misaligned_plan(h, plan_dev)) return SSA_ERR_ARG;
   a.vc = v_cache;
   a.out = out;
   (void)hipGetLastError();

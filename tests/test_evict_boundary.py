@@ -443,3 +443,27 @@ def test_a_score_plan_names_its_batch(n):
     reqs = plan[128:128 + 8 * n].view(np.int32).reshape(n, 2)
     assert np.array_equal(reqs[:, 0], c) and np.array_equal(reqs[:, 1], u)
     assert not plan[128 + 8 * n:h["off_items"]].any()
+
+
+def test_misaligned_plans_are_refused():
+    """plan_dev at another multiple than 8: the kernels would read another header, write
+    nothing and say nothing.  Only calls with something to do look at it."""
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    s, vp = ctypes.byref(shape), ctypes.c_void_p
+    score, ws = ssa.score_plan(shape, [1, 1], [10, 20])
+    evict, ews = ssa.evict_plan(shape, [100], [70], 4, 8)
+    plan, _ = ssa.ssa_plan(shape, [1, 1], [10, 20])
+    w = ssa.SsaLayerWeights(16, 16, 16, 16, 16, 16, 16, 256, 128, 64, 1e-5)
+    p = vp(16)
+    for dev in (4097, 4098, 4100, 4092):
+        at = vp(dev)
+        assert call_scores(shape, score, dev=dev) == ssa.SSA_ERR_ARG
+        assert call_scores(shape, score, dev=dev, fn="ssa_decode_scored", n_ptr=16) == ssa.SSA_ERR_ARG
+        assert LIB.ssa_evict_select(s, evict.ctypes.data, at, p, p, p, p, ews, None) == ssa.SSA_ERR_ARG
+        assert LIB.ssa_evict_compact(s, evict.ctypes.data, at, p, p, p, p, p, p,
+                                     None) == ssa.SSA_ERR_ARG
+        e = ssa.SsaLayerEviction(score_plan_host=score.ctypes.data, score_plan_dev=dev,
+                                 scores_out=16, score_workspace=16, score_ws_bytes=ws, decay=1.0)
+        assert LIB.ssa_layer_forward_evicting(s, plan.ctypes.data, p, ctypes.byref(w),
+                                              ctypes.byref(e), p, p, p, p, p, p, 1 << 30,
+                                              None) == ssa.SSA_ERR_ARG
