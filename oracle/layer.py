@@ -75,18 +75,21 @@ def from_bits(b) -> np.ndarray:
 
 
 def decoder_layer(x, wts, hq, hkv, d, q_len, ctx_len, block_table, k_cache, v_cache, eps,
-                  base=500000.0, scale=None):
+                  base=500000.0, scale=None, shift=None):
     """One decoder layer over the new tokens of a batch B = {(c_i, u_i)}.
 
     x [T, hidden] and the weights (dict: attn_norm, w_q, w_k, w_v, w_o, mlp_norm,
     w_gate, w_up, w_down, as bf16 bit arrays) are bf16; k_cache / v_cache are the
-    pools before the iteration (bf16 bits).  Returns (out [T, hidden] float64,
+    pools before the iteration (bf16 bits).  shift: per request, how far its tokens'
+    positions lie past their cache indexes (None: not at all).  Returns (out [T, hidden] float64,
     bf16-exact; the pools after the append)."""
     from oracle import oracle as attn_oracle  # the attention and kv_append oracle
     f = {k: from_bits(v) for k, v in wts.items()}
     xf = from_bits(x)
     t = xf.shape[0]
     pos = positions(q_len, ctx_len)
+    if shift is not None:
+        pos = pos + np.repeat(shift, q_len)
     xn = bf16_round(rms_norm(xf, f["attn_norm"], eps))
     q = bf16_round(linear(xn, f["w_q"])).reshape(t, hq, d)
     k = bf16_round(linear(xn, f["w_k"])).reshape(t, hkv, d)

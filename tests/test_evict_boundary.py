@@ -467,3 +467,19 @@ def test_misaligned_plans_are_refused():
         assert LIB.ssa_layer_forward_evicting(s, plan.ctypes.data, p, ctypes.byref(w),
                                               ctypes.byref(e), p, p, p, p, p, p, 1 << 30,
                                               None) == ssa.SSA_ERR_ARG
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_norms_of_chunk_columns_have_room_for_two_numbers(seed):
+    """A padded column's maximum and reciprocal sum per kv head: no other range of the
+    workspace begins within them."""
+    rng = np.random.default_rng(100 + seed)
+    c, u = rng.choice([2, 17, 64, 300, 1000], 5), rng.choice([0, 40, 5000, 30000], 5)
+    hq, hkv, d = [(8, 8, 64), (32, 8, 128), (28, 4, 128), (16, 1, 64), (5, 5, 128)][seed % 5]
+    plan, ws = ssa.score_plan(shape_of(hq, hkv, d, c + u), c, u)
+    h, items = parse(plan)
+    starts = {int(x[f]) for n in LISTS for x in items[n] for f in ("off0", "off1")
+              if f == "off0" or x["nsplit"] > 1} | {ws // 4}
+    for x in items["lse"]:
+        end = int(x["off0"]) + 2 * hkv * int(x["cols_pad"])
+        assert end <= ws // 4 and not any(x["off0"] < s < end for s in starts)

@@ -215,3 +215,109 @@ def test_an_evicting_layer_refuses_half_given_parts(torch_dev):
     torch.cuda.synchronize()
     assert torch.equal(k.view(torch.int16), before[0].view(torch.int16))
     assert torch.equal(v.view(torch.int16), before[1].view(torch.int16))
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 2, 128)])
+@pytest.mark.parametrize("c", [1, 20])
+@pytest.mark.parametrize("gain", [30, 3000])
+def test_far_logits_give_their_weight_to_the_keys_that_have_it(torch_dev, heads, c, gain):
+    """Logits up to 1e4 and more, nearly all weight on one key a row: every key's score
+    by the oracle's.  A logit and the sum's logarithm are each off by D 2^-24 A, so a
+    weight by a factor of at most exp(rel) (rel: the bar of the other tests); weights
+    under 2^-126 may be zero."""
+    from oracle import evict
+    from paper_2606_05933_amd import workload
+    b = batch(*heads, [c, c], [300, 3000], seed=48)
+    b.q = workload.f32_to_bf16_bits(workload.bf16_bits_to_f32(b.q) * np.float32(gain))
+    x = Scored(torch_dev, b, old=False)
+    ref, size = evict.key_scores(b, x.kc)
+    bar = np.expm1(x.rel(size)) * ref + c * b.shape.group * 2.0 ** -126
+    known = ~np.isnan(ref)
+    if gain == 30:  # the bar tells a row's keys from one another
+        assert np.nanmax(x.rel(size)) < 0.01 and np.nanmax(ref) > 100 * np.nanmedian(ref)
+
+    def check():
+        torch_dev.cuda.synchronize()
+        got = x.out_scores.cpu().numpy().astype(np.float64)
+        err = np.abs(got - ref)
+        assert (err <= bar)[known].all(), float(np.nanmax((err / bar)[known]))
+
+    x.scores()
+    check()
+    if c == 1:
+        x.out_scores.fill_(-7.0)
+        x.decode()
+        check()
+        x.check_out()
+
+
+@pytest.mark.parametrize("cu,shift", [([(20, 30), (1, 100), (1, 5), (37, 0)], [400, 77, 0, 0]),
+                                      ([(1, 90), (1, 700), (1, 3)], [30, 900, 0])])
+def test_an_evicting_layer_matches_the_oracle(torch_dev, cu, shift):
+    """The whole shifted layer, its output included, and its scores, eagerly and replayed
+    from a graph.  Between x and out lie seven bf16 tensors, each at most a step apart
+    from the oracle's: the bar of the plain layer's test."""
+    torch = torch_dev
+    from oracle import evict, layer as olay
+    from paper_2606_05933_amd import ssa, workload
+    from paper_2606_05933_amd.device import bits_of
+    hidden, inter, hq, hkv, d = 256, 256, 4, 2, 64
+    c, u = [p[0] for p in cu], [p[1] for p in cu]
+    wts = workload.layer_weights(49, hidden, inter, hq, hkv, d)
+    b = batch(hq, hkv, d, c, u, seed=49)
+    T = b.num_tokens
+    shift = np.asarray(shift, np.int32)
+    shape = ssa.make_shape(hq, hkv, d, b.num_pages, b.max_pages_per_req, d ** -0.5)
+    w = ssa.LayerWeights(wts, hq, hkv, d, max_position=2048)
+    plan, _ = ssa.ssa_plan(shape, c, u)
+    sp, sws = ssa.score_plan(shape, c, u)
+    x = workload.normal_bf16((T, hidden), 50)
+    xd, k, v = dev(torch, x), dev(torch, b.k_cache), dev(torch, b.v_cache)
+    out = torch.zeros((T, hidden), dtype=torch.bfloat16, device="cuda")
+    scores = torch.full((b.num_pages, hkv, 16), -7.0, device="cuda")
+    ws = torch.zeros(ssa.layer_workspace_size(shape, plan, w), dtype=torch.uint8, device="cuda")
+    score_ws = torch.full((sws,), 0xFF, dtype=torch.uint8, device="cuda")
+    held = [dev(torch, a) for a in (plan, b.block_table, sp, shift)]
+
+    def layer():
+        ssa.layer_forward_evicting(shape, plan, held[0], w, xd, out, k, v, held[1], ws, sp, held[2],
+                                   None, 1.0, scores, score_ws, shift, held[3])
+
+    layer()
+    torch.cuda.synchronize()
+    ref, kc_ref, vc_ref = olay.decoder_layer(x, wts, hq, hkv, d, b.q_len, b.ctx_len, b.block_table,
+                                             b.k_cache, b.v_cache, eps=1e-5, shift=shift)
+    got = out.float().cpu().numpy().astype(np.float64)
+    err = np.abs(got - ref)
+    say(f"    out: max_abs={err.max():.3e} mean_abs={err.mean():.3e}")
+    assert np.isfinite(got).all()
+    assert (err <= 2.0 ** -5 * (np.abs(ref) + 1.0)).all() and err.mean() <= 3e-3
+    plain, _, _ = olay.decoder_layer(x, wts, hq, hkv, d, b.q_len, b.ctx_len, b.block_table, b.k_cache,
+                                     b.v_cache, eps=1e-5)
+    assert np.abs(plain - ref).mean() > 4 * err.mean(), "the shift does not show"
+    # each row's weights add up to 1 over the keys that it sees
+    sc = scores.cpu().numpy().astype(np.float64)
+    for i in range(len(c)):
+        t = np.arange(c[i] + u[i])
+        sums = sc[b.block_table[i, t // 16], :, t % 16].sum(axis=0)
+        assert np.allclose(sums, c[i] * hq // hkv, rtol=1e-5)
+    want = [t.clone() for t in (out, k, v, scores)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        layer()  # warm the stream before capture
+        with torch.cuda.graph(graph, stream=side):
+            layer()
+    for r in range(4):
+        k.copy_(dev(torch, b.k_cache))
+        v.copy_(dev(torch, b.v_cache))
+        out.zero_()
+        scores.fill_(-7.0)
+        score_ws.fill_(0xA5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, e in zip((out, k, v, scores), want):
+            a, e = (t.view(torch.int16) if t.dtype == torch.bfloat16 else t for t in (a, e))
+            assert torch.equal(a, e), r
