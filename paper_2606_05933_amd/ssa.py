@@ -913,10 +913,12 @@ def evict_plan(shape: SsaShape, kv_len, budget, sink: int, recent: int, out=None
     return out, wb.value
 
 
-# The 128-byte plan headers (ssa_evict_format.h, ssa_plan_format.h).
+# The plan headers' magics (kind and version) and the int32 words of their first 128 bytes
+# that the wrappers read (ssa_evict_format.h, ssa_plan_format.h).
 _SCORE_MAGIC, _EVICT_MAGIC, _PLAN_MAGIC = 0x32435353, 0x31565353, 0x31415353
-
-
+_SCORE_REQS, _SCORE_TOKENS = 4, 5
+_EVICT_REQS, _EVICT_KEEP_LO, _EVICT_KEEP_HI = 3, 20, 21
+_PLAN_REQS, _PLAN_TOKENS = 4, 5
 _HeaderWords = ctypes.c_int32 * 32
 
 
@@ -992,10 +994,10 @@ def _scored_args(what, shape, plan_host, plan_dev, q, k_cache, block_table, scor
     at, h = _header(plan_host, _SCORE_MAGIC, what)
     check = _Buffers()
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
-    rows = h[5] * shape.num_q_heads * shape.head_dim
+    rows = h[_SCORE_TOKENS] * shape.num_q_heads * shape.head_dim
     return (check, rows, at, check.plan(plan_dev, plan_host), check("q", q, rows, 2),
             check("k_cache", k_cache, slots * shape.head_dim, 2),
-            check("block_table", block_table, h[4] * shape.max_pages_per_req, 4),
+            check("block_table", block_table, h[_SCORE_REQS] * shape.max_pages_per_req, 4),
             check("scores_in", scores_in, slots, 4), check("scores_out", scores_out, slots, 4),
             *check.workspace(workspace))
 
@@ -1028,7 +1030,7 @@ def decode_scored(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, blo
 
 def _num_keep(h, shape) -> int:
     """Entries of the kept keys' lists, from an eviction plan's header."""
-    return (h[20] & 0xFFFFFFFF | h[21] << 32) * shape.num_kv_heads
+    return (h[_EVICT_KEEP_LO] & 0xFFFFFFFF | h[_EVICT_KEEP_HI] << 32) * shape.num_kv_heads
 
 
 def evict_select(shape: SsaShape, plan_host, plan_dev, scores, block_table, keep, workspace,
@@ -1041,7 +1043,7 @@ def evict_select(shape: SsaShape, plan_host, plan_dev, scores, block_table, keep
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
     rc = LIB.ssa_evict_select(
         shape, at, check.plan(plan_dev, plan_host), check("scores", scores, slots, 4),
-        check("block_table", block_table, h[3] * shape.max_pages_per_req, 4),
+        check("block_table", block_table, h[_EVICT_REQS] * shape.max_pages_per_req, 4),
         check("keep", keep, _num_keep(h, shape), 4), ws, n, check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_evict_select")
@@ -1054,7 +1056,7 @@ def evict_compact(shape: SsaShape, plan_host, plan_dev, keep, block_table, new_t
     at, h = _header(plan_host, _EVICT_MAGIC, "ssa_evict_compact")
     check = _Buffers()
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
-    entries = h[3] * shape.max_pages_per_req
+    entries = h[_EVICT_REQS] * shape.max_pages_per_req
     rc = LIB.ssa_evict_compact(
         shape, at, check.plan(plan_dev, plan_host), check("keep", keep, _num_keep(h, shape), 4),
         check("block_table", block_table, entries, 4), check("new_table", new_table, entries, 4),
@@ -1073,9 +1075,9 @@ def check_evict_tables(shape: SsaShape, plan_host, block_table_host, new_table_h
     for t in (block_table_host, new_table_host):
         if t is not None:
             t = np.ascontiguousarray(t, dtype=np.int32)
-            if t.shape != (h[3], shape.max_pages_per_req):
+            if t.shape != (h[_EVICT_REQS], shape.max_pages_per_req):
                 raise ValueError(f"table of shape {t.shape}, the plan needs "
-                                 f"({h[3]}, {shape.max_pages_per_req})")
+                                 f"({h[_EVICT_REQS]}, {shape.max_pages_per_req})")
         tables.append(t)
     _check(LIB.ssa_check_evict_tables(shape, at, _ptr(tables[0]), _ptr(tables[1])),
            "ssa_check_evict_tables")
@@ -1088,7 +1090,8 @@ def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shif
     the same on the device) positions past their cache index."""
     at, h = _header(plan_host, _PLAN_MAGIC, "ssa_rope_append_shifted")
     check = _Buffers()
-    n, tokens, d, hq, hkv = h[4], h[5], shape.head_dim, shape.num_q_heads, shape.num_kv_heads
+    n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
+    d, hq, hkv = shape.head_dim, shape.num_q_heads, shape.num_kv_heads
     pool = shape.num_pages * hkv * shape.page_size * d
     if not (isinstance(shift_host, np.ndarray) and shift_host.dtype == np.int32
             and shift_host.flags.c_contiguous):
@@ -1118,7 +1121,7 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
     what = "ssa_layer_forward_evicting"
     at, h = _header(plan_host, _PLAN_MAGIC, what)
     check = _Buffers()
-    n, tokens = h[4], h[5]
+    n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
     e = SsaLayerEviction(decay=decay)
     if score_plan_host is not None:
