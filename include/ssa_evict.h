@@ -121,7 +121,9 @@ int ssa_evict_plan(const ssa_shape* shape, const int32_t* kv_len_host, const int
  * Hkv lists of n_i cache indexes, ascending, one after another (request i's
  * lists start at Hkv * (n_0 + ... + n_{i-1})).  Of equal scores the lowest index
  * stays first; a NaN counts as -infinity; -0 equals +0.  A request that keeps all
- * its keys lists 0 .. n_i - 1.
+ * its keys lists 0 .. n_i - 1.  Requests of more than 8192 keys most of whose scores
+ * are equal, or nearly, take time with the square of their length (131072 equal
+ * scores: 0.6 ms; spread ones: 0.03 ms).
  * Errors: NULL, the shape errors, PLAN_MISMATCH, WORKSPACE, ARG (a misaligned
  * pointer or plan), HIP.
  */

@@ -253,7 +253,9 @@ __global__ __launch_bounds__(kShortThreads) void evict_select_kernel(EvictArgs a
 //               and lists the scores in it, (key, index) in one word that orders them;
 //   write       every segment finds the last candidate that stays (few: about 1 in
 //               200 where scores spread over a dozen octaves), and from the counts and
-//               the candidates before it the place of its first index.
+//               the candidates before it the place of its first index.  Segments times
+//               candidates: 8 lists of 131072 take 28 us of spread scores, 80 of scores
+//               from 1.0 to 1.2, 575 of equal ones.
 constexpr int kSegThreads = 512;
 constexpr int kSegGroups = kSegKeys / 4 / kSegThreads;
 constexpr int kCandDigit = 10, kCandBins = 1 << kCandDigit;

@@ -124,8 +124,8 @@ __device__ __forceinline__ void add_scores4(const ScoreArgs& a, const ScoreItem&
 // ---------------------------------------------------------------------------
 // One counted row: logits over a key range.  Memory bounds it: 32 rows of 8k to 33k
 // keys, 64/8 heads of 128, with the output: 2.46 GB of keys and values and 0.17 GB of
-// logits in 525 us, 5.0 TB/s where a large copy reaches 4.8 (without the logits'
-// stores 435 us), and 48 us for the join; 622 us together before a block's loads were
+// logits in 527 us, 5.0 TB/s where a copy of 4 GiB reaches 4.8 and the attention launch's
+// reads 6.5 (without the logits' stores 435 us), and 48 us for the join; 622 us together before a block's loads were
 // issued a step ahead and the pieces cut to 1024 keys.  The non-temporal hint changes
 // nothing.
 //
@@ -281,9 +281,9 @@ __device__ __forceinline__ void decode_item(const ScoreArgs& a, const ScoreItem&
     m = mn;
     if constexpr (OUT) {
       // A weight enters the matrix product as three bf16 values, the rounded one and what
-      // that misses twice over: all of its 24 bits.  Memory bounds this loop.  (One
-      // alone put as much error into the output as its own rounding to bf16, two moved
-      // 1 in 500 of the rounded outputs.)
+      // that misses twice over: all of its 24 bits.  Memory bounds this loop, and they
+      // cost no time.  (One alone put as much error into the output as its own rounding
+      // to bf16.)
       u32x4 part[3];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -457,15 +457,16 @@ __device__ __forceinline__ void decode_join_item(const ScoreArgs& a, const Score
 // ---------------------------------------------------------------------------
 // Several rows: both passes.  The issue of matrix and vector instructions bounds them:
 // per 32 x 64 scores a wave runs 16 products (512 cycles), 32 exponentials (half
-// rate), 32 multiply-adds and 30 additions.  Four chunks of 64 to 1024 rows, 267 M
-// scores of 28/4 heads: 84 us and 101 us; of the first pass's cycles the matrix unit is
-// busy 0.35, and 0.46 of those have a vector instruction beside.  Waves of 32 vectors
-// (twice as many resident) take 97 and 108 us.  A wave holds 64 stationary vectors (columns in the
-// first pass, keys in the second) as B operands of the 32x32x16 product and runs
-// the streamed rows (keys, columns) past them in 32-row tiles; NC waves lie side
-// by side over the same rows, 4 / NC one behind the other.  Lane n of a 32x32
-// result owns stationary vector n % 32 and, of the tile, the 16 rows
-// (r & 3) + 8 (r >> 2) + 4 (n / 32): sums over rows stay in the lane to the end.
+// rate), 32 multiply-adds and 32 additions (second pass: 64 and 8).  Four chunks of 64
+// to 1024 rows, 267 M scores of 28/4 heads: 83 us and 104 us; of the first pass's cycles
+// the matrix unit is busy 0.35, and 0.46 of those have a vector instruction beside.
+// Waves of 32 vectors (twice as many resident) took 97 and 108 us when the second pass
+// took 101.  A wave holds 64 stationary vectors (columns in the first pass, keys in the
+// second) as B operands of the 32x32x16 product and runs the streamed rows (keys,
+// columns) past them in 32-row tiles; NC waves lie side by side over the same rows, 4 /
+// NC one behind the other.  Lane n of a 32x32 result owns stationary vector n % 32 and,
+// of the tile, the 16 rows (r & 3) + 8 (r >> 2) + 4 (n / 32): sums over rows stay in the
+// lane to the end.
 __device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
 }
@@ -622,7 +623,7 @@ __device__ __forceinline__ void lse_update(const f32x16& x, float c, int limit, 
 }
 
 // Two tiles a stage where four waves share them (half the barriers; 85.7 us of the
-// chunks above, 82.5 with).  The second pass is slower with two (105 us, 111 with).
+// chunks above, 82.5 with).  The second pass was slower with two (105 us, 111 with).
 template <int D, int NC>
 using LseCfg = ChunkCfg<D, NC, NC == 4 ? 2 : 1>;
 template <int D, int NC>
