@@ -446,8 +446,6 @@ def _handle(state):
     shape = ssa.make_shape(hq, hkv, d, state["num_pages"], state["width"], state.get("scale", 1.0))
     h = {"shape": shape}
     if kind == "pages":
-        h["workspace"] = torch.empty(ssa.pages_workspace_size(len(state["old_len"])),
-                                     dtype=torch.uint8, device="cuda")
         state["handle"] = h
         return h
     c, u = state["c"], state["u"]
@@ -476,7 +474,7 @@ def _own(state):
     if kind == "pages":
         ssa.pages_resize(h["shape"], state["old_len"], state["new_len"], state["block_table"],
                          state["free_pages"], state["page_state"], state["page_state_out"],
-                         state["row_start"], state["slots"], h["workspace"])
+                         state["row_start"], state["slots"])
         return {k: state[k] for k in ("block_table", "free_pages", "page_state_out", "row_start",
                                       "slots")}
     plan = (h["shape"], h["plan"], h["plan_dev"])
