@@ -54,6 +54,67 @@ int ssa_rope_append(const ssa_shape* shape, const void* plan_host, const void* p
  */
 int ssa_rope_table(int32_t max_position, int32_t d, double base, float* out);
 
+/*
+ * Which dims of a head the rotary embedding turns, and in which pairs; the other dims
+ * of a query or key are copied bit for bit.
+ *   layout      SSA_ROPE_HALF: (i, i + rotary_dim / 2), or SSA_ROPE_INTERLEAVED:
+ *               (2 i, 2 i + 1), each for i < rotary_dim / 2, turned by the i-th angle
+ *   rotary_dim  the first dims of a head: a multiple of 16, 16 to D
+ */
+enum { SSA_ROPE_HALF = 0, SSA_ROPE_INTERLEAVED = 1 };
+typedef struct ssa_rope_form {
+  int32_t layout;
+  int32_t rotary_dim;
+} ssa_rope_form;
+
+/*
+ * ssa_rope_append in another form, and at shifted positions where shift_host and
+ * shift_dev (both or neither NULL) are given, as ssa_rope_append_shifted (ssa_evict.h).
+ *   cos_sin  [max_position, rotary_dim] fp32, rows as ssa_rope_append's with rotary_dim
+ *            in D's place (ssa_rope_table, ssa_rope_table_scaled)
+ * SSA_ROPE_HALF with rotary_dim = D gives ssa_rope_append's results bit for bit.
+ * Errors: those of ssa_rope_append_shifted; NULL also for form; ARG also for its values.
+ */
+int ssa_rope_append_as(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                       const ssa_rope_form* form, const uint16_t* qkv, const float* cos_sin,
+                       int32_t max_position, const int32_t* shift_host, const int32_t* shift_dev,
+                       uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
+                       const int32_t* block_table, void* stream);
+
+/*
+ * Angles per position t_i = base^(-2i/d) scaled for contexts past the trained length:
+ *   SSA_ROPE_SCALE_NONE    t_i
+ *   SSA_ROPE_SCALE_LINEAR  t_i / factor
+ *   SSA_ROPE_SCALE_BASE    (base factor^(d / (d - 2)))^(-2i/d): the slowest angle is
+ *                          divided by factor, the fastest not at all (d > 2)
+ *   SSA_ROPE_SCALE_PARTS   with r_i = trained_positions t_i / 2 pi, the turns within the
+ *                          trained length: t_i where r_i >= high, t_i / factor where r_i <=
+ *                          low, in between w t_i + (1 - w) t_i / factor with w =
+ *                          (r_i - low) / (high - low)
+ * magnitude multiplies every cosine and sine (0.1 ln(factor) + 1 where attention is to be
+ * sharpened with the length; 1: nothing).
+ */
+enum {
+  SSA_ROPE_SCALE_NONE = 0,
+  SSA_ROPE_SCALE_LINEAR = 1,
+  SSA_ROPE_SCALE_BASE = 2,
+  SSA_ROPE_SCALE_PARTS = 3
+};
+typedef struct ssa_rope_scaling {
+  int32_t kind;
+  int32_t trained_positions; /* PARTS only: >= 1 */
+  double factor;             /* >= 1 (NONE: not read) */
+  double low, high;          /* PARTS only: 0 <= low < high */
+  double magnitude;          /* > 0 */
+} ssa_rope_scaling;
+
+/*
+ * ssa_rope_table with scaled angles.  Errors: those of ssa_rope_table; SSA_ERR_NULL
+ * (scaling); SSA_ERR_ARG (its values, not finite ones among them).
+ */
+int ssa_rope_table_scaled(int32_t max_position, int32_t d, double base,
+                          const ssa_rope_scaling* scaling, float* out);
+
 /* Epilogues of ssa_linear. */
 enum {
   SSA_EPILOGUE_NONE = 0,     /* out = x W^T                                   [M, N] */

@@ -4,8 +4,8 @@
 // tokens of one request inside one page, at most 16), workgroups of 8 heads
 // each; for a decode request's single row, one workgroup for all its heads.  A
 // rotating workgroup rotates 8 of the segment's query and key heads
-// (rotate-half pairs (i, i + D/2), cos/sin from the position's row of the
-// table) and writes the queries to q_out and the keys to their slots of the
+// (pairs (i, i + D/2), or as a ssa_rope_form says; cos/sin from the position's
+// row of the table) and writes the queries to q_out and the keys to their slots of the
 // key page (slot-major rows); a value workgroup stages 8 value heads' rows in
 // LDS and writes them to the dim-major value page as 16-byte half rows (8
 // slots of one dim), the layout ssa_mixed_attention reads.  Each thread issues
@@ -47,6 +47,24 @@ __device__ __forceinline__ void rotate8(u32x4 x1, u32x4 x2, const float* cs, int
   }
 }
 
+// Rotate 8 neighbouring pairs (2 i, 2 i + 1): dims 16 u .. 16 u + 15 of one head; cs: the
+// cosines of the first of them on, the sines `half` further.
+__device__ __forceinline__ void rotate8_interleaved(u32x4 x1, u32x4 x2, const float* cs, int half,
+                                                   u32x4* o1, u32x4* o2) {
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const f32x4 c = *reinterpret_cast<const f32x4*>(cs + 4 * n);
+    const f32x4 s = *reinterpret_cast<const f32x4*>(cs + half + 4 * n);
+    const u32x4 x = n ? x2 : x1;
+    u32x4* o = n ? o2 : o1;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float a = bf16_lo(x[w]), b = bf16_hi(x[w]);
+      (*o)[w] = pack2(a * c[w] - b * s[w], b * c[w] + a * s[w]);
+    }
+  }
+}
+
 struct RopeArgs {
   const uint8_t* plan;
   uint64_t hash;
@@ -62,11 +80,45 @@ struct RopeArgs {
   int workgroups;
   const int32_t* shift;  // position minus cache index of each request, or null (all zero)
   int max_position;
+  int rotary;  // dims of a head that turn: the table's row (kWhole: D)
 };
 
 // Heads per workgroup of a grouped segment: group y < rot_groups rotates
 // query/key heads 8 y .. 8 y + 7 (of the Hq + Hkv rotated ones); the others copy
 // value heads.
+// Which dims of a head turn, in which pairs.  A head is D / 16 units of 16 dims, two
+// 16-byte pieces; the first rotary / 16 of them turn, the others are copied.
+enum RopeForm {
+  kWhole,      // pairs (i, i + D/2) of the whole head
+  kHalf,     // pairs (i, i + rotary/2) of the first `rotary` dims
+  kInterleaved  // pairs (2 i, 2 i + 1) of the first `rotary` dims
+};
+template <int D, int FORM>
+struct Unit {
+  int first, second;  // dims where its pieces begin
+  bool turns;
+  int at;  // its first pair's place in the table's row
+  __device__ __forceinline__ Unit(int u, int rotary)
+      : first(u * 16), second(u * 16 + 8), turns(FORM == kWhole || u < rotary / 16), at(u * 8) {
+    if (FORM == kWhole || (FORM == kHalf && turns)) {
+      first = u * 8;
+      second = u * 8 + (FORM == kWhole ? D : rotary) / 2;
+    }
+  }
+  __device__ __forceinline__ void rotate(u32x4 x1, u32x4 x2, const float* cs, int rotary, u32x4* o1,
+                                         u32x4* o2) const {
+    const int half = (FORM == kWhole ? D : rotary) / 2;
+    if (!turns) {
+      *o1 = x1;
+      *o2 = x2;
+    } else if (FORM == kInterleaved) {
+      rotate8_interleaved(x1, x2, cs + at, half, o1, o2);
+    } else {
+      rotate8(x1, x2, cs, half, at, o1, o2);
+    }
+  }
+};
+
 constexpr int kHeadGroup = 8;
 constexpr int kSingleMaxHeads = 16 * kHeadGroup;  // rotated heads of one row per workgroup
 // Workgroups go in rows of this many: one row of more than 2^24 workgroups would
@@ -81,9 +133,10 @@ constexpr int kGridRow = 1 << 16;
 // 9.3).  Segment-major ids put a segment's head groups, which share its cache
 // lines of the table and the rows, side by side (2048 chunk tokens, plan on the
 // device: 13.6 -> 10.5 us; bytes at the copy rate 10).
-template <int D>
+template <int D, int FORM>
 __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) {
-  constexpr int HALF = D / 2, UPH = HALF / 8;     // 8-pair units per head
+  using U = Unit<D, FORM>;
+  constexpr int UPH = D / 16;                     // 8-pair units per head
   constexpr int HG = kHeadGroup;
   constexpr int RU = 16 * HG * UPH / kLayerThreads;  // rotation units per thread
   constexpr int VU = 16 * HG * (D / 8) / kLayerThreads;  // value chunks per thread
@@ -102,6 +155,7 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
   if (hdr->magic != kPlanMagic || hdr->hash != a.hash) return;
   const int n = sg.n, slot0 = sg.pos0 % 16, tid = threadIdx.x;
   const size_t stride = (size_t)(a.hq + 2 * a.hkv) * D;
+  const int table_row = FORM == kWhole ? D : a.rotary;
   const size_t pb = (size_t)a.bt[(size_t)sg.req * a.maxp + sg.pos0 / 16] * a.hkv * 16 * D;
   // the table's row of the segment's first position; the host has checked its own
   // copy of the shifts, and the bound keeps another one inside the table
@@ -117,9 +171,10 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
     for (int j = 0; j < RU; ++j) {
       const int idx = tid + j * kLayerThreads;
       if (idx < nu) {
-        const uint16_t* src = row + (size_t)(idx / UPH) * D + (idx % UPH) * 8;
-        x1[j] = ld16(src);
-        x2[j] = ld16(src + HALF);
+        const U u(idx % UPH, a.rotary);
+        const uint16_t* src = row + (size_t)(idx / UPH) * D;
+        x1[j] = ld16(src + u.first);
+        x2[j] = ld16(src + u.second);
       }
       if (idx < nv) v[j] = ld16(row + (size_t)nrot * D + idx * 8);
     }
@@ -127,13 +182,14 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
     for (int j = 0; j < RU; ++j) {
       const int idx = tid + j * kLayerThreads;
       if (idx < nu) {
-        const int h = idx / UPH, i = (idx % UPH) * 8;
+        const int h = idx / UPH;
+        const U u(idx % UPH, a.rotary);
         u32x4 o1, o2;
-        rotate8(x1[j], x2[j], a.cos_sin + (size_t)at0 * D, HALF, i, &o1, &o2);
+        u.rotate(x1[j], x2[j], a.cos_sin + (size_t)at0 * table_row, a.rotary, &o1, &o2);
         uint16_t* dst = h < a.hq ? a.q_out + ((size_t)sg.row0 * a.hq + h) * D
                                  : a.kc + pb + (size_t)(h - a.hq) * 16 * D + (size_t)slot0 * D;
-        st16(dst + i, o1);
-        st16(dst + HALF + i, o2);
+        st16(dst + u.first, o1);
+        st16(dst + u.second, o2);
       }
       if (idx < nv) {
         uint16_t* dst = a.vc + pb + (size_t)idx * 8 * 16 + slot0;
@@ -157,23 +213,25 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
       const int idx = tid + j * kLayerThreads;
       if (idx >= nu) continue;
       const int r = idx / (nh * UPH), rem = idx % (nh * UPH);
-      const int h = h0 + rem / UPH, i = (rem % UPH) * 8;
+      const int h = h0 + rem / UPH;
+      const U u(rem % UPH, a.rotary);
       const uint16_t* src = a.qkv + (size_t)(sg.row0 + r) * stride + (size_t)h * D;
-      x1[j] = ld16(src + i);
-      x2[j] = ld16(src + HALF + i);
+      x1[j] = ld16(src + u.first);
+      x2[j] = ld16(src + u.second);
     }
 #pragma unroll
     for (int j = 0; j < RU; ++j) {
       const int idx = tid + j * kLayerThreads;
       if (idx >= nu) continue;
       const int r = idx / (nh * UPH), rem = idx % (nh * UPH);
-      const int h = h0 + rem / UPH, i = (rem % UPH) * 8;
+      const int h = h0 + rem / UPH;
+      const U u(rem % UPH, a.rotary);
       u32x4 o1, o2;
-      rotate8(x1[j], x2[j], a.cos_sin + (size_t)(at0 + r) * D, HALF, i, &o1, &o2);
+      u.rotate(x1[j], x2[j], a.cos_sin + (size_t)(at0 + r) * table_row, a.rotary, &o1, &o2);
       uint16_t* dst = h < a.hq ? a.q_out + ((size_t)(sg.row0 + r) * a.hq + h) * D
                                : a.kc + pb + (size_t)(h - a.hq) * 16 * D + (size_t)(slot0 + r) * D;
-      st16(dst + i, o1);
-      st16(dst + HALF + i, o2);
+      st16(dst + u.first, o1);
+      st16(dst + u.second, o2);
     }
     return;
   }
@@ -225,13 +283,31 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
 
 namespace {
 
+bool rope_form_ok(const ssa_rope_form& f, int32_t head_dim) {
+  return (f.layout == SSA_ROPE_HALF || f.layout == SSA_ROPE_INTERLEAVED) && f.rotary_dim >= 16 &&
+         f.rotary_dim <= head_dim && f.rotary_dim % 16 == 0;
+}
+
+template <int D>
+void launch_rope(RopeForm form, dim3 grid, hipStream_t stream, const RopeArgs& a) {
+  const dim3 block(kLayerThreads);
+  if (form == kInterleaved)
+    hipLaunchKernelGGL((rope_append_kernel<D, kInterleaved>), grid, block, 0, stream, a);
+  else if (form == kHalf)
+    hipLaunchKernelGGL((rope_append_kernel<D, kHalf>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((rope_append_kernel<D, kWhole>), grid, block, 0, stream, a);
+}
+
 int rope_append(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                 const uint16_t* qkv, const float* cos_sin, int32_t max_position,
                 const int32_t* shift_host, const int32_t* shift_dev, uint16_t* q_out,
-                uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table, void* stream) {
+                uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table, void* stream,
+                const ssa_rope_form* as = nullptr) {
   const PlanHeader* h = nullptr;
   int rc = check_plan(shape, plan_host, &h);
   if (rc) return rc;
+  if (as && !rope_form_ok(*as, h->head_dim)) return SSA_ERR_ARG;
   if (!plan_dev) return SSA_ERR_NULL;
   const ReqEntry* reqs = reinterpret_cast<const ReqEntry*>(
       static_cast<const uint8_t*>(plan_host) + h->off_reqs);
@@ -253,14 +329,15 @@ int rope_append(const ssa_shape* shape, const void* plan_host, const void* plan_
   if (wgs > INT32_MAX) return SSA_ERR_ARG;
   RopeArgs a{static_cast<const uint8_t*>(plan_dev), h->hash, h->off_segments, qkv, cos_sin,
              q_out, k_cache, v_cache, block_table, h->hq, h->hkv, h->max_pages_per_req, grouped,
-             (int32_t)wgs, shift_dev, max_position};
+             (int32_t)wgs, shift_dev, max_position, as ? as->rotary_dim : h->head_dim};
   const dim3 grid(wgs < kGridRow ? wgs : kGridRow, (wgs + kGridRow - 1) / kGridRow);
+  const RopeForm form = as && as->layout == SSA_ROPE_INTERLEAVED ? kInterleaved
+                        : a.rotary < h->head_dim               ? kHalf
+                                                               : kWhole;
   if (h->head_dim == 128)
-    hipLaunchKernelGGL(rope_append_kernel<128>, grid, dim3(kLayerThreads), 0,
-                       static_cast<hipStream_t>(stream), a);
+    launch_rope<128>(form, grid, static_cast<hipStream_t>(stream), a);
   else
-    hipLaunchKernelGGL(rope_append_kernel<64>, grid, dim3(kLayerThreads), 0,
-                       static_cast<hipStream_t>(stream), a);
+    launch_rope<64>(form, grid, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
 }
 
@@ -284,6 +361,16 @@ int ssa_rope_append_shifted(const ssa_shape* shape, const void* plan_host, const
   if (!shift_host || !shift_dev) return SSA_ERR_NULL;
   return rope_append(shape, plan_host, plan_dev, qkv, cos_sin, max_position, shift_host, shift_dev,
                      q_out, k_cache, v_cache, block_table, stream);
+}
+
+int ssa_rope_append_as(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                       const ssa_rope_form* form, const uint16_t* qkv, const float* cos_sin,
+                       int32_t max_position, const int32_t* shift_host, const int32_t* shift_dev,
+                       uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
+                       const int32_t* block_table, void* stream) {
+  if (!form || !shift_host != !shift_dev) return SSA_ERR_NULL;
+  return rope_append(shape, plan_host, plan_dev, qkv, cos_sin, max_position, shift_host, shift_dev,
+                     q_out, k_cache, v_cache, block_table, stream, form);
 }
 
 }  // extern "C"

@@ -20,6 +20,8 @@ int check_plan(const ssa_shape* s, const void* plan_host, const PlanHeader** out
 namespace {
 using namespace ssa;
 
+constexpr double kPi = 3.14159265358979323846;
+
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }
 
 // Byte offsets of the regions of the layer workspace.  Where the split tickets
@@ -163,15 +165,42 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
 extern "C" {
 
 int ssa_rope_table(int32_t max_position, int32_t d, double base, float* out) {
-  if (!out) return SSA_ERR_NULL;
+  const ssa_rope_scaling none = {SSA_ROPE_SCALE_NONE, 0, 1.0, 0.0, 0.0, 1.0};
+  return ssa_rope_table_scaled(max_position, d, base, &none, out);
+}
+
+int ssa_rope_table_scaled(int32_t max_position, int32_t d, double base,
+                          const ssa_rope_scaling* scaling, float* out) {
+  if (!out || !scaling) return SSA_ERR_NULL;
   if (max_position < 1 || d < 2 || d % 2 || !std::isfinite(base) || !(base > 1.0)) return SSA_ERR_ARG;
+  const ssa_rope_scaling& s = *scaling;
+  if (s.kind < SSA_ROPE_SCALE_NONE || s.kind > SSA_ROPE_SCALE_PARTS || !std::isfinite(s.magnitude) ||
+      !(s.magnitude > 0.0))
+    return SSA_ERR_ARG;
+  if (s.kind != SSA_ROPE_SCALE_NONE && (!std::isfinite(s.factor) || !(s.factor >= 1.0)))
+    return SSA_ERR_ARG;
+  if (s.kind == SSA_ROPE_SCALE_BASE) {
+    if (d <= 2) return SSA_ERR_ARG;
+    base *= std::pow(s.factor, (double)d / (d - 2));
+    if (!std::isfinite(base)) return SSA_ERR_ARG;
+  }
+  if (s.kind == SSA_ROPE_SCALE_PARTS &&
+      (s.trained_positions < 1 || !std::isfinite(s.high) || !(s.low >= 0.0) || !(s.low < s.high)))
+    return SSA_ERR_ARG;
   const int half = d / 2;
   for (int i = 0; i < half; ++i) {
-    const double t = std::pow(base, -2.0 * i / d);
+    double t = std::pow(base, -2.0 * i / d);
+    if (s.kind == SSA_ROPE_SCALE_LINEAR) {
+      t /= s.factor;
+    } else if (s.kind == SSA_ROPE_SCALE_PARTS) {
+      const double turns = s.trained_positions * t / (2.0 * kPi);
+      const double w = std::min(1.0, std::max(0.0, (turns - s.low) / (s.high - s.low)));
+      t = w * t + (1.0 - w) * t / s.factor;
+    }
     for (int64_t p = 0; p < max_position; ++p) {
       const double a = (double)p * t;
-      out[p * d + i] = (float)std::cos(a);
-      out[p * d + half + i] = (float)std::sin(a);
+      out[p * d + i] = (float)(s.magnitude * std::cos(a));
+      out[p * d + half + i] = (float)(s.magnitude * std::sin(a));
     }
   }
   return SSA_OK;

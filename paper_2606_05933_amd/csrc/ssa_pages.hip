@@ -1,0 +1,149 @@
+// HIP kernel for gfx950 of ssa_pages_resize (include/ssa_pages.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "../../include/ssa_pages.h"
+
+namespace ssa {
+int validate_shape(const ssa_shape* s);
+}
+
+namespace {
+
+constexpr int kPage = SSA_PAGE_SIZE;
+constexpr int kMaxReqs = 65536;
+constexpr int kMaxTokens = 1 << 30;  // of a request
+constexpr int kWavesPerGroup = 4;
+
+struct PagesArgs {
+  int32_t n, pieces;
+  int32_t num_pages, maxp, most;  // most: of a request's tokens
+  const int32_t* old_len;
+  const int32_t* new_len;
+  int32_t* table;
+  int32_t* ring;
+  const int32_t* state;
+  int32_t* state_out;
+  int32_t* row_start;
+  int64_t* slots;
+  int64_t max_rows;
+};
+
+struct Sums {
+  int64_t taken, given, rows;
+};
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor((long long)x, o, 64);
+  return x;
+}
+__device__ __forceinline__ int pages_of(int len) { return (len + kPage - 1) / kPage; }
+
+// A wave takes one piece of one request.  It adds up what the requests take, give and add
+// itself, those before its own apart: one launch, and no workgroup waits for another.
+// The lengths are read by every wave (64 requests 512 bytes), so latency bounds it as long
+// as the requests are some thousands: the lengths, the state, the ring or the table.
+__global__ __launch_bounds__(64 * kWavesPerGroup) void pages_resize_kernel(PagesArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * kWavesPerGroup +
+                       __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int req = (int)(unit / a.pieces), piece = (int)(unit % a.pieces);
+  if (req > 0 && req >= a.n) return;  // no requests: one wave copies the state
+  const int head = a.state[0], count = a.state[1];
+  Sums before{0, 0, 0}, all{0, 0, 0};
+  bool bad = false;
+  for (int i = lane; i < a.n; i += 64) {
+    const int from = a.old_len[i], to = a.new_len[i];
+    if (from < 0 || to < 0 || from > a.most || to > a.most) {
+      bad = true;
+      continue;
+    }
+    const int p = pages_of(from), q = pages_of(to);
+    all.taken += max(q - p, 0);
+    all.given += max(p - q, 0);
+    all.rows += max(to - from, 0);
+    if (i < req) {
+      before.taken += max(q - p, 0);
+      before.given += max(p - q, 0);
+      before.rows += max(to - from, 0);
+    }
+  }
+  all = Sums{wave_sum(all.taken), wave_sum(all.given), wave_sum(all.rows)};
+  int status = __any(bad) ? SSA_PAGES_LENGTH : 0;
+  int64_t missing = 0;
+  if (head < 0 || head >= a.num_pages || count < 0 || count > a.num_pages) {
+    status |= SSA_PAGES_RING;
+  } else if (!status) {
+    if (all.taken > count) {
+      status |= SSA_PAGES_SHORT;
+      missing = all.taken - count;
+    }
+    if (count + all.given > a.num_pages) status |= SSA_PAGES_RING;
+  }
+  if (all.rows > (a.slots ? a.max_rows : INT32_MAX)) status |= SSA_PAGES_ROWS;
+  if (unit == 0 && lane == 0) {
+    a.state_out[0] = status ? head : (int)((head + all.taken) % a.num_pages);
+    a.state_out[1] = status ? count : (int)(count - all.taken + all.given);
+    a.state_out[2] = status;
+    a.state_out[3] = (int)(missing < INT32_MAX ? missing : INT32_MAX);
+    if (!status && a.row_start) a.row_start[0] = 0;
+  }
+  if (status || req >= a.n) return;
+  before = Sums{wave_sum(before.taken), wave_sum(before.given), wave_sum(before.rows)};
+  const int from = a.old_len[req], to = a.new_len[req];
+  const int p = pages_of(from), q = pages_of(to);
+  int32_t* row = a.table + (size_t)req * a.maxp;
+  if (piece == 0 && lane == 0 && a.row_start)
+    a.row_start[req + 1] = (int32_t)(before.rows + max(to - from, 0));
+  // entry k >= p takes ring entry (head + before.taken + k - p) mod num_pages
+  auto wrapped = [&](int64_t at) { return (int)(at < a.num_pages ? at : at - a.num_pages); };
+  const int64_t take0 = ((int64_t)head + before.taken) % a.num_pages;
+  const int64_t give0 = ((int64_t)head + count + before.given) % a.num_pages;
+  const int step = a.pieces * 64, mine = piece * 64 + lane;
+  for (int k = p + mine; k < q; k += step) row[k] = a.ring[wrapped(take0 + (k - p))];
+  for (int k = q + mine; k < p; k += step) a.ring[wrapped(give0 + (k - q))] = row[k];
+  if (!a.slots) return;
+  int64_t* slots = a.slots + before.rows;
+  for (int64_t t = (int64_t)from + mine; t < to; t += step) {
+    const int k = (int)(t / kPage);
+    const int page = k < p ? row[k] : a.ring[wrapped(take0 + (k - p))];
+    slots[t - from] = (int64_t)page * kPage + t % kPage;
+  }
+}
+
+}  // namespace
+
+extern "C" int ssa_pages_resize(const ssa_shape* shape, int32_t num_reqs, const int32_t* old_len,
+                                const int32_t* new_len, int32_t* block_table, int32_t* free_pages,
+                                const int32_t* state, int32_t* state_out, int32_t* row_start,
+                                int64_t* slots, int64_t max_rows, void* stream) {
+  const int rc = ssa::validate_shape(shape);
+  if (rc) return rc;
+  if (num_reqs < 0 || num_reqs > kMaxReqs) return SSA_ERR_LENGTH;
+  if (!state || !state_out) return SSA_ERR_NULL;
+  if (max_rows < 0 || std::max(state, (const int32_t*)state_out) < std::min(state, (const int32_t*)state_out) + 4)
+    return SSA_ERR_ARG;
+  if (num_reqs > 0 && (!old_len || !new_len || !block_table || !free_pages)) return SSA_ERR_NULL;
+  PagesArgs a{};
+  a.n = num_reqs;
+  a.num_pages = shape->num_pages;
+  a.maxp = shape->max_pages_per_req;
+  a.most = std::min(shape->max_pages_per_req, kMaxTokens / kPage) * kPage;
+  a.old_len = old_len;
+  a.new_len = new_len;
+  a.table = block_table;
+  a.ring = free_pages;
+  a.state = state;
+  a.state_out = state_out;
+  a.row_start = row_start;
+  a.slots = slots;
+  a.max_rows = max_rows;
+  a.pieces = 8;
+  const int64_t units = (int64_t)std::max(1, num_reqs) * a.pieces;
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(pages_resize_kernel, dim3((units + kWavesPerGroup - 1) / kWavesPerGroup),
+                     dim3(64 * kWavesPerGroup), 0, static_cast<hipStream_t>(stream), a);
+  return hipGetLastError() == hipSuccess ? SSA_OK : SSA_ERR_HIP;
+}

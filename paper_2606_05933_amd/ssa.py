@@ -94,6 +94,21 @@ class SsaLayerEviction(ctypes.Structure):
         ("shift_dev", ctypes.c_void_p), ("decay", ctypes.c_float)]
 
 
+class SsaRopeForm(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32)]
+
+
+class SsaRopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("trained_positions", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
+
+
+class SsaSparseConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("block_keys", "top_blocks", "sink_blocks",
+                                              "recent_blocks")]
+
+
 class SsaLinearPlanInfo(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_m", "tile_n", "threads", "tiles_m", "tiles_n",
                                               "splits")]
@@ -215,6 +230,18 @@ def _load():
                                                P(SsaLayerEviction), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ssa_rope_append_shifted.argtypes = [P(SsaShape), vp, vp, vp, vp, i32, vp, vp, vp, vp, vp,
                                             vp, vp]
+    lib.ssa_rope_append_as.argtypes = [P(SsaShape), vp, vp, P(SsaRopeForm), vp, vp, i32, vp, vp, vp,
+                                       vp, vp, vp, vp]
+    lib.ssa_rope_table_scaled.argtypes = [i32, i32, ctypes.c_double, P(SsaRopeScaling), vp]
+    lib.ssa_pages_resize.argtypes = [P(SsaShape), i32, vp, vp, vp, vp, vp, vp, vp, vp,
+                                     ctypes.c_int64, vp]
+    lib.ssa_block_summary.argtypes = [P(SsaShape), vp, vp, i32, vp, vp, vp, vp]
+    lib.ssa_sparse_plan_size.argtypes = [P(SsaShape), P(SsaSparseConfig), vp, vp, i32, P(sz), P(sz),
+                                         ip]
+    lib.ssa_sparse_plan.argtypes = [P(SsaShape), P(SsaSparseConfig), vp, vp, i32, vp, sz]
+    lib.ssa_block_scores.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp]
+    lib.ssa_block_select.argtypes = [P(SsaShape), vp, vp, vp, vp, vp]
+    lib.ssa_sparse_attention.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ssa_priority_sort.argtypes = [P(SsaCandidate), i32, ctypes.c_double, ctypes.c_double,
                                       ctypes.c_double, ip]
     lib.ssa_batch_constructor.argtypes = [P(SsaPredictor), ip, i32, P(SsaCandidate), i32, i32,
@@ -242,7 +269,10 @@ EXPORTED = ("ssa_status_string", "ssa_plan_size", "ssa_plan", "ssa_check_block_t
             "ssa_probe_hbm_gather", "ssa_probe_mfma_bf16", "ssa_score_plan_size",
             "ssa_score_plan", "ssa_key_scores", "ssa_decode_scored", "ssa_evict_plan_size",
             "ssa_evict_plan", "ssa_evict_select", "ssa_evict_compact", "ssa_check_evict_tables",
-            "ssa_rope_append_shifted", "ssa_layer_forward_evicting")
+            "ssa_rope_append_shifted", "ssa_layer_forward_evicting", "ssa_rope_append_as",
+            "ssa_rope_table_scaled", "ssa_pages_resize", "ssa_block_summary",
+            "ssa_sparse_plan_size", "ssa_sparse_plan", "ssa_block_scores", "ssa_block_select",
+            "ssa_sparse_attention")
 
 EPILOGUE_NONE, EPILOGUE_RESIDUAL, EPILOGUE_SWIGLU = 0, 1, 2
 
@@ -1148,3 +1178,176 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
         check.stream(stream))
     if rc:
         raise SsaError(rc, what)
+
+
+# Rotary forms (include/ssa_layer.h), block tables on the device (include/ssa_pages.h) and
+# attention over selected blocks (include/ssa_sparse.h).
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+# ssa_pages_resize's status bits
+PAGES_SHORT, PAGES_LENGTH, PAGES_ROWS, PAGES_RING = 1, 2, 4, 8
+
+
+def _choice(name, value, choices):
+    if value not in choices:
+        raise ValueError(f"{name} {value!r}: one of {', '.join(choices)} expected")
+    return choices[value]
+
+
+def rope_cos_sin_scaled(max_position: int, d: int, base: float = 500000.0, scaling: str = "none",
+                        factor: float = 1.0, trained_positions: int = 0, low: float = 0.0,
+                        high: float = 0.0, magnitude: float = 1.0) -> np.ndarray:
+    """ssa_rope_table_scaled: the rotary table (fp32 [max_position, d], host) of angles
+    scaled for contexts past the trained length ("none", "linear", "base" or "parts")."""
+    if max_position < 1 or d < 2:
+        raise SsaError(SSA_ERR_ARG, "ssa_rope_table_scaled")
+    s = SsaRopeScaling(_choice("scaling", scaling, ROPE_SCALINGS), int(trained_positions),
+                       float(factor), float(low), float(high), float(magnitude))
+    out = np.empty((max_position, d), dtype=np.float32)
+    _check(LIB.ssa_rope_table_scaled(max_position, d, float(base), ctypes.byref(s), _address(out)),
+           "ssa_rope_table_scaled")
+    return out
+
+
+def rope_append_as(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_cache, v_cache,
+                   block_table, layout: str = "half", rotary_dim: int | None = None,
+                   shift_host=None, shift_dev=None, stream=None):
+    """ssa_rope_append_as: rope_append that turns the first rotary_dim dims (None: all) of
+    each query and key head in pairs of its halves ("half") or of neighbours
+    ("interleaved"), at shifted positions where shifts are given."""
+    what = "ssa_rope_append_as"
+    at, h = _header(plan_host, _PLAN_MAGIC, what)
+    check = _Buffers()
+    n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
+    d, hq, hkv = shape.head_dim, shape.num_q_heads, shape.num_kv_heads
+    rotary = d if rotary_dim is None else int(rotary_dim)
+    if rotary < 1:
+        raise SsaError(SSA_ERR_ARG, what)
+    form = SsaRopeForm(_choice("layout", layout, ROPE_LAYOUTS), rotary)
+    pool = shape.num_pages * hkv * shape.page_size * d
+    if shift_host is not None:
+        shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
+        if shift_host.size != n:
+            raise ValueError(f"{shift_host.size} shifts for {n} requests")
+    rc = LIB.ssa_rope_append_as(
+        shape, at, check.plan(plan_dev, plan_host), form,
+        check("qkv", qkv, tokens * (hq + 2 * hkv) * d, 2), check("cos_sin", cos_sin, rotary, 4),
+        cos_sin.numel() // rotary, _address(shift_host), check("shift_dev", shift_dev, n, 4),
+        check("q_out", q_out, tokens * hq * d, 2), check("k_cache", k_cache, pool, 2),
+        check("v_cache", v_cache, pool, 2),
+        check("block_table", block_table, n * shape.max_pages_per_req, 4), check.stream(stream))
+    if rc:
+        raise SsaError(rc, what)
+
+
+def pages_resize(shape: SsaShape, old_len, new_len, block_table, free_pages, state, state_out,
+                 row_start=None, slots=None, stream=None):
+    """ssa_pages_resize: requests go from old_len to new_len cached tokens (int32 [n] on the
+    device); block_table (int32 [n, max_pages_per_req]) takes pages of the ring free_pages
+    (int32 [num_pages]) or gives them back, row_start (int32 [n + 1]) and slots (int64, one
+    for each new row it has room for) are the new tokens' rows and slots.  state is int32
+    [4] (head, count, status, missing), state_out another one."""
+    check = _Buffers()
+    n = 0 if old_len is None else old_len.numel()
+    if new_len is not None and new_len.numel() != n:
+        raise ValueError("old_len and new_len differ in length")
+    rc = LIB.ssa_pages_resize(
+        shape, n, check("old_len", old_len, n, 4), check("new_len", new_len, n, 4),
+        check("block_table", block_table, n * shape.max_pages_per_req, 4),
+        check("free_pages", free_pages, shape.num_pages, 4), check("state", state, 4, 4),
+        check("state_out", state_out, 4, 4), check("row_start", row_start, n + 1, 4),
+        check("slots", slots, 0, 8), 0 if slots is None else slots.numel(), check.stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_pages_resize")
+
+
+def block_summary(shape: SsaShape, plan_host, plan_dev, block_keys: int, k_cache, block_table,
+                  summary, stream=None):
+    """ssa_block_summary: the highest and lowest values (bf16 [num_pages, Hkv, 2, D], in
+    the page where a block begins) of the blocks that the plan's new tokens lie in."""
+    at, h = _header(plan_host, _PLAN_MAGIC, "ssa_block_summary")
+    check = _Buffers()
+    rows = shape.num_pages * shape.num_kv_heads * shape.head_dim
+    rc = LIB.ssa_block_summary(
+        shape, at, check.plan(plan_dev, plan_host), block_keys,
+        check("k_cache", k_cache, rows * shape.page_size, 2),
+        check("block_table", block_table, h[_PLAN_REQS] * shape.max_pages_per_req, 4),
+        check("summary", summary, rows * 2, 2), check.stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_block_summary")
+
+
+def sparse_plan(shape: SsaShape, q_len, ctx_len, block_keys: int, top_blocks: int,
+                sink_blocks: int = 1, recent_blocks: int = 1, out=None):
+    """Plan blob of block_scores, block_select and sparse_attention (a host buffer: numpy
+    uint8, or written into `out`), the workspace's bytes and the scores' max_blocks."""
+    ql, pq = _lens(q_len)
+    cl, pc = _lens(ctx_len)
+    if ql.shape != cl.shape:
+        raise ValueError("q_len and ctx_len differ in length")
+    cfg = SsaSparseConfig(int(block_keys), int(top_blocks), int(sink_blocks), int(recent_blocks))
+    pb, wb, mb = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_int32()
+    _check(LIB.ssa_sparse_plan_size(ctypes.byref(shape), ctypes.byref(cfg), pq, pc, ql.shape[0],
+                                    ctypes.byref(pb), ctypes.byref(wb), ctypes.byref(mb)),
+           "ssa_sparse_plan_size")
+    out, ptr, cap = _plan_buffer(out, pb.value)
+    _check(LIB.ssa_sparse_plan(ctypes.byref(shape), ctypes.byref(cfg), pq, pc, ql.shape[0], ptr,
+                               cap), "ssa_sparse_plan")
+    return out, wb.value, mb.value
+
+
+# The sparse plan's magic and the int32 words of its header that the wrappers read
+# (ssa_sparse_format.h).
+_SPARSE_MAGIC = 0x31505353
+_SPARSE_REQS, _SPARSE_TOKENS, _SPARSE_TOP, _SPARSE_MAX_BLOCKS = 4, 5, 13, 16
+
+
+def block_scores(shape: SsaShape, plan_host, plan_dev, q, summary, block_table, scores,
+                 stream=None):
+    """ssa_block_scores: per new row, kv head and block (fp32 [T, Hkv, max_blocks]) the
+    highest bound of the block's logits over the kv head's query heads."""
+    at, h = _header(plan_host, _SPARSE_MAGIC, "ssa_block_scores")
+    check = _Buffers()
+    tokens, hkv, d = h[_SPARSE_TOKENS], shape.num_kv_heads, shape.head_dim
+    rc = LIB.ssa_block_scores(
+        shape, at, check.plan(plan_dev, plan_host), check("q", q, tokens * shape.num_q_heads * d, 2),
+        check("summary", summary, shape.num_pages * hkv * 2 * d, 2),
+        check("block_table", block_table, h[_SPARSE_REQS] * shape.max_pages_per_req, 4),
+        check("scores", scores, tokens * hkv * h[_SPARSE_MAX_BLOCKS], 4), check.stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_block_scores")
+
+
+def block_select(shape: SsaShape, plan_host, plan_dev, scores, blocks, stream=None):
+    """ssa_block_select: per new row and kv head the blocks to look at (int32 [T, Hkv,
+    top_blocks], ascending, -1 behind them)."""
+    at, h = _header(plan_host, _SPARSE_MAGIC, "ssa_block_select")
+    check = _Buffers()
+    lists = h[_SPARSE_TOKENS] * shape.num_kv_heads
+    rc = LIB.ssa_block_select(
+        shape, at, check.plan(plan_dev, plan_host),
+        check("scores", scores, lists * h[_SPARSE_MAX_BLOCKS], 4),
+        check("blocks", blocks, lists * h[_SPARSE_TOP], 4), check.stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_block_select")
+
+
+def sparse_attention(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, block_table,
+                     blocks, out, workspace, stream=None):
+    """ssa_sparse_attention: attention of every new row over the keys of the blocks that
+    its list names for each kv head (out as ssa_mixed_attention's).  The workspace has to
+    be zero before its first use."""
+    at, h = _header(plan_host, _SPARSE_MAGIC, "ssa_sparse_attention")
+    check = _Buffers()
+    ws, n = check.workspace(workspace)
+    tokens, hkv, d = h[_SPARSE_TOKENS], shape.num_kv_heads, shape.head_dim
+    rows, pool = tokens * shape.num_q_heads * d, shape.num_pages * hkv * shape.page_size * d
+    rc = LIB.ssa_sparse_attention(
+        shape, at, check.plan(plan_dev, plan_host), check("q", q, rows, 2),
+        check("k_cache", k_cache, pool, 2), check("v_cache", v_cache, pool, 2),
+        check("block_table", block_table, h[_SPARSE_REQS] * shape.max_pages_per_req, 4),
+        check("blocks", blocks, tokens * hkv * h[_SPARSE_TOP], 4), check("out", out, rows, 2),
+        ws, n, check.stream(stream))
+    if rc:
+        raise SsaError(rc, "ssa_sparse_attention")

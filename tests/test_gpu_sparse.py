@@ -1,0 +1,437 @@
+"""GPU parity of block summaries, scores, selection and attention over selected blocks
+(include/ssa_sparse.h) with the float64 oracle (oracle/sparse.py).
+
+Bars, from the arithmetic:
+* summaries, lists: bit for bit.
+* scores: a sum of 2 D products of two bf16 values (exact in fp32), each addition off by
+  at most 2^-24 of a partial sum, which is at most the sum A of the terms' magnitudes:
+      |err| <= 2 D 2^-24 A.
+* attention: logits of D products, so off by D 2^-24 A; the exponents' fma and the
+  exponential add a few 2^-24 of their argument (<= 2 A log2 e) and value; sums of
+  positive terms at most 2^-24 for each of the L / 32 + 128 links of their longest chain; a
+  weight enters the products whole (three bf16 parts, 2^-24); the result is rounded to
+  bf16:
+      |err| <= 2^-8 |ref| + 2^-24 (2 (2 D A + 8 A + 2 L / 32 + 256) + 1) sum |w v|.
+"""
+import numpy as np
+import pytest
+
+from test_gpu_evict import HEADS, dev, say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch_dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    torch.cuda.set_device(0)
+    return torch
+
+
+def bits(t):
+    """uint16 numpy array of a bf16 tensor."""
+    import torch
+    return t.view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+class Sparse:
+    """A batch on the device, its new rows appended, with its plans."""
+
+    def __init__(self, torch, heads, c, u, block, top, sink=1, recent=1, seed=0, plan="device",
+                 scale=None):
+        from oracle import oracle
+        from paper_2606_05933_amd import ssa, workload
+        self.torch, self.ssa, self.block = torch, ssa, block
+        self.top, self.sink, self.recent = top, sink, recent
+        self.b = b = workload.make_batch(workload.Shape(*heads, scale=scale), c, u, seed=seed,
+                                         spare_pages=5, extra_pages_per_req=2)
+        say(f"[gpu sparse] heads={heads} c={list(c)[:8]} u={list(u)[:8]} block={block} top={top} "
+            f"seed={seed}")
+        self.kc, self.vc = oracle.batch_kv_append(b)
+        s = b.shape
+        self.shape = ssa.make_shape(s.hq, s.hkv, s.d, b.num_pages, b.max_pages_per_req,
+                                    s.softmax_scale)
+        self.batch_plan, _ = ssa.ssa_plan(self.shape, b.q_len, b.ctx_len)
+        self.plan, ws, self.max_blocks = ssa.sparse_plan(self.shape, b.q_len, b.ctx_len, block, top,
+                                                         sink, recent)
+        if plan == "pinned":
+            self.plan = self.plan_dev = torch.from_numpy(self.plan).pin_memory()
+            self.batch_plan = self.batch_dev = torch.from_numpy(self.batch_plan).pin_memory()
+        else:
+            self.plan_dev, self.batch_dev = dev(torch, self.plan), dev(torch, self.batch_plan)
+        self.upload()
+        # behind the tickets the workspace holds anything
+        self.ws = torch.full((ws,), 0xFF, dtype=torch.uint8, device="cuda")
+        self.ws[:4096] = 0
+        T, hkv = b.num_tokens, s.hkv
+        self.scores = torch.full((T, hkv, self.max_blocks), -7.0, device="cuda")
+        self.blocks = torch.full((T, hkv, top), -9, dtype=torch.int32, device="cuda")
+        self.out = torch.full((T + 1, s.hq, s.d), 3.0, dtype=torch.bfloat16, device="cuda")
+        self.summary = dev(torch, np.full((b.num_pages, hkv, 2, s.d), 0x1234, np.uint16))
+
+    def upload(self):
+        b, torch = self.b, self.torch
+        self.q, self.k, self.v = dev(torch, b.q), dev(torch, self.kc), dev(torch, self.vc)
+        self.table = dev(torch, b.block_table)
+
+    def summarise(self, stream=None):
+        self.ssa.block_summary(self.shape, self.batch_plan, self.batch_dev, self.block, self.k,
+                               self.table, self.summary, stream)
+
+    def score(self, stream=None):
+        self.ssa.block_scores(self.shape, self.plan, self.plan_dev, self.q, self.summary, self.table,
+                              self.scores, stream)
+
+    def select(self, stream=None):
+        self.ssa.block_select(self.shape, self.plan, self.plan_dev, self.scores, self.blocks, stream)
+
+    def attend(self, stream=None):
+        self.ssa.sparse_attention(self.shape, self.plan, self.plan_dev, self.q, self.k, self.v,
+                                  self.table, self.blocks, self.out, self.ws, stream)
+
+    def rows(self):
+        """(request, token row, position) of every new row."""
+        row = 0
+        for i in range(self.b.num_reqs):
+            for j in range(int(self.b.q_len[i])):
+                yield i, row, int(self.b.ctx_len[i]) + j
+                row += 1
+
+    def whole_summary(self):
+        """All blocks' summaries by the oracle, on the device: bits [num_pages, Hkv, 2, D]."""
+        from oracle import sparse
+        b = self.b
+        whole = np.full((b.num_pages, b.shape.hkv, 2, b.shape.d), 0x7FC0, np.uint16)  # NaN
+        length = b.q_len + b.ctx_len
+        import dataclasses
+        for at, x in sparse.summary(dataclasses.replace(b, q_len=np.where(b.q_len > 0, length, 0),
+                                                        ctx_len=np.zeros_like(length)),
+                                    self.kc, self.block).items():
+            whole[at] = x
+        self.summary = dev(self.torch, whole)
+        return whole
+
+    def check_scores(self, whole):
+        from oracle import sparse
+        b, s = self.b, self.b.shape
+        g, got = s.group, self.scores.cpu().numpy().astype(np.float64)
+        for i, row, pos in self.rows():
+            n = pos // self.block + 1
+            at = b.block_table[i, np.arange(n) * self.block // 16]
+            for h in range(s.hkv):
+                hl = sparse._f64(whole[at, h])
+                ref, size = sparse.bounds(sparse._f64(b.q[row, h * g:(h + 1) * g]), hl[:, 0], hl[:, 1])
+                err = np.abs(got[row, h, :n] - ref)
+                assert (err <= 2 * s.d * 2.0 ** -24 * size).all(), (i, row, h, err.max())
+                assert (got[row, h, n:] == -7.0).all(), "scores of no block were written"
+
+    def check_lists(self):
+        from oracle import sparse
+        got, scores = self.blocks.cpu().numpy(), self.scores.cpu().numpy()
+        for i, row, pos in self.rows():
+            for h in range(self.b.shape.hkv):
+                ref = sparse.select(scores[row, h, :pos // self.block + 1], self.top, self.sink,
+                                    self.recent)
+                assert np.array_equal(got[row, h], ref), (i, row, h, got[row, h], ref)
+
+    def check_out(self):
+        from oracle import sparse
+        b = self.b
+        lists = self.blocks.cpu().numpy()
+        ref, mass, a = sparse.attention(b, self.kc, self.vc, lists, self.block)
+        keys = self.top * self.block
+        rel = 2.0 ** -24 * (2 * (2 * b.shape.d * a + 8 * a + 2 * keys / 32 + 256) + 1)
+        got = self.out.float().cpu().numpy().astype(np.float64)
+        assert (got[-1] == 3.0).all(), "a row behind the last one was written"
+        err, tol = np.abs(got[:-1] - ref), 2.0 ** -8 * np.abs(ref) + rel * mass
+        assert (err <= tol).all(), (float(np.nanmax(err)), np.argwhere(~(err <= tol))[:5])
+        assert not self.ws[:4096].any(), "tickets are left"
+
+
+MIXED = [((3, 1, 0, 1, 40), (0, 15, 9, 900, 333)), ((1,), (0,)), ((1, 1, 1), (16, 31, 2000)),
+         ((70, 1), (1000, 4095)), ((2, 0, 1), (127, 5, 128))]
+
+
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("cu", MIXED)
+@pytest.mark.parametrize("heads", [(8, 8, 64), (28, 4, 128), (5, 5, 64), (6, 6, 128)])
+def test_summaries_are_the_keys_extremes(torch_dev, heads, cu, block):
+    x = Sparse(torch_dev, heads, *cu, block, 4, seed=block)
+    rng = np.random.default_rng(block)
+    # zeros of both signs, infinities and numbers that are none, among the keys
+    odd = rng.choice(np.array([0x0000, 0x8000, 0x7F80, 0xFF80, 0x7FC1, 0xFFC1], np.uint16), x.kc.shape)
+    x.kc = np.where(rng.random(x.kc.shape) < 0.02, odd, x.kc)
+    x.upload()
+    x.summarise()
+    from oracle import sparse
+    got = bits(x.summary)
+    want = np.full_like(got, 0x1234)
+    for at, v in sparse.summary(x.b, x.kc, block).items():
+        want[at] = v
+    assert np.array_equal(got, want), np.argwhere(got != want)[:5]
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("block,cu", [(16, MIXED[0]), (64, MIXED[3]), (32, MIXED[2]), (128, MIXED[4]),
+                                      (16, ((100, 1), (2500, 6000)))])
+def test_scores_bound_the_blocks(torch_dev, heads, block, cu):
+    x = Sparse(torch_dev, heads, *cu, block, 4, seed=1)
+    whole = x.whole_summary()
+    x.score()
+    x.check_scores(whole)
+
+
+def test_scores_bound_every_logit(torch_dev):
+    """The bound is one: no <q, k> of a block is above it (by more than its rounding)."""
+    from oracle import sparse
+    x = Sparse(torch_dev, (8, 2, 128), (5, 1), (700, 300), 32, 4, seed=4)
+    x.whole_summary()
+    x.score()
+    got = x.scores.cpu().numpy().astype(np.float64)
+    for i, row, pos in x.rows():
+        for h in range(2):
+            k = sparse._f64(sparse.cached(x.b, x.kc, i, h, pos + 1))
+            q = sparse._f64(x.b.q[row, 4 * h:4 * h + 4])
+            size = (np.abs(q) @ np.abs(k).T).max()
+            for n in range(pos // 32 + 1):
+                logits = q @ k[n * 32:(n + 1) * 32].T
+                assert logits.max() <= got[row, h, n] + 2 * 256 * 2.0 ** -24 * size
+
+
+@pytest.mark.parametrize("heads,c,u,block", [
+    ((8, 8, 64), (1, 1, 3), (10, 600, 900), 16),
+    ((28, 4, 128), (40, 1), (3000, 7000), 16),       # up to 438 blocks: one wave
+    ((4, 2, 128), (1, 2), (20000, 30000), 16),       # 1876: four waves
+    ((2, 2, 64), (1, 1, 1), (90000, 500, 131071), 16),  # 8192: sixteen
+    ((1, 1, 64), (1, 2), (524285, 70000), 16),       # 32768: the most
+])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd", "narrow"])
+@pytest.mark.parametrize("top,sink,recent", [(1, 0, 1), (5, 1, 2), (64, 3, 1), (100, 50, 50)])
+def test_selection(torch_dev, heads, c, u, block, kind, top, sink, recent):
+    """Only the plan and the scores: no pool is touched."""
+    from oracle import sparse
+    from paper_2606_05933_amd import ssa
+    torch = torch_dev
+    say(f"[gpu sparse select] {heads} c={c} u={u} {kind} top={top}")
+    hq, hkv, d = heads
+    shape = ssa.make_shape(hq, hkv, d, 1 << 20, 40000, 0.1)
+    plan, _, stride = ssa.sparse_plan(shape, c, u, block, top, sink, recent)
+    T = sum(c)
+    rng = np.random.default_rng(top)
+    size = (T, hkv, stride)
+    if kind == "spread":
+        s = rng.lognormal(0, 3, size) * rng.choice([-1, 1], size)
+    elif kind == "ties":
+        s = rng.integers(0, 3, size).astype(np.float64)
+    elif kind == "odd":
+        s = rng.choice([np.nan, -np.nan, np.inf, -np.inf, 0.0, -0.0, 1.0, -1e-40, 3e38], size)
+    else:
+        s = 1.0 + rng.integers(0, 2000, size) * 2.0 ** -23
+    s = s.astype(np.float32)
+    blocks = torch.full((T + 1, hkv, top), -9, dtype=torch.int32, device="cuda")
+    ssa.block_select(shape, plan, dev(torch, plan), dev(torch, s), blocks)
+    got, row = blocks.cpu().numpy(), 0
+    assert (got[-1] == -9).all()
+    for i in range(len(c)):
+        for j in range(c[i]):
+            for h in range(hkv):
+                ref = sparse.select(s[row, h, :(u[i] + j) // block + 1], top, sink, recent)
+                assert np.array_equal(got[row, h], ref), (i, j, h)
+            row += 1
+
+
+def random_lists(rng, x):
+    """Lists as ssa_block_select does not make them: unordered, named twice, out of range,
+    empty ones."""
+    s = x.b.shape
+    lists = np.full((x.b.num_tokens, s.hkv, x.top), -1, np.int32)
+    for _, row, pos in x.rows():
+        n = pos // x.block + 1
+        for h in range(s.hkv):
+            lists[row, h] = rng.integers(0, n, x.top)
+            kind = rng.integers(0, 6)
+            if kind == 0:
+                lists[row, h] = -1
+            elif kind == 1:
+                lists[row, h, rng.random(x.top) < 0.7] = -1
+            elif kind == 2:
+                bad = rng.random(x.top) < 0.5
+                lists[row, h, bad] = rng.choice([n, n + 7, -5, 2 ** 31 - 1, -2 ** 31], int(bad.sum()))
+            elif kind == 3:
+                lists[row, h] = n - 1  # the partial block, over and over
+            elif kind == 4:
+                lists[row, h] = rng.permutation(np.resize(np.arange(n), x.top))
+    x.blocks.copy_(dev(x.torch, lists))
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("block,top,cu", [(16, 5, MIXED[0]), (64, 3, MIXED[3]), (32, 40, MIXED[2]),
+                                          (128, 2, MIXED[4]), (16, 1, MIXED[1]), (16, 600, MIXED[0])])
+def test_attention_over_any_lists(torch_dev, heads, block, top, cu):
+    x = Sparse(torch_dev, heads, *cu, block, top, 0, 1, seed=7)
+    random_lists(np.random.default_rng(top), x)
+    x.attend()
+    x.check_out()
+    first = bits(x.out)
+    x.attend()  # the workspace as the call left it, and the same bits
+    assert np.array_equal(bits(x.out), first)
+
+
+@pytest.mark.parametrize("heads,u,block,top", [((8, 2, 128), 5000, 64, 64), ((16, 1, 64), 9000, 16, 500),
+                                               ((4, 4, 64), 3000, 128, 20), ((13, 1, 128), 20000, 32, 33)])
+def test_cut_lists_of_few_rows(torch_dev, heads, u, block, top):
+    x = Sparse(torch_dev, heads, (1,), (u,), block, top, seed=11)
+    assert x.ws.numel() > 4096, "the list is not cut"
+    rng = np.random.default_rng(1)
+    lists = np.sort(rng.permutation(u // block + 1)[:top]).astype(np.int32)
+    lists = np.pad(lists, (0, top - len(lists)), constant_values=-1)
+    x.blocks.copy_(dev(torch_dev, np.broadcast_to(lists, (1, heads[1], top))))
+    x.attend()
+    x.check_out()
+    lists[3:] = -1  # most pieces hold nothing
+    x.blocks.copy_(dev(torch_dev, np.broadcast_to(lists, (1, heads[1], top))))
+    x.attend()
+    x.check_out()
+    x.blocks.fill_(-1)
+    x.attend()
+    assert not x.out[:-1].any(), "a row without keys gives zeros"
+
+
+def test_all_blocks_give_the_attention_call(torch_dev):
+    """Lists of every block: ssa_mixed_attention's result, to the two calls' rounding."""
+    from oracle import oracle
+    x = Sparse(torch_dev, (28, 4, 128), *MIXED[0], 32, 64, seed=2)
+    x.blocks.copy_(torch_dev.arange(64, dtype=torch_dev.int32, device="cuda").expand(x.blocks.shape))
+    x.attend()
+    x.check_out()
+    ref, _ = oracle.batch_attention(x.b, x.kc, x.vc)
+    got = x.out[:-1].float().cpu().numpy().astype(np.float64)
+    assert np.abs(got - ref).max() <= 2e-2 and np.abs(got - ref).mean() <= 2e-3
+
+
+@pytest.mark.parametrize("plan", ["device", "pinned"])
+@pytest.mark.parametrize("heads,block,top,cu", [((32, 8, 128), 16, 8, ((1, 1, 20), (500, 3000, 700))),
+                                                ((8, 8, 64), 64, 3, ((1, 5, 0, 1), (64, 900, 3, 1)))])
+def test_the_calls_in_order(torch_dev, heads, block, top, cu, plan):
+    """Summaries of the whole prompt, then of the new tokens, scores, lists, attention, on a
+    stream of their own."""
+    torch = torch_dev
+    x = Sparse(torch, heads, *cu, block, top, 1, 2, seed=5, plan=plan)
+    whole = x.whole_summary()
+    made = bits(x.summary)
+    b = x.b
+    import dataclasses
+    y = dataclasses.replace(b, q_len=np.where(b.q_len > 0, b.ctx_len, 0), ctx_len=0 * b.ctx_len)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        x.summary.fill_(1.0)
+        first, _ = x.ssa.ssa_plan(x.shape, y.q_len, y.ctx_len)
+        x.ssa.block_summary(x.shape, first, dev(torch, first), block, x.k, x.table, x.summary)
+        x.summarise()
+        x.score()
+        x.select()
+        x.attend()
+    s.synchronize()
+    got = bits(x.summary)
+    for i in range(b.num_reqs):
+        n = int(b.q_len[i] + b.ctx_len[i])
+        if b.q_len[i]:
+            at = b.block_table[i, np.arange(-(-n // block)) * block // 16]
+            assert np.array_equal(got[at], made[at])
+    x.check_scores(whole)
+    x.check_lists()
+    x.check_out()
+
+
+def test_replayed_graph(torch_dev):
+    """All calls in one graph, replayed with eager work of the same workspace between."""
+    torch = torch_dev
+    x = Sparse(torch, (32, 8, 128), (1, 4, 1), (5000, 300, 40), 32, 20, 1, 2, seed=9)
+    assert x.ws.numel() > 4096
+    x.whole_summary()
+
+    def run():
+        x.summarise()
+        x.score()
+        x.select()
+        x.attend()
+
+    run()
+    torch.cuda.synchronize()
+    want = bits(x.out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(4):
+        x.out.fill_(3.0)
+        x.blocks.fill_(-9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(bits(x.out), want), i
+        x.attend()
+    x.check_lists()
+    x.check_out()
+
+
+def test_values_that_are_no_numbers(torch_dev):
+    """NaN and infinite keys and values of named blocks show, and nothing else does: other
+    blocks, later positions, and the slots behind a request's last key."""
+    torch = torch_dev
+    x = Sparse(torch, (4, 2, 128), (3, 1), (200, 70), 16, 4, seed=3)
+    b = x.b
+    lists = np.full((4, 2, 4), -1, np.int32)
+    lists[:, :, :2] = [1, 3]
+    lists[:3, :, 2] = [[12], [12], [12]]
+    x.blocks.copy_(dev(torch, lists))
+    # request 0: NaN in block 2 (named by no one), in position 202 (seen by row 2 alone)
+    x.kc[b.block_table[0, 2], :, 3] = 0x7FC0
+    x.vc[b.block_table[0, 2], :, :, 5] = 0x7F80
+    x.vc[b.block_table[0, 12], 0, :, 10] = 0x7FC0
+    # request 1: an infinite value of a named key
+    x.vc[b.block_table[1, 1], 1, 7, 2] = 0xFF80
+    x.upload()
+    x.attend()
+    got = x.out[:-1].float().cpu().numpy().reshape(4, 2, 2, 128)
+    bad = np.isnan(got)
+    assert bad[2, 0].all() and not bad[:2].any() and not bad[2, 1].any() and not bad[3].any()
+    assert (got[3, 1, :, 7] == -np.inf).all()
+    assert np.isfinite(np.delete(got[3], 7, axis=2)).all()
+
+
+def test_far_offsets(torch_dev):
+    """Pages whose bytes lie past 2^32 from the pools' first one."""
+    torch = torch_dev
+    from paper_2606_05933_amd import ssa
+    hq, hkv, d = 8, 8, 128
+    pages = (1 << 32) // (hkv * 16 * d * 2) * 2 + 9  # 8 GiB a pool
+    shape = ssa.make_shape(hq, hkv, d, pages, 4, 0.1)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k = torch.zeros((pages, hkv, 16, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros((pages, hkv, d, 16), dtype=torch.bfloat16, device="cuda")
+    summary = torch.zeros((pages, hkv, 2, d), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([pages - 1, pages // 2 + 5, pages - 3], device="cuda")
+    k[at] = torch.empty((3, hkv, 16, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    v[at] = torch.empty((3, hkv, d, 16), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    q = torch.empty((1, hq, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    table = torch.tensor([[*at.tolist(), 0]], dtype=torch.int32, device="cuda")
+    near = torch.tensor([[0, 1, 2, 3]], dtype=torch.int32, device="cuda")
+    outs = []
+    for t, kk, vv, n in ((table, k, v, pages), (near, k[at].clone(), v[at].clone(), 3)):
+        s = ssa.make_shape(hq, hkv, d, n, 4, 0.1)
+        whole, _ = ssa.ssa_plan(s, [47], [0])
+        plan, ws, stride = ssa.sparse_plan(s, [1], [46], 16, 2, 0, 1)
+        sm = summary[:n]
+        ssa.block_summary(s, whole, dev(torch, whole), 16, kk, t, sm)
+        scores = torch.zeros((1, hkv, stride), device="cuda")
+        blocks = torch.zeros((1, hkv, 2), dtype=torch.int32, device="cuda")
+        out = torch.zeros((1, hq, d), dtype=torch.bfloat16, device="cuda")
+        pd = dev(torch, plan)
+        ssa.block_scores(s, plan, pd, q, sm, t, scores)
+        ssa.block_select(s, plan, pd, scores, blocks)
+        ssa.sparse_attention(s, plan, pd, q, kk, vv, t, blocks, out,
+                             torch.zeros(ws, dtype=torch.uint8, device="cuda"))
+        outs.append((sm[t[0, :3].long()].clone(), scores, blocks, out))
+    for a, c in zip(*outs):
+        assert torch.equal(a, c)
+    assert outs[0][3].any()
