@@ -82,8 +82,8 @@ typedef struct ssa_sparse_config {
  *   max_blocks  blocks of a row of scores: those of the longest request with a new
  *               token, rounded up to a multiple of four (at least four)
  * Errors: those of ssa_plan_size (without TUNING); SHAPE also for Hq D > 2^24; LENGTH
- * also for a request of more than 32768 blocks and where the plan would pass 2 GiB or a
- * launch 2^31 workgroups; ARG (config); PLAN_SIZE (plan_bytes too small).
+ * also for a request of more than 32768 blocks, for Hkv max_blocks > 2^24, and where the
+ * plan would pass 2 GiB or a launch 2^31 workgroups; ARG (config); PLAN_SIZE (plan_bytes too small).
  */
 int ssa_sparse_plan_size(const ssa_shape* shape, const ssa_sparse_config* config,
                          const int32_t* q_len_host, const int32_t* ctx_len_host, int32_t num_reqs,

@@ -31,85 +31,104 @@ struct PagesArgs {
   int64_t max_rows;
 };
 
-struct Sums {
-  int64_t taken, given, rows;
-};
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+// Sums that stay at 2^32 - 1 instead of passing it: what is left of valid ones is below
+// 2^31.
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) {
+  return __builtin_elementwise_add_sat(a, b);
+}
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor((long long)x, o, 64);
+  for (int o = 32; o > 0; o >>= 1) x = add(x, (uint32_t)__shfl_xor((int)x, o, 64));
   return x;
 }
-__device__ __forceinline__ int pages_of(int len) { return (len + kPage - 1) / kPage; }
+struct Sums {
+  uint32_t taken, given, rows;
+  __device__ __forceinline__ void count(int from, int to) {
+    const int p = pages_of(from), q = pages_of(to);
+    taken = add(taken, max(q - p, 0));
+    given = add(given, max(p - q, 0));
+    rows = add(rows, max(to - from, 0));
+  }
+  __device__ __forceinline__ Sums over_wave() const {
+    return Sums{wave_sum(taken), wave_sum(given), wave_sum(rows)};
+  }
+  static __device__ __forceinline__ int pages_of(int len) { return (len + kPage - 1) / kPage; }
+};
 
 // A wave takes one piece of one request.  It adds up what the requests take, give and add
 // itself, those before its own apart: one launch, and no workgroup waits for another.
-// The lengths are read by every wave (64 requests 512 bytes), so latency bounds it as long
-// as the requests are some thousands: the lengths, the state, the ring or the table.
+// The lengths are read by every wave that has something to write (64 requests 512 bytes), so
+// latency bounds it as long as the requests are some thousands: the lengths, then the ring
+// or the table.
 __global__ __launch_bounds__(64 * kWavesPerGroup) void pages_resize_kernel(PagesArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * kWavesPerGroup +
                        __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int req = (int)(unit / a.pieces), piece = (int)(unit % a.pieces);
   if (req > 0 && req >= a.n) return;  // no requests: one wave copies the state
+  const int from = a.n > 0 ? a.old_len[req] : 0, to = a.n > 0 ? a.new_len[req] : 0;
+  // lengths that are none differ by more than any piece's first token, or are of no piece
+  const int64_t tokens = (int64_t)to - from;
+  if (piece > 0 && tokens <= piece * 64 && -tokens / kPage < piece * 64) return;
   const int head = a.state[0], count = a.state[1];
   Sums before{0, 0, 0}, all{0, 0, 0};
   bool bad = false;
+#pragma unroll 4
   for (int i = lane; i < a.n; i += 64) {
-    const int from = a.old_len[i], to = a.new_len[i];
-    if (from < 0 || to < 0 || from > a.most || to > a.most) {
+    const int f = a.old_len[i], t = a.new_len[i];
+    if (f < 0 || t < 0 || f > a.most || t > a.most) {
       bad = true;
       continue;
     }
-    const int p = pages_of(from), q = pages_of(to);
-    all.taken += max(q - p, 0);
-    all.given += max(p - q, 0);
-    all.rows += max(to - from, 0);
-    if (i < req) {
-      before.taken += max(q - p, 0);
-      before.given += max(p - q, 0);
-      before.rows += max(to - from, 0);
-    }
+    all.count(f, t);
+    if (i < req) before.count(f, t);
   }
-  all = Sums{wave_sum(all.taken), wave_sum(all.given), wave_sum(all.rows)};
+  all = all.over_wave();
+  before = before.over_wave();
   int status = __any(bad) ? SSA_PAGES_LENGTH : 0;
-  int64_t missing = 0;
+  uint32_t missing = 0;
   if (head < 0 || head >= a.num_pages || count < 0 || count > a.num_pages) {
     status |= SSA_PAGES_RING;
   } else if (!status) {
-    if (all.taken > count) {
+    if (all.taken > (uint32_t)count) {
       status |= SSA_PAGES_SHORT;
-      missing = all.taken - count;
+      missing = all.taken - (uint32_t)count;
     }
-    if (count + all.given > a.num_pages) status |= SSA_PAGES_RING;
+    if ((int64_t)count + all.given > a.num_pages) status |= SSA_PAGES_RING;
   }
-  if (all.rows > (a.slots ? a.max_rows : INT32_MAX)) status |= SSA_PAGES_ROWS;
+  if (all.rows > (a.slots ? min(a.max_rows, (int64_t)INT32_MAX) : INT32_MAX))
+    status |= SSA_PAGES_ROWS;
   if (unit == 0 && lane == 0) {
-    a.state_out[0] = status ? head : (int)((head + all.taken) % a.num_pages);
-    a.state_out[1] = status ? count : (int)(count - all.taken + all.given);
+    a.state_out[0] = status ? head : (int)(((int64_t)head + all.taken) % a.num_pages);
+    a.state_out[1] = status ? count : (int)(count - (int64_t)all.taken + all.given);
     a.state_out[2] = status;
-    a.state_out[3] = (int)(missing < INT32_MAX ? missing : INT32_MAX);
+    a.state_out[3] = (int)min(missing, (uint32_t)INT32_MAX);
     if (!status && a.row_start) a.row_start[0] = 0;
   }
   if (status || req >= a.n) return;
-  before = Sums{wave_sum(before.taken), wave_sum(before.given), wave_sum(before.rows)};
-  const int from = a.old_len[req], to = a.new_len[req];
-  const int p = pages_of(from), q = pages_of(to);
+  const int p = Sums::pages_of(from), q = Sums::pages_of(to);
   int32_t* row = a.table + (size_t)req * a.maxp;
   if (piece == 0 && lane == 0 && a.row_start)
     a.row_start[req + 1] = (int32_t)(before.rows + max(to - from, 0));
   // entry k >= p takes ring entry (head + before.taken + k - p) mod num_pages
-  auto wrapped = [&](int64_t at) { return (int)(at < a.num_pages ? at : at - a.num_pages); };
-  const int64_t take0 = ((int64_t)head + before.taken) % a.num_pages;
-  const int64_t give0 = ((int64_t)head + count + before.given) % a.num_pages;
+  auto wrapped = [&](uint32_t at) {
+    return at < (uint32_t)a.num_pages ? at : at - (uint32_t)a.num_pages;
+  };
+  const uint32_t take0 = wrapped((uint32_t)head + before.taken);
+  const uint32_t give0 = wrapped(wrapped((uint32_t)head + count) + before.given);
   const int step = a.pieces * 64, mine = piece * 64 + lane;
-  for (int k = p + mine; k < q; k += step) row[k] = a.ring[wrapped(take0 + (k - p))];
-  for (int k = q + mine; k < p; k += step) a.ring[wrapped(give0 + (k - q))] = row[k];
+#pragma unroll 4
+  for (int k = p + mine; k < q; k += step) row[k] = a.ring[wrapped(take0 + (uint32_t)(k - p))];
+#pragma unroll 4
+  for (int k = q + mine; k < p; k += step) a.ring[wrapped(give0 + (uint32_t)(k - q))] = row[k];
   if (!a.slots) return;
   int64_t* slots = a.slots + before.rows;
-  for (int64_t t = (int64_t)from + mine; t < to; t += step) {
-    const int k = (int)(t / kPage);
-    const int page = k < p ? row[k] : a.ring[wrapped(take0 + (k - p))];
-    slots[t - from] = (int64_t)page * kPage + t % kPage;
+#pragma unroll 4
+  for (int t = from + mine; t < to; t += step) {
+    const int k = t / kPage;
+    // a page taken by this call from the ring, one of before from the table
+    const int32_t* at = k < p ? row + k : a.ring + wrapped(take0 + (uint32_t)(k - p));
+    slots[t - from] = (int64_t)*at * kPage + t % kPage;
   }
 }
 
@@ -140,7 +159,7 @@ extern "C" int ssa_pages_resize(const ssa_shape* shape, int32_t num_reqs, const 
   a.row_start = row_start;
   a.slots = slots;
   a.max_rows = max_rows;
-  a.pieces = 8;
+  a.pieces = 32;
   const int64_t units = (int64_t)std::max(1, num_reqs) * a.pieces;
   (void)hipGetLastError();
   hipLaunchKernelGGL(pages_resize_kernel, dim3((units + kWavesPerGroup - 1) / kWavesPerGroup),

@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <initializer_list>
+#include <type_traits>
 
 #include "../../include/ssa_sparse.h"
 #include "ssa_device.h"
@@ -31,11 +32,17 @@ __device__ __forceinline__ int workgroup_id() {
 // Summaries.  A wave takes one kv head of one block: 16 bytes of a key row a lane, the
 // block's rows dealt to groups of D / 8 lanes, all loads before the first use.  bf16 values
 // are compared as 16-bit integers (negative ones with their other bits inverted), two an
-// instruction, so that the extremes are the keys' own bits.
+// instruction, so that the extremes are the keys' own bits.  Of the plan's append segments (a
+// page of new tokens each) the first one in a block stands for it.  A chunk has one such in
+// BLOCK / 16 of its segments: a wave looks at as many, so that every workgroup has work (with
+// a workgroup a segment, those with work fell to two of the eight dies, and 33768 tokens of
+// 8 heads in blocks of 64 took 29.5 us).
 struct SummaryArgs {
   const uint8_t* plan;
   uint64_t hash;
   int32_t off_segments, off_reqs;
+  int32_t num_runs;  // runs of a block's pages among the chunks' segments
+  int32_t num_chunk_segments;
   int32_t workgroups, head_groups;
   int32_t hkv, maxp, block_keys;
   const uint16_t* kc;
@@ -62,30 +69,18 @@ __device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b) {
                                                                 __builtin_bit_cast(i16x2, b)));
 }
 
+// Block of request `req` from position `first` on.
 template <int D, int BLOCK>
-__global__ __launch_bounds__(kSparseThreads) void block_summary_kernel(SummaryArgs a) {
+__device__ __forceinline__ void summarise(const SummaryArgs& a, int req, int first, int len, int kvh,
+                                          int lane) {
   constexpr int CPR = D / 8, ROWS = 64 / CPR;  // lanes a row, rows a load
-  constexpr int LOADS = BLOCK / ROWS;
-  const int wg = workgroup_id();
-  if (wg >= a.workgroups) return;
-  const auto h = as_uniform<PlanHeader>(a.plan);
-  const auto sg = as_uniform<AppendSeg>(a.plan + a.off_segments) + wg / a.head_groups;
-  const int req = sg->req, pos0 = sg->pos0;
-  if (h->magic != kPlanMagic || h->hash != a.hash) return;
-  const auto rq = as_uniform<ReqEntry>(a.plan + a.off_reqs) + req;
-  // of a block's segments the first one does it
-  if (pos0 % BLOCK != 0 && pos0 != rq->ctx_len) return;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int kvh = wg % a.head_groups * 4 + wave;
-  if (kvh >= a.hkv) return;
-  const int first = pos0 / BLOCK * BLOCK, len = rq->ctx_len + rq->q_len;
+  constexpr int LOADS = BLOCK / ROWS, PER_PAGE = 16 / ROWS;
   const auto row = as_uniform<int32_t>(a.bt + (size_t)req * a.maxp);
   // rows past the last key read that one again
   const int last = min(first + BLOCK, len) - 1;
   u32x4 k[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
-    constexpr int PER_PAGE = 16 / ROWS;  // loads of a page
     const int page = row[min(first / 16 + i / PER_PAGE, last / 16)];
     const int t = min(first + i * ROWS + lane / CPR, last);
     k[i] = ld16(a.kc + (((size_t)page * a.hkv + kvh) * 16 + t % 16) * D + lane % CPR * 8);
@@ -113,6 +108,30 @@ __global__ __launch_bounds__(kSparseThreads) void block_summary_kernel(SummaryAr
   else if (lane < 2 * CPR) st16(to + D, lo);
 }
 
+template <int D, int BLOCK>
+__global__ __launch_bounds__(kSparseThreads) void block_summary_kernel(SummaryArgs a) {
+  const int wg = workgroup_id();
+  if (wg >= a.workgroups) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int kvh = wg % a.head_groups * 4 + wave;
+  if (kvh >= a.hkv) return;
+  const int unit = wg / a.head_groups;
+  const auto h = as_uniform<PlanHeader>(a.plan);
+  if (h->magic != kPlanMagic || h->hash != a.hash) return;
+  int seg = a.num_chunk_segments + (unit - a.num_runs), end = seg + 1;
+  if (unit < a.num_runs) {
+    seg = unit * (BLOCK / 16);
+    end = min(seg + BLOCK / 16, a.num_chunk_segments);
+  }
+  for (; seg < end; ++seg) {
+    const auto sg = as_uniform<AppendSeg>(a.plan + a.off_segments) + seg;
+    const int req = sg->req, pos0 = sg->pos0;
+    const auto rq = as_uniform<ReqEntry>(a.plan + a.off_reqs) + req;
+    if (pos0 % BLOCK == 0 || pos0 == rq->ctx_len)
+      summarise<D, BLOCK>(a, req, pos0 / BLOCK * BLOCK, rq->ctx_len + rq->q_len, kvh, lane);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Launches with a sparse plan.
 struct SparseArgs {
@@ -124,6 +143,7 @@ struct SparseArgs {
   int32_t block_keys, log_block;
   int32_t top, sink, recent, max_blocks;
   int32_t nsplit, split_entries;
+  int32_t tokens, subs, g_magic;  // rows of an attention workgroup, workgroups of a record of rows
   float c;  // softmax_scale * log2(e)
   const uint16_t* q;
   const uint16_t* kc;
@@ -161,12 +181,17 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
 
 // ---------------------------------------------------------------------------
 // Scores.  [max(q, 0), min(q, 0)] times [high, low]: a matrix product over 2 D, exact in its
-// bf16 factors.  Blocks are the rows of the 16x16x32 products, (token, head) pairs of a kv
-// head the columns, whole tokens in a tile; the highest of a token's heads is taken over
-// its lanes.  A wave keeps two tiles of 16 blocks and goes over the item's columns.
-template <int D>
-__global__ __launch_bounds__(kSparseThreads) void block_scores_kernel(SparseArgs a) {
-  constexpr int KS = D / 32;
+// bf16 factors.  A 16x16x32 product has (token, head) rows, the kv head's heads padded to a
+// power of two with its last one, and 16 blocks as columns, so that a token's heads lie in
+// the registers of a lane and, from eight on, in 2 or 4 lanes.  A wave keeps two tiles of
+// blocks.  The queries of four tiles at a time go through LDS, split into their two parts, a
+// tile by each wave, the next four on their way meanwhile: a kv head's queries lie in a few
+// of the cache's channels (1 KB of every 8 at 32/8 heads), and read by every wave for itself
+// they bounded the kernel (512 rows on 32768 keys in blocks of 32: 33 us, so 20).
+template <int D, int LOG_G>  // heads of a group: more than 2^(LOG_G - 1), up to 2^LOG_G
+__global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseArgs a) {
+  constexpr int KS = D / 32, TOKENS = 16 >> LOG_G;  // tokens of a tile
+  __shared__ u32x4 s_query[4][2 * KS][64];  // tile, part of the product, lane
   const int wg = workgroup_id();
   if (wg >= a.workgroups) return;
   const int kvh = wg % a.hkv;
@@ -174,12 +199,19 @@ __global__ __launch_bounds__(kSparseThreads) void block_scores_kernel(SparseArgs
   if (!plan_ok(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r16 = lane & 15, quad = lane >> 4;
-  const int tokens = 16 / a.g;  // of a tile
-  const int token = r16 / a.g, head = r16 - token * a.g;
-  const bool column = token < tokens;
+  const int token = r16 >> LOG_G, head = min(r16 & ((1 << LOG_G) - 1), a.g - 1);
   const int32_t* row = a.bt + (size_t)it->req * a.maxp;
   const int n = it->n, row0 = it->row0, pos0 = it->pos0, blk1 = it->blk1;
-  for (int b0 = it->blk0 + wave * 32; b0 < blk1; b0 += kScorePass) {
+  const uint16_t* const queries = a.q + ((size_t)row0 * a.hq + kvh * a.g + head) * D + quad * 8;
+  u32x4 ahead[KS];
+  auto load_queries = [&](int j0) {  // rows past the last one read it again
+    const uint16_t* from = queries + (size_t)min(j0 + wave * TOKENS + token, n - 1) * a.hq * D;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) ahead[k] = ld16(from + k * 32);
+  };
+  for (int p0 = it->blk0; p0 < blk1; p0 += kScorePass) {
+    const int b0 = p0 + wave * 32;
+    load_queries(0);
     bf16x8 s[2][2 * KS];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -190,57 +222,81 @@ __global__ __launch_bounds__(kSparseThreads) void block_scores_kernel(SparseArgs
 #pragma unroll
       for (int k = 0; k < 2 * KS; ++k) s[t][k] = as_bf16x8(ld16(from + k * 32));
     }
-    for (int j0 = 0; j0 < n; j0 += tokens) {
-      const int j = j0 + token;
-      const bool here = column && j < n;
-      bf16x8 qf[2 * KS];
-      const uint16_t* from =
-          a.q + ((size_t)(row0 + (here ? j : 0)) * a.hq + kvh * a.g + (here ? head : 0)) * D + quad * 8;
+    // a row's scores from block b0 on; rows j0 .. j0 + TOKENS - 1 are `step` floats apart
+    const int step = a.hkv * a.max_blocks;  // at most 2^24
+    float* to = a.scores + ((size_t)row0 * a.hkv + kvh) * a.max_blocks + b0;
+    const bool inner = b0 + 32 <= blk1;
+    for (int g0 = 0; g0 < n; g0 += 4 * TOKENS) {
+      __syncthreads();  // the tiles before have been read
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const u32x4 v = ld16(from + k * 32);
         u32x4 plus, minus;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const uint32_t m = negative_halves(v[w]);
-          plus[w] = v[w] & ~m;
-          minus[w] = v[w] & m;
+          const uint32_t m = negative_halves(ahead[k][w]);
+          plus[w] = ahead[k][w] & ~m;
+          minus[w] = ahead[k][w] & m;
         }
-        qf[k] = as_bf16x8(plus);
-        qf[KS + k] = as_bf16x8(minus);
+        s_query[wave][k][lane] = plus;
+        s_query[wave][KS + k][lane] = minus;
       }
-      f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      if (g0 + 4 * TOKENS < n) load_queries(g0 + 4 * TOKENS);
+      __syncthreads();
+      if (b0 >= blk1) continue;
+      const int end = min(n, g0 + 4 * TOKENS);
+      for (int j0 = g0; j0 < end; j0 += TOKENS, to += (size_t)TOKENS * step) {
+        const auto& query = s_query[(j0 - g0) / TOKENS];
+        // the products with the high and with the low values apart: half as many terms in a
+        // row, and no product waits for the one before
+        f32x4 x[2], y[2];
 #pragma unroll
-      for (int k = 0; k < 2 * KS; ++k)
+        for (int t = 0; t < 2; ++t) x[t] = y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) x[t] = mfma(s[t][k], qf[k], x[t]);
-      // the highest of heads head .. head + 2^i - 1, as far as the group goes
+        for (int k = 0; k < KS; ++k) {
+          const bf16x8 plus = as_bf16x8(query[k][lane]), minus = as_bf16x8(query[KS + k][lane]);
 #pragma unroll
-      for (int o = 1; o < 16; o *= 2) {
-        if (o < a.g) {
-          const bool more = head + o < a.g;
+          for (int t = 0; t < 2; ++t) {
+            x[t] = mfma(plus, s[t][k], x[t]);
+            y[t] = mfma(minus, s[t][KS + k], y[t]);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) x[t] += y[t];
+        // every row of the tile sees every block of it
+        const bool whole = inner && j0 + TOKENS <= n && b0 + 31 <= (pos0 + j0) >> a.log_block;
+        // Lanes without a score store outside the buffer's range, which drops it: every tile has
+        // as many stores, so that the next one's queries are not waited for behind them.
+        const PartWriter tile(to);
+        auto put = [&](int token, int t, float x, bool mine = true) {
+          const int b = t * 16 + r16, j = j0 + token;
+          const bool ok = whole || (j < n && b0 + b < blk1 && b0 + b <= (pos0 + j) >> a.log_block);
+          const uint32_t at = mine && ok ? (uint32_t)(token * step + b) * 4 : 0x80000000u;
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), tile.rsrc, (int)at, 0, 0);
+        };
+        if constexpr (LOG_G == 0) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float y = __shfl_down(x[t][i], o, 16);
-              x[t][i] = more ? fmaxf(x[t][i], y) : x[t][i];
-            }
-        }
-      }
-      if (here && head == 0) {
-        const int seen = ((pos0 + j) >> a.log_block) + 1;
-        float* to = a.scores + ((size_t)(row0 + j) * a.hkv + kvh) * a.max_blocks;
-        const int end = min(seen, blk1);
+            for (int i = 0; i < 4; ++i) put(quad * 4 + i, t, x[t][i]);
+        } else if constexpr (LOG_G == 1) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int b = b0 + t * 16 + quad * 4;
-          if (b + 4 <= end) {
-            *reinterpret_cast<f32x4*>(to + b) = x[t];
-          } else {
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (b + i < end) to[b + i] = x[t][i];
+            for (int i = 0; i < 2; ++i) put(quad * 2 + i, t, fmaxf(x[t][2 * i], x[t][2 * i + 1]));
+        } else {
+          float m[2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            m[t] = fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3]));
+            if constexpr (LOG_G > 2) m[t] = fmaxf(m[t], __shfl_xor(m[t], 16, 64));
+            if constexpr (LOG_G > 3) m[t] = fmaxf(m[t], __shfl_xor(m[t], 32, 64));
+          }
+          const int token = quad >> (LOG_G - 2);
+          if constexpr (LOG_G == 2) {
+            put(token, 0, m[0]);
+            put(token, 1, m[1]);
+          } else {  // of the lanes that have it one a tile
+            put(token, quad & 1, quad & 1 ? m[1] : m[0], LOG_G == 3 || quad < 2);
           }
         }
       }
@@ -287,22 +343,31 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SparseArgs a) 
   }
   const float* from = a.scores_in + list * a.max_blocks;
   const int first = wave * 64 * NR + lane;
+  // registers that hold scores: the others are left out, a few at a time
+  const int used = (n - wave * 64 * NR + 63) / 64;
+  constexpr int STEP = NR < 4 ? NR : 4;
+  auto each = [&](auto body) {
+#pragma unroll
+    for (int i0 = 0; i0 < NR; i0 += STEP)
+      if (i0 < used) {
+#pragma unroll
+        for (int i = i0; i < i0 + STEP; ++i) body(i);
+      }
+  };
   uint32_t k[NR];
   uint32_t any = 0, all = ~0u;
 #pragma unroll
-  for (int i = 0; i < NR; ++i) {
+  for (int i = 0; i < NR; ++i) k[i] = kAbsent;
+  each([&](int i) {
     const int b = first + i * 64;
-    k[i] = kAbsent;
-    if (b < n) {
-      k[i] = order_key(from[b]);
-      if (b < a.sink || b >= n - a.recent) {
-        k[i] = kAlways;
-      } else {
-        any |= k[i];
-        all &= k[i];
-      }
-    }
-  }
+    const float x = from[min(b, n - 1)];
+    uint32_t key = order_key(x);
+    const bool other = b >= a.sink && b < n - a.recent;
+    any |= other ? key : 0;
+    all &= other ? key : ~0u;
+    key = other ? key : kAlways;
+    k[i] = b < n ? key : kAbsent;
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     any |= __shfl_xor(any, o, 64);
@@ -327,8 +392,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SparseArgs a) 
   int turn = 0;
   auto count = [&](uint32_t t) {  // keys >= t of all waves
     int c = 0;
-#pragma unroll
-    for (int i = 0; i < NR; ++i) c += (int)__popcll(__ballot(k[i] >= t));
+    each([&](int i) { c += (int)__popcll(__ballot(k[i] >= t)); });
     if constexpr (WAVES > 1) {
       turn ^= 1;
       if (lane == 0) s_count[turn][wave] = c;
@@ -336,6 +400,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SparseArgs a) 
       c = 0;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) c += s_count[turn][w];
+      c = __builtin_amdgcn_readfirstlane(c);
     }
     return c;
   };
@@ -350,14 +415,10 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SparseArgs a) 
     exact = c == need;
   }
   // keys above t stay, and of those equal to it the first ones
-  int n_in = 0, n_eq = 0;
   const uint32_t above = exact ? t - 1 : t;  // t > 0: -infinity's key is
-#pragma unroll
-  for (int i = 0; i < NR; ++i) {
-    n_in += (int)__popcll(__ballot(k[i] > above));
-    n_eq += (int)__popcll(__ballot(k[i] == t));
-  }
-  if (exact) n_eq = 0;
+  int n_in = 0, n_eq = 0;
+  if (WAVES > 1 || !exact) each([&](int i) { n_in += (int)__popcll(__ballot(k[i] > above)); });
+  if (WAVES > 1 && !exact) each([&](int i) { n_eq += (int)__popcll(__ballot(k[i] == t)); });
   int before_in = 0, before_eq = 0, all_in = n_in;
   if constexpr (WAVES > 1) {
     __syncthreads();  // the last count has been read
@@ -374,111 +435,395 @@ __global__ __launch_bounds__(64 * WAVES) void block_select_kernel(SparseArgs a) 
       all_in += s_count[0][w];
     }
   }
-  const int quota = exact ? 0 : need - all_in;
-#pragma unroll
-  for (int i = 0; i < NR; ++i) {
-    const bool in = k[i] > above, eq = !exact && k[i] == t;
+  if (exact) {
+    each([&](int i) {
+      const bool in = k[i] > above;
+      const uint64_t mask = __ballot(in);
+      if (in) out[before_in + lanes_below(mask)] = first + i * 64;
+      before_in += (int)__popcll(mask);
+    });
+    return;
+  }
+  const int quota = need - all_in;
+  each([&](int i) {
+    const bool in = k[i] > above, eq = k[i] == t;
     const uint64_t mi = __ballot(in), me = __ballot(eq);
     const int eq_at = before_eq + lanes_below(me);
     if (in || (eq && eq_at < quota))
       out[before_in + lanes_below(mi) + min(eq_at, quota)] = first + i * 64;
     before_in += (int)__popcll(mi);
     before_eq += (int)__popcll(me);
-  }
+  });
 }
 
 // ---------------------------------------------------------------------------
-// Attention.  One workgroup takes a piece of a row's list for one kv head.  Its pages (and
-// how many of each one's slots the row sees) go to LDS, those of no block left out; the four
-// waves take two pages (32 keys) each in turn.  The 16x16x32 products have keys as rows and
-// the group's query heads as columns, and key r of a step is row (r & 3) + 4 (r >> 3) of
-// product (r >> 2) & 1, so that the logits of a lane are those whose weights it multiplies
-// with the values (dim-major pages) next.  Keys and values go from memory to registers, a
-// step ahead.
-constexpr int kPassPages = 512;  // pages in LDS at a time
-constexpr uint32_t kMagnitudes = 0x7FFF7FFFu, kInfBits = 0x7F80u;  // above it: NaN
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
-                                                                __builtin_bit_cast(u16x2, b)));
-}
+// 16-byte loads of what other workgroups of the launch have written past their caches;
+// the base is wave-uniform, offsets are bytes from it.
+struct PartReader {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ explicit PartReader(float* base) : rsrc(PartWriter(base).rsrc) {}
+  __device__ f32x4 operator()(int byte_off) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, byte_off, 0,
+                                                                           kCachePolicySc1));
+  }
+};
+
+// Attention.  One workgroup takes as many neighbouring rows of a request as fit in 32 columns
+// (row, query head) of a kv head, and the union of their lists: neighbours mostly look at the
+// same blocks, whose keys and values are then read once, and a block costs the matrix cores the
+// same for one row as for 16 columns of them.  A mask per block says whose it is.  A row alone (a decode)
+// goes by its list as it is, and so do rows one after the other whose lists name a block
+// twice or whose masks would not fit in LDS.
+//
+// The pages (of no block left out) go to LDS; the four waves take two of them, 32 keys, in turn.  The 16x16x32 products have keys as rows; key r of a step is row (r & 3) + 4 (r >> 3)
+// of product (r >> 2) & 1, so that the logits of a lane are those whose weights it multiplies
+// with the values (dim-major pages) next.  Keys and values go from memory to registers, a step
+// ahead.
+constexpr int kPassPages = 512;     // pages in LDS at a time
+constexpr int kMaskBlocks = 8192;   // blocks of a union, 16 bits each
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// The highest x of a column: over the four lanes 16 apart.
+__device__ __forceinline__ float max_over_quads(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+// Keeps the first n of 8 packed bf16 values.
+__device__ __forceinline__ u32x4 first_values(int n) {
+  u32x4 keep;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) keep[w] = (n > 2 * w ? 0xFFFFu : 0u) | (n > 2 * w + 1 ? 0xFFFF0000u : 0u);
+  return keep;
+}
 
 template <int D>
 struct AttentionLds {
-  int2 page[kPassPages + 2];  // page, slots that count
+  int4 page[kPassPages + 2];        // page of the pool, its first position, the rows whose it is
+  uint32_t mask[kMaskBlocks / 2];   // of two blocks each
   int part[2][4];
+  int flag[2];
   float ml[2][4][16];
-  float m[16], inv[16];
-  int last;
-  __attribute__((aligned(16))) float o[4 * 16 * D];
+  float m[32], l[32];               // of the passes so far, and their sums
+  __attribute__((aligned(16))) float sum[32][D];
+  union {
+    int2 block[kPassPages];         // block, the rows whose it is, until the pages are listed
+    __attribute__((aligned(16))) float o[4][16][64];  // the waves' sums, 64 dims at a time
+    float weight[64 * 2 * 32];      // m and l of a list's pieces
+  };
 };
 
 template <int D>
 __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(SparseArgs a) {
   constexpr int KS = D / 32, DT = D / 16;
+  // the joined sums: four dims of column c0 + i CSTEP a thread
+  constexpr int NC = D / 32, CSTEP = 1024 / D;
   __shared__ AttentionLds<D> lds;
   const int wg = workgroup_id();
   if (wg >= a.workgroups) return;
-  const int kvh = wg % a.hkv, split = wg / a.hkv % a.nsplit;
-  Row r;
-  if (!take_row(a, wg / a.hkv / a.nsplit, &r)) return;
+  const int kvh = wg % a.hkv, split = wg / a.hkv % a.nsplit, unit = wg / a.hkv / a.nsplit;
+  // the rows: `rows` of them from token row row0, position pos0 on
+  const bool single = unit >= a.num_groups * a.subs;
+  const int j0 = single ? 0 : unit % a.subs * a.tokens;
+  const auto record = as_uniform<SparseRows>(a.plan + a.off_rows) +
+                      (single ? a.num_groups + (unit - a.num_groups * a.subs) : unit / a.subs);
+  const int rows = min(single ? 1 : a.tokens, record->n - j0);
+  if (!plan_ok(a) || rows <= 0) return;
+  const int row0 = record->row0 + j0, pos0 = record->pos0 + j0, last = pos0 + rows - 1;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r16 = lane & 15, quad = lane >> 4;
-  const size_t list = (size_t)r.row * a.hkv + kvh;
-  const int32_t* blocks = a.blocks_in + list * a.top;
-  const int32_t* table = a.bt + (size_t)r.req * a.maxp;
+  const int columns = rows * a.g;
+  const int32_t* const table = a.bt + (size_t)record->req * a.maxp;
   const int log_pages = a.log_block - 4;
-  const int page0 = (split * a.split_entries) << log_pages;
-  const int page1 = min(a.top, (split + 1) * a.split_entries) << log_pages;
-
-  bf16x8 qf[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    u32x4 v = {0, 0, 0, 0};
-    if (r16 < a.g) v = ld16(a.q + ((size_t)r.row * a.hq + kvh * a.g + r16) * D + s * 32 + quad * 8);
-    qf[s] = as_bf16x8(v);
-  }
-  float m = -kInf, l = 0.f;
-  bool any = false;  // a key counts
-  f32x4 o[DT];
-#pragma unroll
-  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int slot0 = 8 * ((r16 >> 2) & 1) + (r16 & 3);
-  u32x4 kf[2][KS], vf[DT];
-  auto load_keys = [&](int p0, int p1) {
-    const uint16_t* kp =
-        a.kc + ((size_t)(r16 >> 3 ? p1 : p0) * a.hkv + kvh) * 16 * D + slot0 * D + quad * 8;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) kf[t][s] = ld16(kp + t * 4 * D + s * 32);
+  auto token_of = [&](int column) { return (column * a.g_magic) >> 16; };
+  auto list_of = [&](int t) { return a.blocks_in + ((size_t)(row0 + t) * a.hkv + kvh) * a.top; };
+  // (row, query head) of a column
+  auto row_of = [&](int column) {
+    const int t = token_of(column);
+    return ((size_t)(row0 + t) * a.hq + kvh * a.g + (column - t * a.g)) * D;
   };
-  auto load_values = [&](int p0, int p1) {
-    const uint16_t* vp =
-        a.vc + ((size_t)(quad >> 1 ? p1 : p0) * a.hkv + kvh) * 16 * D + r16 * 16 + 8 * (quad & 1);
-#pragma unroll
-    for (int t = 0; t < DT; ++t) vf[t] = ld16(vp + t * 256);
+  // The thread's own number, and its first column and dim of the joined sums, made anew where
+  // they are used: what the compiler knows to be the same all along it keeps in registers all
+  // along, and the products need those.
+  auto anew = [](int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  struct Place {
+    int c0, d0;
+  };
+  auto place = [&] {
+    const int x = anew(tid) * 4;
+    return Place{x / D, x % D};
+  };
+  uint32_t seen;  // rows of which a key counts
+  // m, l and the sums of column c: between the passes they lie in LDS, so that they take no
+  // registers from the products.
+  struct State {
+    float m, l;
+    f32x4 sum;
+  };
+  auto load_state = [&](int c, int d0) {
+    return State{lds.m[c], lds.l[c], *reinterpret_cast<const f32x4*>(&lds.sum[c][d0])};
+  };
+  auto store_state = [&](int c, int d0, const State& x) {
+    *reinterpret_cast<f32x4*>(&lds.sum[c][d0]) = x.sum;
+    if (d0 == 0) {
+      lds.m[c] = x.m;
+      lds.l[c] = x.l;
+    }
   };
 
-  for (int base = page0; base < page1; base += kPassPages) {
-    // the pages of this pass, in the list's order
-    int2 mine[2];
+  // The first `total` pages of lds.page by the matrix cores, for one or two tiles of 16
+  // columns; the waves' sums are joined and added to those of the passes before.
+  auto multiply = [&](int total, auto tiles) __attribute__((always_inline)) {
+    constexpr int NT = tiles;
+    const int r16 = anew(lane) & 15, quad = anew(lane) >> 4;
+    int token[NT];
+    bf16x8 qf[NT][KS];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int column = min(r16 + n * 16, columns - 1);  // the others repeat the last
+      token[n] = token_of(column);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qf[n][s] = as_bf16x8(ld16(a.q + row_of(column) + s * 32 + quad * 8));
+    }
+    float m[NT], l[NT];
+    f32x4 o[NT][DT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n] = -kInf;
+      l[n] = 0.f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int slot0 = 8 * ((r16 >> 2) & 1) + (r16 & 3);
+    u32x4 kf[2][KS], vf[DT];
+    auto load_keys = [&](int p0, int p1) {
+      const uint16_t* kp =
+          a.kc + ((size_t)(r16 >> 3 ? p1 : p0) * a.hkv + kvh) * 16 * D + slot0 * D + quad * 8;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[t][s] = ld16(kp + t * 4 * D + s * 32);
+    };
+    auto load_values = [&](int p0, int p1) {
+      const uint16_t* vp =
+          a.vc + ((size_t)(quad >> 1 ? p1 : p0) * a.hkv + kvh) * 16 * D + r16 * 16 + 8 * (quad & 1);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) vf[t] = ld16(vp + t * 256);
+    };
+    const int steps = (total + 1) / 2;
+    auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(lds.page[i].x); };
+    int p0 = 0, p1 = 0;
+    if (wave < steps) {
+      p0 = page_of(2 * wave);
+      p1 = page_of(2 * wave + 1);
+      load_keys(p0, p1);
+      load_values(p0, p1);
+    }
+    // `more`: the wave has a step after this one.  (A condition known to the compiler: loads
+    // that might not have been issued would be waited for with everything behind them.)
+    auto step = [&](int s, auto more) __attribute__((always_inline)) {
+      const int4 e0 = lds.page[2 * s], e1 = lds.page[2 * s + 1];
+      if constexpr (more) {
+        p0 = page_of(2 * s + 8);
+        p1 = page_of(2 * s + 9);
+      }
+      // the lane's first key, and the last one of the step
+      const int key0 = (quad >> 1 ? e1.y : e0.y) + 8 * (quad & 1);
+      const uint32_t rows_of = quad >> 1 ? e1.z : e0.z;
+      const int far = __builtin_amdgcn_readfirstlane(max(e0.y, e1.y)) + 15;
+      f32x4 logits[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) logits[n][0] = logits[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) logits[n][t] = mfma(as_bf16x8(kf[t][k]), qf[n][k], logits[n][t]);
+      if constexpr (more) load_keys(p0, p1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (far > last) {
+        // a slot that no row sees may hold anything, and 0 times NaN is NaN
+        const u32x4 keep = first_values(last + 1 - key0);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) vf[t] &= keep;
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = logits[n][i >> 2][i & 3];
+        // Is the lane's page the column's row's?  Where it is not, its logits are left out of
+        // the maximum, and their exponents are -infinity.
+        const bool mine = rows_of >> token[n] & 1;
+        if (far > pos0) {  // a row sees a part of it
+          const int nv = pos0 + token[n] + 1 - key0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i >= nv) x[i] = -kInf;
+        }
+        float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                         fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        mx = mine ? mx : -kInf;
+        mx = max_over_quads(mx);
+        const float mn = mx == -kInf ? m[n] : fmaxf(m[n], mx * a.c);
+        const float ms = mn == -kInf ? 0.f : mn;
+        const float alpha = exp2_fast(m[n] - ms), off = mine ? -ms : -kInf;
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = exp2_fast(__builtin_fmaf(x[i], a.c, off));
+        if (far > pos0 && a.c == 0.f) {  // 0 times -infinity is NaN
+          const int nv = mine ? pos0 + token[n] + 1 - key0 : 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i >= nv) p[i] = 0.f;
+        }
+        l[n] = l[n] * alpha + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+        m[n] = mn;
+        // A weight enters the matrix product as three bf16 values, the rounded one and what
+        // that misses twice over: all of its 24 bits.
+        u32x4 part[3];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float x0 = p[2 * w], x1 = p[2 * w + 1];
+#pragma unroll
+          for (int i = 0; i < 3; ++i) {
+            part[i][w] = pack2(x0, x1);
+            x0 -= bf16_lo(part[i][w]);
+            x1 -= bf16_hi(part[i][w]);
+          }
+        }
+        if (__any(alpha != 1.f)) {
+#pragma unroll
+          for (int t = 0; t < DT; ++t) o[n][t] *= alpha;
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+            o[n][t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[i]), o[n][t]);
+        if (n + 1 < NT) __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (more) load_values(p0, p1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int s = wave;
+    for (; s + 4 < steps; s += 4) step(s, std::true_type{});
+    if (s < steps) step(s, std::false_type{});
+    const auto [c0, d0] = place();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      l[n] += __shfl_xor(l[n], 16, 64);
+      l[n] += __shfl_xor(l[n], 32, 64);
+      if (n > 0) __syncthreads();
+      if (quad == 0) {
+        lds.ml[0][wave][r16] = m[n];
+        lds.ml[1][wave][r16] = l[n];
+      }
+      constexpr int PER = NC / 2;  // of a thread's columns, 16 / CSTEP in a tile
+      State x[PER];
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {  // 64 dims at a time
+        if (h > 0) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          *reinterpret_cast<f32x4*>(&lds.o[wave][r16][t * 16 + 4 * quad]) = o[n][h * 4 + t];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int c = c0 + i * CSTEP;
+          if (h == 0) x[i] = load_state(n * 16 + c, d0);
+          if (d0 / 64 != h) continue;
+          float mm = x[i].m;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) mm = fmaxf(mm, lds.ml[0][w][c]);
+          const float ms = mm == -kInf ? 0.f : mm, scale = exp2_fast(x[i].m - ms);
+          x[i].sum *= scale;
+          x[i].l *= scale;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float f = exp2_fast(lds.ml[0][w][c] - ms);
+            x[i].sum += *reinterpret_cast<const f32x4*>(&lds.o[w][c][d0 % 64]) * f;
+            x[i].l += lds.ml[1][w][c] * f;
+          }
+          x[i].m = mm;
+        }
+      }
+      __syncthreads();  // m and l have been read by all threads of a column
+#pragma unroll
+      for (int i = 0; i < PER; ++i) store_state(n * 16 + c0 + i * CSTEP, d0, x[i]);
+    }
+  };
+  // The same, key by key without the matrix cores, for values that are not finite: they reach
+  // only the rows that see their keys, and with the whole weight.  (In the products above, 0
+  // times an infinite value is NaN, for a row that does not see its key and for a part of a
+  // weight.)  About 100 times slower.
+  auto go_through = [&](int total) __attribute__((always_inline)) {
+    const auto [c0, d0] = place();
+    State x[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) x[n] = load_state(c0 + n * CSTEP, d0);
+    __syncthreads();
+    for (int i = 0; i < total; ++i) {
+      const int4 e = lds.page[i];
+      const size_t base = ((size_t)e.x * a.hkv + kvh) * 16 * D;
+      for (int s = 0; s < 16 && e.y + s <= last; ++s) {
+        const u32x2 k = *reinterpret_cast<const u32x2*>(a.kc + base + s * D + d0);
+        f32x4 v;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) v[d] = bf16_lo(a.vc[base + (size_t)(d0 + d) * 16 + s]);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+          const int c = c0 + n * CSTEP, t = token_of(c);
+          u32x2 q = {0, 0};
+          if (c < columns) q = *reinterpret_cast<const u32x2*>(a.q + row_of(c) + d0);
+          float y = bf16_lo(q[0]) * bf16_lo(k[0]);
+          y = __builtin_fmaf(bf16_hi(q[0]), bf16_hi(k[0]), y);
+          y = __builtin_fmaf(bf16_lo(q[1]), bf16_lo(k[1]), y);
+          y = __builtin_fmaf(bf16_hi(q[1]), bf16_hi(k[1]), y);
+          for (int o = 1; o < D / 4; o *= 2) y += __shfl_xor(y, o, 64);
+          if (c >= columns || !(e.z >> t & 1) || e.y + s > pos0 + t) continue;
+          const float mn = y == -kInf ? x[n].m : fmaxf(x[n].m, y * a.c);
+          const float ms = mn == -kInf ? 0.f : mn, scale = exp2_fast(x[n].m - ms);
+          const float p = exp2_fast(__builtin_fmaf(y, a.c, -ms));
+          if (scale != 1.f) {
+            x[n].sum *= scale;
+            x[n].l *= scale;
+          }
+          x[n].sum += v * p;
+          x[n].l += p;
+          x[n].m = mn;
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n) store_state(c0 + n * CSTEP, d0, x[n]);
+  };
+  // beside the last page of an odd number: the same one, of no row
+  auto pad = [&](int total, int i, int4 e) {
+    if (i == total - 1 && total & 1) lds.page[total] = int4{e.x, e.y, 0, 0};
+  };
+  // Pages base .. base + kPassPages - 1 of row t's list, up to page1; how many.
+  auto list_pages = [&](int t, int base, int page1) {
+    const int32_t* list = list_of(t);
+    const int pos = pos0 + t;
+    int4 mine[2];
     uint64_t mask[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int p = base + i * kSparseThreads + tid;
-      mine[i] = int2{0, 0};
+      mine[i] = int4{0, 0, 0, 0};
       if (p < page1) {
-        const int b = blocks[p >> log_pages];
-        if (b >= 0 && b <= r.pos >> a.log_block) {
-          const int at = (b << log_pages) + (p & ((1 << log_pages) - 1));  // page of the request
-          if (at * 16 <= r.pos) mine[i] = int2{table[at], min(16, r.pos + 1 - at * 16)};
+        const int b = list[p >> log_pages];
+        if (b >= 0 && b <= pos >> a.log_block) {
+          const int at = (b << log_pages) + (p & ((1 << log_pages) - 1));
+          if (at * 16 <= pos) mine[i] = int4{table[at], at * 16, 1 << t, 0};
         }
       }
-      mask[i] = __ballot(mine[i].y > 0);
+      mask[i] = __ballot(mine[i].z != 0);
       if (lane == 0) lds.part[i][wave] = (int)__popcll(mask[i]);
     }
     __syncthreads();
@@ -494,215 +839,222 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (mine[i].y > 0) {
+      if (mine[i].z) {
         lds.page[at[i]] = mine[i];
-        // beside the last one of an odd number: the same page, none of its slots
-        if (at[i] == total - 1 && total & 1) lds.page[total] = int2{mine[i].x, 0};
+        pad(total, at[i], mine[i]);
       }
+    if (total > 0) seen |= 1u << t;
+    return __builtin_amdgcn_readfirstlane(total);
+  };
+  // The union's masks; a thread's words of them, how many blocks earlier threads have, and all
+  // of its pages.  -1: a list names a block twice.
+  int word0 = 0, word1 = 0, before = 0;
+  auto make_union = [&] {
+    const int blocks = (last >> a.log_block) + 1;
+    if (tid < 2) lds.flag[tid] = 0;
+    for (int i = tid; i < (blocks + 1) / 2; i += kSparseThreads) lds.mask[i] = 0;
     __syncthreads();
-    total = __builtin_amdgcn_readfirstlane(total);
-    if (total == 0) continue;
-    any = true;
-    const int steps = (total + 1) / 2;
-    auto pages = [&](int s, int* p0, int* p1) {
-      *p0 = __builtin_amdgcn_readfirstlane(lds.page[2 * s].x);
-      *p1 = __builtin_amdgcn_readfirstlane(lds.page[2 * s + 1].x);
-    };
-    int p0 = 0, p1 = 0;
-    if (wave < steps) {
-      pages(wave, &p0, &p1);
-      load_keys(p0, p1);
-      load_values(p0, p1);
+#pragma unroll 4
+    for (int i = tid; i < rows * a.top; i += kSparseThreads) {
+      const int t = i / a.top, b = list_of(t)[i - t * a.top];
+      if (b < 0 || b > (pos0 + t) >> a.log_block) continue;
+      const uint32_t bit = 1u << (t + 16 * (b & 1));
+      if (atomicOr(&lds.mask[b >> 1], bit) & bit) lds.flag[0] = 1;
     }
-    for (int s = wave; s < steps; s += 4) {
-      const bool more = s + 4 < steps;
-      if (more) pages(s + 4, &p0, &p1);
-      const int c0 = __builtin_amdgcn_readfirstlane(lds.page[2 * s].y);
-      const int c1 = __builtin_amdgcn_readfirstlane(lds.page[2 * s + 1].y);
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        s0 = mfma(as_bf16x8(kf[0][k]), qf[k], s0);
-        s1 = mfma(as_bf16x8(kf[1][k]), qf[k], s1);
-      }
-      if (more) load_keys(p0, p1);
-      __builtin_amdgcn_sched_barrier(0);
-      float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-      const bool cut = c0 + c1 < 32;
-      const int nv = (quad >> 1 ? c1 : c0) - 8 * (quad & 1);  // this lane's keys that count
-      if (cut) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i >= nv) x[i] = -kInf;
-      }
-      float mx = x[0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = mx == -kInf ? m : fmaxf(m, mx * a.c);
-      const float ms = mn == -kInf ? 0.f : mn;
-      const float alpha = exp2_fast(m - ms);
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = exp2_fast(__builtin_fmaf(x[i], a.c, -ms));
-      if (cut) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i >= nv) p[i] = 0.f;  // scale 0 times -inf is NaN
-      }
-      l = l * alpha + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-      m = mn;
-      // A weight enters the matrix product as three bf16 values, the rounded one and what
-      // that misses twice over: all of its 24 bits.
-      u32x4 part[3];
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float x0 = p[2 * w], x1 = p[2 * w + 1];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          part[i][w] = pack2(x0, x1);
-          x0 -= bf16_lo(part[i][w]);
-          x1 -= bf16_hi(part[i][w]);
-        }
-      }
-      if (__any(alpha != 1.f)) {
-#pragma unroll
-        for (int t = 0; t < DT; ++t) o[t] *= alpha;
-      }
-      if (cut) {
-        // a slot that does not count may hold anything, and 0 times NaN is NaN
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            if (2 * w >= nv) vf[t][w] = 0;
-            else if (2 * w + 1 >= nv) vf[t][w] &= 0xFFFFu;
-          }
-      }
-#pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[0]), o[t]);
-      // An infinite value times a part that is zero or negative is not what it is times
-      // the weight: the rounded weight alone has it.
-      uint32_t most = 0;
-#pragma unroll
-      for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) most = max_halves(most, vf[t][w] & kMagnitudes);
-      if (__any((most & 0xFFFFu) >= kInfBits || most >> 16 >= kInfBits)) {
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t v = vf[t][w] & kMagnitudes;
-            if ((v & 0xFFFFu) >= kInfBits) vf[t][w] &= 0xFFFF0000u;
-            if (v >> 16 >= kInfBits) vf[t][w] &= 0xFFFFu;
-          }
-      }
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[1]), o[t]);
-        o[t] = mfma(as_bf16x8(vf[t]), as_bf16x8(part[2]), o[t]);
-      }
-      if (more) load_values(p0, p1);
-      __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    if (lds.flag[0]) return -1;
+    const int per = (blocks + 2 * kSparseThreads - 1) / (2 * kSparseThreads);
+    word0 = tid * per;
+    word1 = min(word0 + per, (blocks + 1) / 2);
+    int n = 0;
+    uint32_t mine = 0;
+    for (int i = word0; i < word1; ++i) {
+      const uint32_t x = lds.mask[i];
+      n += ((x & 0xFFFFu) != 0) + (x >> 16 != 0);
+      mine |= x | x >> 16;
     }
-    __syncthreads();  // the pages have been read
+    before = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(before, d, 64);
+      if (lane >= d) before += y;
+      mine |= __shfl_xor(mine, d, 64);
+    }
+    if (lane == 63) {
+      lds.part[0][wave] = before;
+      atomicOr(&lds.flag[1], (int)(mine & 0xFFFFu));
+    }
+    __syncthreads();
+    int total = 0;
+    before -= n;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += lds.part[0][w];
+      total += lds.part[0][w];
+    }
+    seen = lds.flag[1];  // whatever this workgroup's share
+    return __builtin_amdgcn_readfirstlane(total) << log_pages;
+  };
+  // `pages` pages of the union from page `base` on.
+  auto union_pages = [&](int base, int pages) {
+    const int b0 = base >> log_pages, b1 = (base + pages - 1) >> log_pages;
+    int at = before;
+    for (int i = word0; i < word1; ++i) {
+      const uint32_t x = lds.mask[i];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int rows_of = (int)(x >> (16 * h) & 0xFFFFu);
+        if (!rows_of) continue;
+        if (at >= b0 && at <= b1) lds.block[at - b0] = int2{2 * i + h, rows_of};
+        ++at;
+      }
+    }
+    __syncthreads();
+    for (int i = tid; i < pages; i += kSparseThreads) {
+      const int p = base + i;
+      const int2 b = lds.block[(p >> log_pages) - b0];
+      // a page behind the last row's position: that one's, of no row
+      const int page = (b.x << log_pages) + (p & ((1 << log_pages) - 1));
+      const bool here = page * 16 <= last;
+      const int4 e = {table[here ? page : last / 16], (here ? page : last / 16) * 16,
+                      here ? b.y : 0, 0};
+      lds.page[i] = e;
+      pad(pages, i, e);
+    }
+    return pages;
+  };
+  for (bool finite = true;; finite = false) {
+    {
+      const auto [c0, d0] = place();
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        store_state(c0 + i * CSTEP, d0, State{-kInf, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}});
+    }
+    seen = 0;
+    __syncthreads();
+    // this workgroup's pages of the union, as many steps to every wave, or of each row's list
+    int share = -1, base, end, t = rows - 1;
+    if (rows > 1 && (last >> a.log_block) < kMaskBlocks) share = make_union();
+    const bool joint = share >= 0;
+    if (joint) {
+      const int total = share;
+      if (a.nsplit > 1) share = ((total + a.nsplit - 1) / a.nsplit + 7) / 8 * 8;
+      base = min(total, split * share);
+      end = min(total, base + share);
+    } else {
+      t = 0;
+      base = split * a.split_entries << log_pages;
+      end = min(a.top, (split + 1) * a.split_entries) << log_pages;
+    }
+    for (;;) {
+      if (base >= end) {
+        if (++t >= rows) break;
+        base = split * a.split_entries << log_pages;
+      }
+      const int total = joint ? union_pages(base, min(kPassPages, end - base)) : list_pages(t, base, end);
+      __syncthreads();
+      if (finite && columns <= 16)
+        multiply(total, std::integral_constant<int, 1>{});
+      else if (finite)
+        multiply(total, std::integral_constant<int, 2>{});
+      else
+        go_through(total);
+      __syncthreads();  // the pages and sums have been read
+      base += kPassPages;
+    }
+    if (!finite) break;
+    float zero = 0.f;
+    const auto [c0, d0] = place();
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int c = c0 + i * CSTEP;
+      const State x = load_state(c, d0);
+      if (c < columns)
+        zero += x.l * 0.f + (x.sum[0] * 0.f + x.sum[1] * 0.f) + (x.sum[2] * 0.f + x.sum[3] * 0.f);
+    }
+    if (tid == 0) lds.flag[0] = 0;
+    __syncthreads();
+    if (__any(zero != 0.f) && lane == 0) lds.flag[0] = 1;
+    __syncthreads();
+    if (!lds.flag[0]) break;
+    __syncthreads();
   }
 
-  // join the waves
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (quad == 0) {
-    lds.ml[0][wave][r16] = m;
-    lds.ml[1][wave][r16] = l;
-  }
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-    *reinterpret_cast<f32x4*>(lds.o + (wave * 16 + r16) * D + t * 16 + 4 * quad) = o[t];
-  __syncthreads();
-  const int rec_floats = sparse_rec_floats(a.g, D), rec_o = sparse_rec_o(a.g);
-  float* records = a.nsplit > 1 ? a.records + list * a.nsplit * rec_floats : nullptr;
-  if (tid < 16) {
-    float mm = -kInf, ll = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, lds.ml[0][w][tid]);
-    const float ms = mm == -kInf ? 0.f : mm;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) ll += lds.ml[1][w][tid] * exp2_fast(lds.ml[0][w][tid] - ms);
-    // no key: zeros; keys whose logits are all -infinity have no weights
-    lds.m[tid] = ms;
-    lds.inv[tid] = mm != -kInf ? 1.f / ll : any ? __builtin_nanf("") : 0.f;
-    if (a.nsplit > 1 && tid < a.g) {
-      float* rec = records + (int64_t)split * rec_floats;
-      if (mm == -kInf && any) ll = 1.f;
-      __hip_atomic_store(rec + tid, mm, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(rec + a.g + tid, ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-  }
-  __syncthreads();
-  auto joined = [&](int g, int d) {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-      v += *reinterpret_cast<const f32x4*>(lds.o + (w * 16 + g) * D + d) *
-           exp2_fast(lds.ml[0][w][g] - lds.m[g]);
-    return v;
+  const auto [c0, d0] = place();
+  const int cols = a.tokens * a.g;  // of a record
+  const int rec_floats = sparse_rec_floats(cols, D), rec_o = sparse_rec_o(cols);
+  const int ticket = unit * a.hkv + kvh;
+  auto store = [&, d0 = d0](int c, f32x4 v) {
+    *reinterpret_cast<u32x2*>(a.out + row_of(c) + d0) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
   };
-  uint16_t* out = a.out + ((size_t)r.row * a.hq + kvh * a.g) * D;
-  auto store = [&](int e, f32x4 v) {
-    *reinterpret_cast<u32x2*>(out + e) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+  // no key: zeros; keys whose logits are all -infinity have no weights
+  auto inverse = [&](float m, float l, bool any) {
+    return m != -kInf ? 1.f / l : any ? __builtin_nanf("") : 0.f;
   };
   if (a.nsplit == 1) {
-    for (int e = tid * 4; e < a.g * D; e += kSparseThreads * 4)
-      store(e, joined(e / D, e % D) * lds.inv[e / D]);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int c = c0 + i * CSTEP;
+      const State x = load_state(c, d0);
+      if (c < columns) store(c, x.sum * inverse(x.m, x.l, seen >> token_of(c) & 1));
+    }
     return;
   }
   // A piece: its record goes past this die's cache (device scope) and has arrived before
   // the ticket is taken; the last piece to finish joins all of them in their order.
-  {
-    const PartWriter write(records + (int64_t)split * rec_floats + rec_o);
-    for (int e = tid * 4; e < a.g * D; e += kSparseThreads * 4)
-      write(e * 4, __builtin_bit_cast(u32x4, joined(e / D, e % D)));
+  float* const records = a.records + (size_t)ticket * a.nsplit * rec_floats;
+  float* const rec = records + (int64_t)split * rec_floats;
+  const PartWriter write(rec + rec_o);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int c = c0 + i * CSTEP;
+    if (c >= columns) continue;
+    const State x = load_state(c, d0);
+    write((c * D + d0) * 4, __builtin_bit_cast(u32x4, x.sum));
+    if (d0 == 0) {
+      const bool any = seen >> token_of(c) & 1;
+      const float l = x.m != -kInf ? x.l : any ? 1.f : 0.f;
+      __hip_atomic_store(rec + c, x.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(rec + cols + c, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
   }
   vm_wait<0>();
   __syncthreads();
   if (tid == 0) {
-    const int before = __hip_atomic_fetch_add(a.tickets + list, 1, __ATOMIC_RELAXED,
-                                              __HIP_MEMORY_SCOPE_AGENT);
-    lds.last = before == a.nsplit - 1;
-    if (lds.last)
-      __hip_atomic_store(a.tickets + list, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int earlier = __hip_atomic_fetch_add(a.tickets + ticket, 1, __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    lds.flag[0] = earlier == a.nsplit - 1;
+    if (lds.flag[0])
+      __hip_atomic_store(a.tickets + ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if (!lds.last) return;
-  auto get = [&](int64_t at) {
-    return __hip_atomic_load(records + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
-  // weights of the pieces, then their sums
-  float* weight = lds.o;  // [G][nsplit]
-  if (tid < a.g) {
-    float mm = -kInf, ll = 0.f, some = 0.f;
-    for (int s = 0; s < a.nsplit; ++s) mm = fmaxf(mm, get((int64_t)s * rec_floats + tid));
-    const float ms = mm == -kInf ? 0.f : mm;
-    for (int s = 0; s < a.nsplit; ++s) {
-      const float w = exp2_fast(get((int64_t)s * rec_floats + tid) - ms);
-      const float ls = get((int64_t)s * rec_floats + a.g + tid);
-      weight[tid * a.nsplit + s] = w;
-      ll += ls * w;
-      some += ls;
-    }
-    lds.inv[tid] = mm != -kInf ? 1.f / ll : some > 0.f ? __builtin_nanf("") : 0.f;
+  if (!lds.flag[0]) return;
+  // m and l of all pieces, their weights, then the sums
+  for (int e = tid; e < a.nsplit * 2 * columns; e += kSparseThreads) {
+    const int s = e / (2 * columns), i = e - s * 2 * columns;
+    lds.weight[e] =
+        __hip_atomic_load(records + (int64_t)s * rec_floats + (i < columns ? i : cols + i - columns),
+                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  for (int e = tid * 4; e < a.g * D; e += kSparseThreads * 4) {
+  const PartReader read(records);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int c = c0 + i * CSTEP;
+    if (c >= columns) continue;
+    const float* const w = lds.weight + c;
+    float m = -kInf, l = 0.f, some = 0.f;
+    for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, w[s * 2 * columns]);
+    const float ms = m == -kInf ? 0.f : m;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int s = 0; s < a.nsplit; ++s) {
-      const float w = weight[e / D * a.nsplit + s];
-      const int64_t at = (int64_t)s * rec_floats + rec_o + e;
-      v += f32x4{get(at), get(at + 1), get(at + 2), get(at + 3)} * w;
+      const float f = exp2_fast(w[s * 2 * columns] - ms), ls = w[s * 2 * columns + columns];
+      l += ls * f;
+      some += ls;
+      v += read((s * rec_floats + rec_o + c * D + d0) * 4) * f;
     }
-    store(e, v * lds.inv[e / D]);
+    store(c, v * inverse(m, l, some > 0.f));
   }
 }
 
@@ -753,6 +1105,9 @@ SparseArgs sparse_args(const SparseHeader* h, const void* plan_dev) {
   a.max_blocks = h->max_blocks;
   a.nsplit = h->nsplit;
   a.split_entries = h->split_entries;
+  a.tokens = sparse_tokens(a.g);
+  a.subs = sparse_subs(a.g);
+  a.g_magic = (65536 + a.g - 1) / a.g;  // x / g for x < 32: (x g_magic) >> 16
   a.c = h->softmax_scale * 1.44269504088896340736f;
   return a;
 }
@@ -766,6 +1121,17 @@ int launch_summary(const SummaryArgs& a, void* stream) {
     case 32: return launch(block_summary_kernel<D, 32>, a, kSparseThreads, stream);
     case 64: return launch(block_summary_kernel<D, 64>, a, kSparseThreads, stream);
     default: return launch(block_summary_kernel<D, 128>, a, kSparseThreads, stream);
+  }
+}
+
+template <int D>
+int launch_scores(const SparseArgs& a, void* stream) {
+  switch (log2_of(2 * a.g - 1)) {
+    case 0: return launch(block_scores_kernel<D, 0>, a, kSparseThreads, stream);
+    case 1: return launch(block_scores_kernel<D, 1>, a, kSparseThreads, stream);
+    case 2: return launch(block_scores_kernel<D, 2>, a, kSparseThreads, stream);
+    case 3: return launch(block_scores_kernel<D, 3>, a, kSparseThreads, stream);
+    default: return launch(block_scores_kernel<D, 4>, a, kSparseThreads, stream);
   }
 }
 
@@ -797,7 +1163,10 @@ int ssa_block_summary(const ssa_shape* shape, const void* plan_host, const void*
   a.bt = block_table;
   a.summary = summary;
   a.head_groups = (h->hkv + 3) / 4;
-  const int64_t wgs = (int64_t)h->num_segments * a.head_groups;
+  a.num_chunk_segments = h->num_chunk_segments;
+  a.num_runs = (h->num_chunk_segments + block_keys / 16 - 1) / (block_keys / 16);
+  const int64_t wgs =
+      ((int64_t)a.num_runs + h->num_segments - h->num_chunk_segments) * a.head_groups;
   if (wgs > INT32_MAX) return SSA_ERR_ARG;
   a.workgroups = (int32_t)wgs;
   return h->head_dim == 128 ? launch_summary<128>(a, stream) : launch_summary<64>(a, stream);
@@ -819,8 +1188,7 @@ int ssa_block_scores(const ssa_shape* shape, const void* plan_host, const void* 
   a.summary = summary;
   a.bt = block_table;
   a.scores = scores;
-  return h->head_dim == 128 ? launch(block_scores_kernel<128>, a, kSparseThreads, stream)
-                            : launch(block_scores_kernel<64>, a, kSparseThreads, stream);
+  return h->head_dim == 128 ? launch_scores<128>(a, stream) : launch_scores<64>(a, stream);
 }
 
 int ssa_block_select(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
@@ -836,10 +1204,16 @@ int ssa_block_select(const ssa_shape* shape, const void* plan_host, const void* 
   a.workgroups = rows_of(h) * h->hkv;
   a.scores_in = scores;
   a.blocks = blocks;
-  // the longest list's waves and registers
-  if (h->most_blocks <= 512) return launch(block_select_kernel<1, 8>, a, 64, stream);
-  if (h->most_blocks <= 2048) return launch(block_select_kernel<4, 8>, a, 256, stream);
-  if (h->most_blocks <= 8192) return launch(block_select_kernel<16, 8>, a, 1024, stream);
+  // the longest list's waves and registers: one wave where the lists fill the chip, several
+  // where there are few
+  const bool many = (int64_t)h->num_tokens * h->hkv >= 1024;
+  const int32_t most = h->most_blocks;
+  if (most <= 512) return launch(block_select_kernel<1, 8>, a, 64, stream);
+  if (most <= 1024 && many) return launch(block_select_kernel<1, 16>, a, 64, stream);
+  if (most <= 1024) return launch(block_select_kernel<4, 4>, a, 256, stream);
+  if (most <= 2048 && many) return launch(block_select_kernel<1, 32>, a, 64, stream);
+  if (most <= 2048) return launch(block_select_kernel<4, 8>, a, 256, stream);
+  if (most <= 8192) return launch(block_select_kernel<16, 8>, a, 1024, stream);
   return launch(block_select_kernel<16, 32>, a, 1024, stream);
 }
 
@@ -857,7 +1231,7 @@ int ssa_sparse_attention(const ssa_shape* shape, const void* plan_host, const vo
   if (misaligned({q, k_cache, v_cache, blocks, out, workspace}) || misaligned_plan(plan_dev))
     return SSA_ERR_ARG;
   SparseArgs a = sparse_args(h, plan_dev);
-  a.workgroups = rows_of(h) * h->hkv * h->nsplit;
+  a.workgroups = (h->num_groups * a.subs + h->num_singles) * h->hkv * h->nsplit;
   a.q = q;
   a.kc = k_cache;
   a.vc = v_cache;

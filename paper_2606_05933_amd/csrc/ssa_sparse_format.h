@@ -61,9 +61,13 @@ struct SparseScore {
 };
 static_assert(sizeof(SparseScore) == 32, "score item size");
 
-// One piece's record of a row and kv head: m and l for G heads, padded to four floats,
-// then o [G][D].
-constexpr int sparse_rec_o(int g) { return (2 * g + 3) / 4 * 4; }
-constexpr int sparse_rec_floats(int g, int d) { return sparse_rec_o(g) + g * d; }
+// Rows of a chunk record that an attention workgroup takes, 32 columns (row, head of the
+// group) at most, and workgroups of a record.
+constexpr int sparse_tokens(int g) { return 32 / g < kRowGroup ? 32 / g : kRowGroup; }
+constexpr int sparse_subs(int g) { return (kRowGroup + sparse_tokens(g) - 1) / sparse_tokens(g); }
+// One piece's record of a workgroup's rows and kv head: m and l for `cols` columns (row,
+// head of the group), padded to four floats, then o [cols][D].
+constexpr int sparse_rec_o(int cols) { return (2 * cols + 3) / 4 * 4; }
+constexpr int sparse_rec_floats(int cols, int d) { return sparse_rec_o(cols) + cols * d; }
 
 }  // namespace ssa

@@ -19,8 +19,13 @@ constexpr int64_t kMaxLen = 1 << 30;
 constexpr int64_t kMaxQueryRow = 1 << 24;
 // Workgroups that a launch should have, at least: four on each of 256 compute units.
 constexpr int64_t kFillGroups = 1024;
+// And of attention: two on each, which its registers allow.  (32 decode rows of 4096 keys, 64/8
+// heads: 116, 105, 117 and 109 us in lists cut for 256, 512, 768 and 1024 workgroups, 8
+// such rows 28, 32 and 35 in those for 512, 768 and 1024.)
+constexpr int64_t kAttentionGroups = 512;
 // Keys of a piece of a row's list, at least: 32 for each of four waves, twice.
 constexpr int64_t kPieceKeys = 256;
+constexpr int64_t kMaxScoreRow = 1 << 24;
 constexpr int kMaxScoreTiles = 16;
 constexpr int64_t kMaxSplits = 64;  // pieces of a list: one workgroup joins them
 
@@ -78,7 +83,8 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
 
   // Score items: a chunk's are 128 blocks by as many 16-column tiles (tokens x heads of
   // a group) as leave enough workgroups; a decode row's as many passes of 128 blocks.
-  const int64_t tokens_per_tile = 16 / g;
+  int64_t tokens_per_tile = 16;
+  while (tokens_per_tile * g > 16) tokens_per_tile /= 2;  // heads padded to a power of two
   auto chunk_items = [&](int64_t tiles) {
     int64_t items = 0;
     for (int32_t i = 0; i < n; ++i)
@@ -90,7 +96,7 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
     return items;
   };
   int64_t tiles = kMaxScoreTiles;
-  while (tiles > 1 && groups > 0 && chunk_items(tiles) * hkv < kFillGroups) tiles /= 2;
+  while (tiles > 1 && groups > 0 && chunk_items(tiles) * hkv < kFillGroups / 2) tiles /= 2;
   const int64_t passes = std::max<int64_t>(1, single_passes * hkv / (2 * kFillGroups));
   // nothing is built that would not fit
   const int64_t max_scores = (groups > 0 ? chunk_items(tiles) : 0) + single_passes;
@@ -125,13 +131,14 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
 
   SparseHeader& h = p->hdr;
   std::memset(&h, 0, sizeof h);
-  // The lists are cut only where the rows are too few for the compute units, so that the
-  // tickets of cut lists always fit.
-  const int64_t lists = tokens * hkv;
+  // The lists are cut only where the workgroups are too few for the compute units, so that
+  // the tickets of cut lists always fit.
+  const int64_t units = (int64_t)p->groups.size() * sparse_subs(g) + (int64_t)p->singles.size();
+  const int64_t lists = units * hkv;
   int64_t entries = top;
-  if (lists > 0 && lists < kFillGroups)
+  if (lists > 0 && lists < kAttentionGroups)
     entries = std::min(top, std::max(std::max(ceil_div(kPieceKeys, bk), ceil_div(top, kMaxSplits)),
-                                     ceil_div(top * lists, kFillGroups)));
+                                     ceil_div(top * lists, kAttentionGroups)));
   h.split_entries = (int32_t)entries;
   h.nsplit = (int32_t)ceil_div(top, entries);
   h.magic = kSparseMagic;
@@ -157,12 +164,14 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
   h.off_scores = (int32_t)off_scores;
   h.score_tiles = (int32_t)tiles;
   h.plan_bytes = off_scores + (int64_t)p->scores.size() * (int64_t)sizeof(SparseScore);
+  // 16 rows of scores are within a 32-bit byte offset
+  if ((int64_t)hkv * h.max_blocks > kMaxScoreRow) return SSA_ERR_LENGTH;
   // workgroups of a launch
   if ((int64_t)h.num_scores * hkv > INT32_MAX ||
-      ((int64_t)h.num_groups * kRowGroup + h.num_singles) * hkv * h.nsplit > INT32_MAX)
+      std::max(((int64_t)h.num_groups * kRowGroup + h.num_singles) * hkv, lists * h.nsplit) > INT32_MAX)
     return SSA_ERR_LENGTH;
   h.ws_bytes = kSparseTickets * 4;
-  if (h.nsplit > 1) h.ws_bytes += lists * h.nsplit * (int64_t)sparse_rec_floats(g, d) * 4;
+  if (h.nsplit > 1) h.ws_bytes += lists * h.nsplit * (int64_t)sparse_rec_floats(sparse_tokens(g) * g, d) * 4;
   uint64_t hv = 1469598103934665603ull;
   const int32_t f[10] = {s->num_q_heads,         s->num_kv_heads, s->head_dim,     s->page_size,
                          s->num_pages,           s->max_pages_per_req, cfg->block_keys,
