@@ -136,6 +136,47 @@ int ssa_sparse_attention(const ssa_shape* shape, const void* plan_host, const vo
                          const int32_t* block_table, const int32_t* blocks, uint16_t* out,
                          void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * What a decoder layer does for long contexts.  Each part may be left out (NULL).
+ *   rope      as ssa_rope_append_as: the layer's cos_sin has rows of rope->rotary_dim then
+ *   shift_host, shift_dev   as ssa_rope_append_shifted (ssa_evict.h)
+ *   summary, block_keys     after RoPE and append, ssa_block_summary of the new keys
+ *   plan_host, plan_dev     ssa_sparse_plan of the same batch as the layer's plan: its rows
+ *            attend over the blocks that they select (ssa_block_scores, ssa_block_select,
+ *            ssa_sparse_attention), not over all keys.  Then summary (of the plan's
+ *            block_keys), scores, blocks and the workspace have to be there; scores and blocks
+ *            hold what the two calls gave.  Without, attention is ssa_mixed_attention: a
+ *            prompt may run so, with its summaries kept for the rows that follow.
+ *   workspace ssa_sparse_attention's, not the layer's
+ */
+typedef struct ssa_layer_sparse {
+  const ssa_rope_form* rope;
+  const int32_t* shift_host;
+  const int32_t* shift_dev;
+  uint16_t* summary;
+  const void* plan_host;
+  const void* plan_dev;
+  float* scores;
+  int32_t* blocks;
+  void* workspace;
+  size_t ws_bytes;
+  int32_t block_keys;
+} ssa_layer_sparse;
+
+/*
+ * ssa_layer_forward with `sparse`'s parts, in the same launches but for RoPE and attention.
+ * Without any of them, out and the caches are bit for bit those of ssa_layer_forward.
+ * Everything is validated before the first launch.
+ * Errors: those of ssa_layer_forward and of the calls that stand for the parts; NULL
+ * (sparse); ARG also where block_keys is not the plan's; PLAN_MISMATCH also where the two
+ * plans are not of the same batch (q_len and ctx_len of every request).
+ */
+int ssa_layer_forward_sparse(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                             const ssa_layer_weights* w, const ssa_layer_sparse* sparse,
+                             const uint16_t* x, uint16_t* out, uint16_t* k_cache, uint16_t* v_cache,
+                             const int32_t* block_table, void* workspace, size_t ws_bytes,
+                             void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,7 @@
 #include "../../include/ssa_evict.h"
 #include "../../include/ssa_layer.h"
 #include "ssa_device.h"
+#include "ssa_layer_internal.h"
 #include "ssa_plan_format.h"
 
 namespace ssa {
@@ -281,12 +282,12 @@ __global__ __launch_bounds__(kLayerThreads) void rope_append_kernel(RopeArgs a) 
 
 }  // namespace
 
-namespace {
-
-bool rope_form_ok(const ssa_rope_form& f, int32_t head_dim) {
+bool ssa::rope_form_ok(const ssa_rope_form& f, int32_t head_dim) {
   return (f.layout == SSA_ROPE_HALF || f.layout == SSA_ROPE_INTERLEAVED) && f.rotary_dim >= 16 &&
          f.rotary_dim <= head_dim && f.rotary_dim % 16 == 0;
 }
+
+namespace {
 
 template <int D>
 void launch_rope(RopeForm form, dim3 grid, hipStream_t stream, const RopeArgs& a) {

@@ -9,9 +9,11 @@
 
 #include "../../include/ssa_evict.h"
 #include "../../include/ssa_layer.h"
+#include "../../include/ssa_sparse.h"
 #include "ssa_evict_format.h"
 #include "ssa_layer_internal.h"
 #include "ssa_plan_format.h"
+#include "ssa_sparse_format.h"
 
 namespace ssa {
 int check_plan(const ssa_shape* s, const void* plan_host, const PlanHeader** out);
@@ -77,10 +79,10 @@ int layer_ws(const ssa_shape* shape, const void* plan_host, const ssa_layer_weig
   return SSA_OK;
 }
 
-// e: the parts of ssa_layer_forward_evicting, or null.
+// e: the parts of ssa_layer_forward_evicting, sp: of ssa_layer_forward_sparse; or null.
 int layer_forward(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
-                  const ssa_layer_weights* w, const ssa_layer_eviction* e, const uint16_t* x,
-                  uint16_t* out, uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
+                  const ssa_layer_weights* w, const ssa_layer_eviction* e,
+                  const ssa_layer_sparse* sp, const uint16_t* x, uint16_t* out, uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
                   void* workspace, size_t ws_bytes, void* stream) {
   const PlanHeader* h = nullptr;
   LayerWs l;
@@ -89,9 +91,12 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
   if (!plan_dev) return SSA_ERR_NULL;
   const ReqEntry* reqs =
       reinterpret_cast<const ReqEntry*>(static_cast<const uint8_t*>(plan_host) + h->off_reqs);
-  const int32_t* shift = e ? e->shift_host : nullptr;
+  const int32_t* shift = e ? e->shift_host : sp ? sp->shift_host : nullptr;
+  const int32_t* shift_dev = e ? e->shift_dev : sp ? sp->shift_dev : nullptr;
   const void* const score_plan = e ? e->score_plan_host : nullptr;
-  if (e && (!e->shift_host != !e->shift_dev)) return SSA_ERR_NULL;
+  const void* const sparse_plan = sp ? sp->plan_host : nullptr;
+  if (!shift != !shift_dev) return SSA_ERR_NULL;
+  if (sp && sp->rope && !rope_form_ok(*sp->rope, h->head_dim)) return SSA_ERR_ARG;
   for (int32_t i = 0; i < h->num_reqs; ++i) {
     if (reqs[i].q_len <= 0) continue;
     const int64_t s = shift ? shift[i] : 0;
@@ -108,6 +113,18 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
       if (scored[i].q_len != reqs[i].q_len || scored[i].ctx_len != reqs[i].ctx_len)
         return SSA_ERR_PLAN_MISMATCH;
   }
+  if (sparse_plan) {
+    const SparseHeader* sh = nullptr;
+    if ((rc = check_sparse_plan(shape, sparse_plan, &sh))) return rc;
+    if (sh->num_reqs != h->num_reqs) return SSA_ERR_PLAN_MISMATCH;
+    const SparseReq* of = reinterpret_cast<const SparseReq*>(
+        static_cast<const uint8_t*>(sparse_plan) + sizeof(SparseHeader));
+    for (int32_t i = 0; i < h->num_reqs; ++i)
+      if (of[i].q_len != reqs[i].q_len || of[i].ctx_len != reqs[i].ctx_len)
+        return SSA_ERR_PLAN_MISMATCH;
+    if (!sp->summary) return SSA_ERR_NULL;
+    if (sp->block_keys != sh->block_keys) return SSA_ERR_ARG;
+  }
   if (t == 0) return SSA_OK;
   if (!x || !out || !k_cache || !v_cache || !block_table || !w->attn_norm || !w->w_qkv ||
       !w->w_o || !w->mlp_norm || !w->w_gate_up || !w->w_down || !w->cos_sin)
@@ -119,6 +136,19 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
                              k_cache, block_table, e->scores_in, e->decay, e->scores_out,
                              e->score_workspace, e->score_ws_bytes)))
     return rc;
+  if (sp && sp->summary &&
+      (rc = check_block_summary(shape, plan_host, plan_dev, sp->block_keys, k_cache, block_table,
+                                sp->summary)))
+    return rc;
+  if (sparse_plan) {
+    const char* const of = static_cast<const char*>(workspace);
+    if ((rc = check_sparse_calls(shape, sparse_plan, sp->plan_dev,
+                                 reinterpret_cast<const uint16_t*>(of + l.q), k_cache, v_cache,
+                                 sp->summary, block_table, sp->scores, sp->blocks,
+                                 reinterpret_cast<const uint16_t*>(of + l.a), sp->workspace,
+                                 sp->ws_bytes)))
+      return rc;
+  }
   char* ws = static_cast<char*>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
   uint16_t *xn = at(l.xn), *qkv = at(l.qkv), *q = at(l.q), *a = at(l.a), *hb = at(l.h),
@@ -136,19 +166,37 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
   if ((rc = ssa_linear(t, nqkv, hid, SSA_EPILOGUE_NONE, xn, w->w_qkv, nullptr, qkv, gws,
                        l.gemm_bytes, stream)))
     return rc;
-  rc = shift ? ssa_rope_append_shifted(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position,
-                                       shift, e->shift_dev, q, k_cache, v_cache, block_table, stream)
-             : ssa_rope_append(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position, q,
-                               k_cache, v_cache, block_table, stream);
+  if (sp && sp->rope)
+    rc = ssa_rope_append_as(shape, plan_host, plan_dev, sp->rope, qkv, w->cos_sin, w->max_position,
+                            shift, shift_dev, q, k_cache, v_cache, block_table, stream);
+  else
+    rc = shift ? ssa_rope_append_shifted(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position,
+                                         shift, shift_dev, q, k_cache, v_cache, block_table,
+                                         stream)
+               : ssa_rope_append(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position, q,
+                                 k_cache, v_cache, block_table, stream);
   if (rc) return rc;
+  if (sp && sp->summary &&
+      (rc = ssa_block_summary(shape, plan_host, plan_dev, sp->block_keys, k_cache, block_table,
+                              sp->summary, stream)))
+    return rc;
   if (score_plan &&
       (rc = ssa_key_scores(shape, score_plan, e->score_plan_dev, q, k_cache, block_table,
                            e->scores_in, e->decay, e->scores_out, e->score_workspace,
                            e->score_ws_bytes, stream)))
     return rc;
-  if ((rc = ssa_mixed_attention(shape, plan_host, plan_dev, q, k_cache, v_cache, block_table, a,
-                                ws + l.attn, l.attn_bytes, stream)))
+  if (sparse_plan) {
+    if ((rc = ssa_block_scores(shape, sparse_plan, sp->plan_dev, q, sp->summary, block_table,
+                               sp->scores, stream)) ||
+        (rc = ssa_block_select(shape, sparse_plan, sp->plan_dev, sp->scores, sp->blocks, stream)) ||
+        (rc = ssa_sparse_attention(shape, sparse_plan, sp->plan_dev, q, k_cache, v_cache,
+                                   block_table, sp->blocks, a, sp->workspace, sp->ws_bytes,
+                                   stream)))
+      return rc;
+  } else if ((rc = ssa_mixed_attention(shape, plan_host, plan_dev, q, k_cache, v_cache,
+                                       block_table, a, ws + l.attn, l.attn_bytes, stream))) {
     return rc;
+  }
   if ((rc = ssa_linear(t, hid, qd, SSA_EPILOGUE_RESIDUAL, a, w->w_o, x, hb, gws, l.gemm_bytes,
                        stream)))
     return rc;
@@ -221,7 +269,7 @@ int ssa_layer_forward(const ssa_shape* shape, const void* plan_host, const void*
                       const ssa_layer_weights* w, const uint16_t* x, uint16_t* out,
                       uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
                       void* workspace, size_t ws_bytes, void* stream) {
-  return layer_forward(shape, plan_host, plan_dev, w, nullptr, x, out, k_cache, v_cache,
+  return layer_forward(shape, plan_host, plan_dev, w, nullptr, nullptr, x, out, k_cache, v_cache,
                        block_table, workspace, ws_bytes, stream);
 }
 
@@ -231,7 +279,17 @@ int ssa_layer_forward_evicting(const ssa_shape* shape, const void* plan_host, co
                                uint16_t* v_cache, const int32_t* block_table, void* workspace,
                                size_t ws_bytes, void* stream) {
   if (!eviction) return SSA_ERR_NULL;
-  return layer_forward(shape, plan_host, plan_dev, w, eviction, x, out, k_cache, v_cache,
+  return layer_forward(shape, plan_host, plan_dev, w, eviction, nullptr, x, out, k_cache, v_cache,
+                       block_table, workspace, ws_bytes, stream);
+}
+
+int ssa_layer_forward_sparse(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                             const ssa_layer_weights* w, const ssa_layer_sparse* sparse,
+                             const uint16_t* x, uint16_t* out, uint16_t* k_cache, uint16_t* v_cache,
+                             const int32_t* block_table, void* workspace, size_t ws_bytes,
+                             void* stream) {
+  if (!sparse) return SSA_ERR_NULL;
+  return layer_forward(shape, plan_host, plan_dev, w, nullptr, sparse, x, out, k_cache, v_cache,
                        block_table, workspace, ws_bytes, stream);
 }
 

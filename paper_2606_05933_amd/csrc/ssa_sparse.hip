@@ -9,12 +9,12 @@
 
 #include "../../include/ssa_sparse.h"
 #include "ssa_device.h"
+#include "ssa_layer_internal.h"
 #include "ssa_plan_format.h"
 #include "ssa_sparse_format.h"
 
 namespace ssa {
 int check_plan(const ssa_shape* s, const void* plan_host, const PlanHeader** out);
-int check_sparse_plan(const ssa_shape* s, const void* plan_host, const SparseHeader** out);
 }  // namespace ssa
 
 namespace {
@@ -1114,6 +1114,14 @@ SparseArgs sparse_args(const SparseHeader* h, const void* plan_dev) {
 
 int32_t rows_of(const SparseHeader* h) { return h->num_groups * kRowGroup + h->num_singles; }
 
+int32_t summary_runs(const PlanHeader* h, int32_t block_keys) {
+  return (h->num_chunk_segments + block_keys / 16 - 1) / (block_keys / 16);
+}
+int64_t summary_workgroups(const PlanHeader* h, int32_t block_keys) {
+  return ((int64_t)summary_runs(h, block_keys) + h->num_segments - h->num_chunk_segments) *
+         ((h->hkv + 3) / 4);
+}
+
 template <int D>
 int launch_summary(const SummaryArgs& a, void* stream) {
   switch (a.block_keys) {
@@ -1137,11 +1145,9 @@ int launch_scores(const SparseArgs& a, void* stream) {
 
 }  // namespace
 
-extern "C" {
-
-int ssa_block_summary(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
-                      int32_t block_keys, const uint16_t* k_cache, const int32_t* block_table,
-                      uint16_t* summary, void* stream) {
+int ssa::check_block_summary(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                             int32_t block_keys, const uint16_t* k_cache,
+                             const int32_t* block_table, const uint16_t* summary) {
   const PlanHeader* h = nullptr;
   const int rc = check_plan(shape, plan_host, &h);
   if (rc) return rc;
@@ -1151,6 +1157,65 @@ int ssa_block_summary(const ssa_shape* shape, const void* plan_host, const void*
   if (h->num_segments == 0) return SSA_OK;
   if (!k_cache || !block_table || !summary) return SSA_ERR_NULL;
   if (misaligned({k_cache, summary}) || misaligned_plan(plan_dev)) return SSA_ERR_ARG;
+  return summary_workgroups(h, block_keys) > INT32_MAX ? SSA_ERR_ARG : SSA_OK;
+}
+
+namespace {
+
+int check_scores(const SparseHeader* h, const void* plan_dev, const uint16_t* q,
+                 const uint16_t* summary, const int32_t* block_table, const float* scores) {
+  if (!plan_dev) return SSA_ERR_NULL;
+  if (h->num_tokens == 0) return SSA_OK;
+  if (!q || !summary || !block_table || !scores) return SSA_ERR_NULL;
+  return misaligned({q, summary, scores}) || misaligned_plan(plan_dev) ? SSA_ERR_ARG : SSA_OK;
+}
+
+int check_select(const SparseHeader* h, const void* plan_dev, const float* scores,
+                 const int32_t* blocks) {
+  if (!plan_dev) return SSA_ERR_NULL;
+  if (h->num_tokens == 0) return SSA_OK;
+  if (!scores || !blocks) return SSA_ERR_NULL;
+  return misaligned({scores, blocks}) || misaligned_plan(plan_dev) ? SSA_ERR_ARG : SSA_OK;
+}
+
+int check_attention(const SparseHeader* h, const void* plan_dev, const uint16_t* q,
+                    const uint16_t* k_cache, const uint16_t* v_cache, const int32_t* block_table,
+                    const int32_t* blocks, const uint16_t* out, const void* workspace,
+                    size_t ws_bytes) {
+  if (!plan_dev) return SSA_ERR_NULL;
+  if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
+  if (h->num_tokens == 0) return SSA_OK;
+  if (!q || !k_cache || !v_cache || !block_table || !blocks || !out) return SSA_ERR_NULL;
+  return misaligned({q, k_cache, v_cache, blocks, out, workspace}) || misaligned_plan(plan_dev)
+             ? SSA_ERR_ARG
+             : SSA_OK;
+}
+
+}  // namespace
+
+int ssa::check_sparse_calls(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                            const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
+                            const uint16_t* summary, const int32_t* block_table,
+                            const float* scores, const int32_t* blocks, const uint16_t* out,
+                            const void* workspace, size_t ws_bytes) {
+  const SparseHeader* h = nullptr;
+  int rc = check_sparse_plan(shape, plan_host, &h);
+  if (rc || (rc = check_scores(h, plan_dev, q, summary, block_table, scores)) ||
+      (rc = check_select(h, plan_dev, scores, blocks)))
+    return rc;
+  return check_attention(h, plan_dev, q, k_cache, v_cache, block_table, blocks, out, workspace,
+                         ws_bytes);
+}
+
+extern "C" {
+
+int ssa_block_summary(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
+                      int32_t block_keys, const uint16_t* k_cache, const int32_t* block_table,
+                      uint16_t* summary, void* stream) {
+  const int rc =
+      check_block_summary(shape, plan_host, plan_dev, block_keys, k_cache, block_table, summary);
+  if (rc) return rc;
+  const PlanHeader* h = static_cast<const PlanHeader*>(plan_host);
   SummaryArgs a{};
   a.plan = static_cast<const uint8_t*>(plan_dev);
   a.hash = h->hash;
@@ -1164,11 +1229,8 @@ int ssa_block_summary(const ssa_shape* shape, const void* plan_host, const void*
   a.summary = summary;
   a.head_groups = (h->hkv + 3) / 4;
   a.num_chunk_segments = h->num_chunk_segments;
-  a.num_runs = (h->num_chunk_segments + block_keys / 16 - 1) / (block_keys / 16);
-  const int64_t wgs =
-      ((int64_t)a.num_runs + h->num_segments - h->num_chunk_segments) * a.head_groups;
-  if (wgs > INT32_MAX) return SSA_ERR_ARG;
-  a.workgroups = (int32_t)wgs;
+  a.num_runs = summary_runs(h, block_keys);
+  a.workgroups = (int32_t)summary_workgroups(h, block_keys);
   return h->head_dim == 128 ? launch_summary<128>(a, stream) : launch_summary<64>(a, stream);
 }
 
@@ -1176,12 +1238,8 @@ int ssa_block_scores(const ssa_shape* shape, const void* plan_host, const void* 
                      const uint16_t* q, const uint16_t* summary, const int32_t* block_table,
                      float* scores, void* stream) {
   const SparseHeader* h = nullptr;
-  const int rc = check_sparse_plan(shape, plan_host, &h);
-  if (rc) return rc;
-  if (!plan_dev) return SSA_ERR_NULL;
-  if (h->num_scores == 0) return SSA_OK;
-  if (!q || !summary || !block_table || !scores) return SSA_ERR_NULL;
-  if (misaligned({q, summary, scores}) || misaligned_plan(plan_dev)) return SSA_ERR_ARG;
+  int rc = check_sparse_plan(shape, plan_host, &h);
+  if (rc || (rc = check_scores(h, plan_dev, q, summary, block_table, scores))) return rc;
   SparseArgs a = sparse_args(h, plan_dev);
   a.workgroups = h->num_scores * h->hkv;
   a.q = q;
@@ -1194,12 +1252,8 @@ int ssa_block_scores(const ssa_shape* shape, const void* plan_host, const void* 
 int ssa_block_select(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                      const float* scores, int32_t* blocks, void* stream) {
   const SparseHeader* h = nullptr;
-  const int rc = check_sparse_plan(shape, plan_host, &h);
-  if (rc) return rc;
-  if (!plan_dev) return SSA_ERR_NULL;
-  if (h->num_tokens == 0) return SSA_OK;
-  if (!scores || !blocks) return SSA_ERR_NULL;
-  if (misaligned({scores, blocks}) || misaligned_plan(plan_dev)) return SSA_ERR_ARG;
+  int rc = check_sparse_plan(shape, plan_host, &h);
+  if (rc || (rc = check_select(h, plan_dev, scores, blocks))) return rc;
   SparseArgs a = sparse_args(h, plan_dev);
   a.workgroups = rows_of(h) * h->hkv;
   a.scores_in = scores;
@@ -1222,14 +1276,10 @@ int ssa_sparse_attention(const ssa_shape* shape, const void* plan_host, const vo
                          const int32_t* block_table, const int32_t* blocks, uint16_t* out,
                          void* workspace, size_t ws_bytes, void* stream) {
   const SparseHeader* h = nullptr;
-  const int rc = check_sparse_plan(shape, plan_host, &h);
-  if (rc) return rc;
-  if (!plan_dev) return SSA_ERR_NULL;
-  if (!workspace || ws_bytes < (size_t)h->ws_bytes) return SSA_ERR_WORKSPACE;
-  if (h->num_tokens == 0) return SSA_OK;
-  if (!q || !k_cache || !v_cache || !block_table || !blocks || !out) return SSA_ERR_NULL;
-  if (misaligned({q, k_cache, v_cache, blocks, out, workspace}) || misaligned_plan(plan_dev))
-    return SSA_ERR_ARG;
+  int rc = check_sparse_plan(shape, plan_host, &h);
+  if (rc || (rc = check_attention(h, plan_dev, q, k_cache, v_cache, block_table, blocks, out,
+                                  workspace, ws_bytes)))
+    return rc;
   SparseArgs a = sparse_args(h, plan_dev);
   a.workgroups = (h->num_groups * a.subs + h->num_singles) * h->hkv * h->nsplit;
   a.q = q;

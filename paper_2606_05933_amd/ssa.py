@@ -109,6 +109,12 @@ class SsaSparseConfig(ctypes.Structure):
                                               "recent_blocks")]
 
 
+class SsaLayerSparse(ctypes.Structure):
+    _fields_ = [("rope", ctypes.POINTER(SsaRopeForm))] + [(n, ctypes.c_void_p) for n in (
+        "shift_host", "shift_dev", "summary", "plan_host", "plan_dev", "scores", "blocks",
+        "workspace")] + [("ws_bytes", ctypes.c_size_t), ("block_keys", ctypes.c_int32)]
+
+
 class SsaLinearPlanInfo(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_m", "tile_n", "threads", "tiles_m", "tiles_n",
                                               "splits")]
@@ -242,6 +248,8 @@ def _load():
     lib.ssa_block_scores.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp]
     lib.ssa_block_select.argtypes = [P(SsaShape), vp, vp, vp, vp, vp]
     lib.ssa_sparse_attention.argtypes = [P(SsaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ssa_layer_forward_sparse.argtypes = [P(SsaShape), vp, vp, P(SsaLayerWeights),
+                                             P(SsaLayerSparse), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ssa_priority_sort.argtypes = [P(SsaCandidate), i32, ctypes.c_double, ctypes.c_double,
                                       ctypes.c_double, ip]
     lib.ssa_batch_constructor.argtypes = [P(SsaPredictor), ip, i32, P(SsaCandidate), i32, i32,
@@ -272,7 +280,7 @@ EXPORTED = ("ssa_status_string", "ssa_plan_size", "ssa_plan", "ssa_check_block_t
             "ssa_rope_append_shifted", "ssa_layer_forward_evicting", "ssa_rope_append_as",
             "ssa_rope_table_scaled", "ssa_pages_resize", "ssa_block_summary",
             "ssa_sparse_plan_size", "ssa_sparse_plan", "ssa_block_scores", "ssa_block_select",
-            "ssa_sparse_attention")
+            "ssa_sparse_attention", "ssa_layer_forward_sparse")
 
 EPILOGUE_NONE, EPILOGUE_RESIDUAL, EPILOGUE_SWIGLU = 0, 1, 2
 
@@ -711,10 +719,11 @@ def interleave_gate_up(w_gate, w_up):
 class LayerWeights:
     """Device copies of one decoder layer's weights in the layout of
     ssa_layer_forward (q/k/v rows stacked, gate/up rows interleaved), and the
-    rotary table.  `host` holds bf16 bit arrays [out, in] (numpy uint16)."""
+    rotary table (cos_sin: another one, fp32 [max_position, rotary dims], as
+    rope_cos_sin_scaled makes it).  `host` holds bf16 bit arrays [out, in] (numpy uint16)."""
 
     def __init__(self, host: dict, hq: int, hkv: int, d: int, max_position: int,
-                 eps: float = 1e-5, base: float = 500000.0):
+                 eps: float = 1e-5, base: float = 500000.0, cos_sin=None):
         import torch
 
         def dev(bits):
@@ -730,7 +739,11 @@ class LayerWeights:
         self.w_o = dev(host["w_o"])
         self.w_gate_up = dev(interleave_gate_up(host["w_gate"], host["w_up"]))
         self.w_down = dev(host["w_down"])
-        self.cos_sin = torch.from_numpy(rope_cos_sin(max_position, d, base)).cuda()
+        if cos_sin is None:
+            cos_sin = rope_cos_sin(max_position, d, base)
+        elif cos_sin.shape[0] != max_position:
+            raise ValueError(f"cos_sin of {cos_sin.shape[0]} positions, not {max_position}")
+        self.cos_sin = torch.from_numpy(np.ascontiguousarray(cos_sin, dtype=np.float32)).cuda()
         self.c = SsaLayerWeights(self.attn_norm.data_ptr(), self.w_qkv.data_ptr(),
                                  self.w_o.data_ptr(), self.mlp_norm.data_ptr(),
                                  self.w_gate_up.data_ptr(), self.w_down.data_ptr(),
@@ -1217,6 +1230,7 @@ def rope_append_as(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_
     each query and key head in pairs of its halves ("half") or of neighbours
     ("interleaved"), at shifted positions where shifts are given."""
     what = "ssa_rope_append_as"
+    pairs = _choice("layout", layout, ROPE_LAYOUTS)
     at, h = _header(plan_host, _PLAN_MAGIC, what)
     check = _Buffers()
     n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
@@ -1224,7 +1238,7 @@ def rope_append_as(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_
     rotary = d if rotary_dim is None else int(rotary_dim)
     if rotary < 1:
         raise SsaError(SSA_ERR_ARG, what)
-    form = SsaRopeForm(_choice("layout", layout, ROPE_LAYOUTS), rotary)
+    form = SsaRopeForm(pairs, rotary)
     pool = shape.num_pages * hkv * shape.page_size * d
     if shift_host is not None:
         shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
@@ -1351,3 +1365,54 @@ def sparse_attention(shape: SsaShape, plan_host, plan_dev, q, k_cache, v_cache, 
         ws, n, check.stream(stream))
     if rc:
         raise SsaError(rc, "ssa_sparse_attention")
+
+
+def layer_forward_sparse(shape: SsaShape, plan_host, plan_dev, weights: LayerWeights, x, out,
+                         k_cache, v_cache, block_table, workspace, layout: str = "half",
+                         rotary_dim: int | None = None, shift_host=None, shift_dev=None,
+                         summary=None, block_keys: int = 0, sparse_plan_host=None,
+                         sparse_plan_dev=None, scores=None, blocks=None, sparse_workspace=None,
+                         stream=None):
+    """ssa_layer_forward_sparse: layer_forward for long contexts.  layout and rotary_dim as
+    rope_append_as (the weights' cos_sin is of that form then), shifts as
+    rope_append_shifted; with a summary the new keys' blocks are summarised; with a sparse
+    plan the rows attend over the blocks that they select.  Buffers of the selection without
+    a sparse plan are refused, and so is one of the two shift arrays without the other."""
+    what = "ssa_layer_forward_sparse"
+    at, h = _header(plan_host, _PLAN_MAGIC, what)
+    check = _Buffers()
+    n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
+    hkv, d = shape.num_kv_heads, shape.head_dim
+    pool = shape.num_pages * hkv * shape.page_size * d
+    p = SsaLayerSparse(block_keys=int(block_keys))
+    rotary = d if rotary_dim is None else int(rotary_dim)
+    form = SsaRopeForm(_choice("layout", layout, ROPE_LAYOUTS), rotary)
+    if form.layout or rotary != d:
+        p.rope = ctypes.pointer(form)
+    if weights.cos_sin.numel() != weights.c.max_position * rotary:
+        raise ValueError(f"the weights' cos_sin has not rows of {rotary}")
+    p.shift_dev = check("shift_dev", shift_dev, n, 4)
+    if shift_host is not None:
+        shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)
+        if shift_host.size != n:
+            raise ValueError(f"{shift_host.size} shifts for {n} requests")
+        p.shift_host = _address(shift_host)
+    p.summary = check("summary", summary, shape.num_pages * hkv * 2 * d, 2)
+    if sparse_plan_host is not None:
+        p.plan_host, sh = _header(sparse_plan_host, _SPARSE_MAGIC, what)
+        p.plan_dev = check.plan(sparse_plan_dev, sparse_plan_host)
+        lists = tokens * hkv
+        p.scores = check("scores", scores, lists * sh[_SPARSE_MAX_BLOCKS], 4)
+        p.blocks = check("blocks", blocks, lists * sh[_SPARSE_TOP], 4)
+        p.workspace, p.ws_bytes = check.workspace(sparse_workspace)
+    elif not (sparse_plan_dev is scores is blocks is sparse_workspace is None):
+        raise ValueError("buffers of the selection are given, but no sparse_plan_host")
+    ws, ws_bytes = check.workspace(workspace)
+    rc = LIB.ssa_layer_forward_sparse(
+        shape, at, check.plan(plan_dev, plan_host), weights.c, p,
+        check("x", x, tokens * weights.hidden, 2), check("out", out, tokens * weights.hidden, 2),
+        check("k_cache", k_cache, pool, 2), check("v_cache", v_cache, pool, 2),
+        check("block_table", block_table, n * shape.max_pages_per_req, 4), ws, ws_bytes,
+        check.stream(stream))
+    if rc:
+        raise SsaError(rc, what)

@@ -286,11 +286,11 @@ def test_cut_lists_of_few_rows(torch_dev, heads, u, block, top):
     rng = np.random.default_rng(1)
     lists = np.sort(rng.permutation(u // block + 1)[:top]).astype(np.int32)
     lists = np.pad(lists, (0, top - len(lists)), constant_values=-1)
-    x.blocks.copy_(dev(torch_dev, np.broadcast_to(lists, (1, heads[1], top))))
+    x.blocks.copy_(dev(torch_dev, np.tile(lists, (1, heads[1], 1))))
     x.attend()
     x.check_out()
     lists[3:] = -1  # most pieces hold nothing
-    x.blocks.copy_(dev(torch_dev, np.broadcast_to(lists, (1, heads[1], top))))
+    x.blocks.copy_(dev(torch_dev, np.tile(lists, (1, heads[1], 1))))
     x.attend()
     x.check_out()
     x.blocks.fill_(-1)
