@@ -185,9 +185,8 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
 // power of two with its last one, and 16 blocks as columns, so that a token's heads lie in
 // the registers of a lane and, from eight on, in 2 or 4 lanes.  A wave keeps two tiles of
 // blocks.  The queries of four tiles at a time go through LDS, split into their two parts, a
-// tile by each wave, the next four on their way meanwhile: a kv head's queries lie in a few
-// of the cache's channels (1 KB of every 8 at 32/8 heads), and read by every wave for itself
-// they bounded the kernel (512 rows on 32768 keys in blocks of 32: 33 us, so 20).
+// tile by each wave, the next four on their way meanwhile: read and split by every wave for
+// itself they bounded the kernel (512 rows on 32768 keys in blocks of 32: 33 us, so 22).
 template <int D, int LOG_G>  // heads of a group: more than 2^(LOG_G - 1), up to 2^LOG_G
 __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseArgs a) {
   constexpr int KS = D / 32, TOKENS = 16 >> LOG_G;  // tokens of a tile
@@ -503,6 +502,7 @@ struct AttentionLds {
   uint32_t mask[kMaskBlocks / 2];   // of two blocks each
   int part[2][4];
   int flag[2];
+  int odd;                          // some sum is not finite
   float ml[2][4][16];
   float m[32], l[32];               // of the passes so far, and their sums
   __attribute__((aligned(16))) float sum[32][D];
@@ -557,12 +557,14 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
     return Place{x / D, x % D};
   };
   uint32_t seen;  // rows of which a key counts
+  bool fresh;     // no pass yet: LDS holds no sums
   // m, l and the sums of column c: between the passes they lie in LDS, so that they take no
   // registers from the products.
   struct State {
     float m, l;
     f32x4 sum;
   };
+  const State nothing = {-kInf, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
   auto load_state = [&](int c, int d0) {
     return State{lds.m[c], lds.l[c], *reinterpret_cast<const f32x4*>(&lds.sum[c][d0])};
   };
@@ -735,7 +737,7 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
           const int c = c0 + i * CSTEP;
-          if (h == 0) x[i] = load_state(n * 16 + c, d0);
+          if (h == 0) x[i] = fresh ? nothing : load_state(n * 16 + c, d0);
           if (d0 / 64 != h) continue;
           float mm = x[i].m;
 #pragma unroll
@@ -754,8 +756,14 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
       }
       __syncthreads();  // m and l have been read by all threads of a column
 #pragma unroll
-      for (int i = 0; i < PER; ++i) store_state(n * 16 + c0 + i * CSTEP, d0, x[i]);
+      for (int i = 0; i < PER; ++i) {
+        store_state(n * 16 + c0 + i * CSTEP, d0, x[i]);
+        // 0 times what is not finite is NaN
+        const float zero = (x[i].l + (x[i].sum[0] + x[i].sum[1]) + (x[i].sum[2] + x[i].sum[3])) * 0.f;
+        if (__any(zero != 0.f) && lane == 0) lds.odd = 1;
+      }
     }
+    fresh = false;
   };
   // The same, key by key without the matrix cores, for values that are not finite: they reach
   // only the rows that see their keys, and with the whole weight.  (In the products above, 0
@@ -765,7 +773,7 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
     const auto [c0, d0] = place();
     State x[NC];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) x[n] = load_state(c0 + n * CSTEP, d0);
+    for (int n = 0; n < NC; ++n) x[n] = fresh ? nothing : load_state(c0 + n * CSTEP, d0);
     __syncthreads();
     for (int i = 0; i < total; ++i) {
       const int4 e = lds.page[i];
@@ -801,6 +809,7 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
     }
 #pragma unroll
     for (int n = 0; n < NC; ++n) store_state(c0 + n * CSTEP, d0, x[n]);
+    fresh = false;
   };
   // beside the last page of an odd number: the same one, of no row
   auto pad = [&](int total, int i, int4 e) {
@@ -924,14 +933,9 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
     return pages;
   };
   for (bool finite = true;; finite = false) {
-    {
-      const auto [c0, d0] = place();
-#pragma unroll
-      for (int i = 0; i < NC; ++i)
-        store_state(c0 + i * CSTEP, d0, State{-kInf, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}});
-    }
     seen = 0;
-    __syncthreads();
+    fresh = true;
+    if (tid == 0) lds.odd = 0;
     // this workgroup's pages of the union, as many steps to every wave, or of each row's list
     int share = -1, base, end, t = rows - 1;
     if (rows > 1 && (last >> a.log_block) < kMaskBlocks) share = make_union();
@@ -962,21 +966,14 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
       __syncthreads();  // the pages and sums have been read
       base += kPassPages;
     }
-    if (!finite) break;
-    float zero = 0.f;
+    // fresh: not one pass, all of whose barriers would lie behind here
+    if (!finite || fresh || !lds.odd) break;
+    __syncthreads();
+  }
+  if (fresh) {
     const auto [c0, d0] = place();
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int c = c0 + i * CSTEP;
-      const State x = load_state(c, d0);
-      if (c < columns)
-        zero += x.l * 0.f + (x.sum[0] * 0.f + x.sum[1] * 0.f) + (x.sum[2] * 0.f + x.sum[3] * 0.f);
-    }
-    if (tid == 0) lds.flag[0] = 0;
-    __syncthreads();
-    if (__any(zero != 0.f) && lane == 0) lds.flag[0] = 1;
-    __syncthreads();
-    if (!lds.flag[0]) break;
+    for (int i = 0; i < NC; ++i) store_state(c0 + i * CSTEP, d0, nothing);
     __syncthreads();
   }
 

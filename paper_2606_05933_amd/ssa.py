@@ -974,10 +974,14 @@ def _address(a):
 
 def _header(plan_host, magic: int, what: str):
     """Address of a plan and its header as int32 words, checked for its kind."""
-    at = _address(plan_host)
-    if at is None:
-        raise SsaError(SSA_ERR_NULL, what)
-    words = _HeaderWords.from_address(at)
+    try:  # a writable array: a third of the time
+        words = _HeaderWords.from_buffer(plan_host)
+        at = ctypes.addressof(words)
+    except (TypeError, ValueError, BufferError):
+        at = _address(plan_host)
+        if at is None:
+            raise SsaError(SSA_ERR_NULL, what)
+        words = _HeaderWords.from_address(at)
     if words[0] != magic:
         raise SsaError(SSA_ERR_PLAN_MISMATCH, what)
     return at, words
@@ -989,7 +993,9 @@ class _Buffers:
     __slots__ = ("device",)
 
     def __init__(self):
-        self.device = _torch.cuda.current_device()
+        if not _torch.cuda.is_initialized():
+            _torch.cuda.init()
+        self.device = _torch._C._cuda_getDevice()
 
     def __call__(self, name, t, numel, itemsize):
         if t is None:
