@@ -77,8 +77,10 @@ def select(score, top, sink, recent):
 
 def keys_of(blocks, block, pos):
     """The key indexes that a list names for a row at `pos`, as often as it does."""
-    t = [n * block + j for n in blocks if 0 <= n <= pos // block for j in range(block)]
-    return np.array([x for x in t if x <= pos], dtype=np.int64)
+    n = np.asarray(blocks, dtype=np.int64)
+    n = n[(n >= 0) & (n <= pos // block)]
+    t = (n[:, None] * block + np.arange(block)).reshape(-1)
+    return t[t <= pos]
 
 
 def attention(b, k_cache, v_cache, blocks, block):

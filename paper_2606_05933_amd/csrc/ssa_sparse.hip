@@ -140,7 +140,7 @@ struct SparseArgs {
   int32_t workgroups;
   int32_t hq, hkv, g, maxp;
   int32_t num_groups, off_rows, off_scores;
-  int32_t block_keys, log_block;
+  int32_t log_block;
   int32_t top, sink, recent, max_blocks;
   int32_t nsplit, split_entries;
   int32_t tokens, subs, g_magic;  // rows of an attention workgroup, workgroups of a record of rows
@@ -1094,7 +1094,6 @@ SparseArgs sparse_args(const SparseHeader* h, const void* plan_dev) {
   a.num_groups = h->num_groups;
   a.off_rows = h->off_rows;
   a.off_scores = h->off_scores;
-  a.block_keys = h->block_keys;
   a.log_block = log2_of(h->block_keys);
   a.top = h->top;
   a.sink = h->sink;

@@ -82,6 +82,7 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
       groups += ceil_div(c, kRowGroup);
     }
   }
+  if ((groups + singles) * (int64_t)sizeof(SparseRows) > INT32_MAX) return SSA_ERR_LENGTH;
 
   // Score items: a chunk's are 128 blocks by as many 16-column tiles (tokens x heads of
   // a group) as leave enough workgroups; a decode row's as many passes of 128 blocks.

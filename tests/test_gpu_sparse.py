@@ -374,16 +374,60 @@ def test_replayed_graph(torch_dev):
     x.check_out()
 
 
-def test_values_that_are_no_numbers(torch_dev):
+@pytest.mark.parametrize("scale", [0.0, 4.0])
+@pytest.mark.parametrize("heads,c,u", [((16, 2, 64), (9, 1), (200, 77)), ((8, 8, 128), (1, 33), (15, 0))])
+def test_scales(torch_dev, heads, c, u, scale):
+    """Scale 0: the mean of the keys' values, also where a row sees a part of a page."""
+    x = Sparse(torch_dev, heads, c, u, 32, 5, seed=21, scale=scale)
+    random_lists(np.random.default_rng(3), x)
+    x.attend()
+    x.check_out()
+
+
+def test_more_pages_than_lds_holds(torch_dev):
+    """Lists and unions of more than 512 pages for a workgroup, and requests of more blocks
+    than a union's masks have room for."""
+    rng = np.random.default_rng(8)
+    # one row whose list of 32768 entries names 150 blocks here and there: 64 pieces of 4096 pages
+    x = Sparse(torch_dev, (4, 2, 64), (1,), (20000,), 128, 32768, seed=22)
+    lists = np.full((1, 2, 32768), -1, np.int32)
+    for h in range(2):
+        lists[0, h, rng.permutation(32768)[:150]] = rng.permutation(157)[:150]
+    lists[0, 1, :600] = rng.permutation(np.resize(np.arange(157), 600))  # a piece of 4096 pages
+    x.blocks.copy_(dev(torch_dev, lists))
+    x.attend()
+    x.check_out()
+    # 512 workgroups of 16 rows each: nothing is cut, and a union has more than 512 blocks
+    x = Sparse(torch_dev, (64, 64, 64), (128,), (9000,), 16, 100, seed=23)
+    assert x.ws.numel() == 4096
+    lists = np.sort(np.argsort(rng.random((128, 64, 563)), axis=2)[:, :, :100], axis=2)
+    x.blocks.copy_(dev(torch_dev, lists.astype(np.int32)))
+    union = len(np.unique(lists[:16, 0]))
+    assert union > 512, union
+    x.attend()
+    x.check_out()
+    # rows past 8192 blocks go by their own lists
+    x = Sparse(torch_dev, (2, 1, 64), (5,), (131070,), 16, 40, seed=24)
+    lists = np.stack([rng.permutation(8192)[:40] for _ in range(5)])[:, None]
+    lists[2:, 0, 7] = 8192
+    x.blocks.copy_(dev(torch_dev, lists.astype(np.int32)))
+    x.attend()
+    x.check_out()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (16, 2, 64), (16, 2, 128), (2, 2, 64)])
+def test_values_that_are_no_numbers(torch_dev, hq, hkv, d):
     """NaN and infinite keys and values of named blocks show, and nothing else does: other
     blocks, later positions, and the slots behind a request's last key."""
     torch = torch_dev
-    x = Sparse(torch, (4, 2, 128), (3, 1), (200, 70), 16, 4, seed=3)
-    b = x.b
+    x = Sparse(torch, (hq, hkv, d), (3, 1), (200, 70), 16, 4, seed=3)
+    b, g = x.b, hq // hkv
     lists = np.full((4, 2, 4), -1, np.int32)
     lists[:, :, :2] = [1, 3]
     lists[:3, :, 2] = [[12], [12], [12]]
     x.blocks.copy_(dev(torch, lists))
+    x.attend()
+    plain = x.out[:-1].float().cpu().numpy().reshape(4, 2, g, d)
     # request 0: NaN in block 2 (named by no one), in position 202 (seen by row 2 alone)
     x.kc[b.block_table[0, 2], :, 3] = 0x7FC0
     x.vc[b.block_table[0, 2], :, :, 5] = 0x7F80
@@ -392,11 +436,40 @@ def test_values_that_are_no_numbers(torch_dev):
     x.vc[b.block_table[1, 1], 1, 7, 2] = 0xFF80
     x.upload()
     x.attend()
-    got = x.out[:-1].float().cpu().numpy().reshape(4, 2, 2, 128)
+    got = x.out[:-1].float().cpu().numpy().reshape(4, 2, g, d)
     bad = np.isnan(got)
     assert bad[2, 0].all() and not bad[:2].any() and not bad[2, 1].any() and not bad[3].any()
     assert (got[3, 1, :, 7] == -np.inf).all()
-    assert np.isfinite(np.delete(got[3], 7, axis=2)).all()
+    got[2, 0] = plain[2, 0]
+    got[3, 1, :, 7] = plain[3, 1, :, 7]
+    # what went key by key agrees with what the matrix cores gave: two roundings to bf16, and
+    # sums of up to 48 terms of magnitude under 5
+    assert (np.abs(got - plain) <= 2.0 ** -7 * np.abs(plain) + 1e-5).all()
+    # a key seen by rows 1 and 2 alone is NaN: so are they, of that kv head
+    x.kc[b.block_table[0, 12], 1, 9, 5] = 0x7FC0
+    x.upload()
+    x.attend()
+    bad = np.isnan(x.out[:-1].float().cpu().numpy().reshape(4, 2, g, d))
+    assert bad[1:3, 1].all() and bad[2, 0].all() and not bad[0].any() and not bad[1, 0].any()
+
+
+def test_logits_of_minus_infinity(torch_dev):
+    """Keys whose logits are all -infinity have no weights: NaN, as of a softmax over them; a
+    row without a key gives zeros."""
+    torch = torch_dev
+    x = Sparse(torch, (4, 2, 64), (2, 1), (100, 60), 16, 3, seed=6)
+    b = x.b
+    b.q[:, :, 0] = 0x3F80  # 1
+    for i in range(2):
+        x.kc[b.block_table[i, 1], :, :, 0] = 0xFF80
+    x.upload()
+    lists = np.full((3, 2, 3), -1, np.int32)
+    lists[:, 0, 0] = 1
+    lists[0, 0, 1] = 2
+    x.blocks.copy_(dev(torch, lists))
+    x.attend()
+    got = x.out[:-1].float().cpu().numpy().reshape(3, 2, 2, 64)
+    assert np.isnan(got[1:, 0]).all() and np.isfinite(got[0, 0]).all() and (got[:, 1] == 0).all()
 
 
 def test_far_offsets(torch_dev):
