@@ -88,7 +88,10 @@ struct RopeArgs {
 // query/key heads 8 y .. 8 y + 7 (of the Hq + Hkv rotated ones); the others copy
 // value heads.
 // Which dims of a head turn, in which pairs.  A head is D / 16 units of 16 dims, two
-// 16-byte pieces; the first rotary / 16 of them turn, the others are copied.
+// 16-byte pieces; the first rotary / 16 of them turn, the others are copied.  So every form moves
+// the same bytes in the same pieces (memory bounds them alike: 3881 rows of 64/8 heads, 160 MB, take
+// 35.5 us with 96 dims in halves, 4.5 TB/s); the whole head stays a form of its own, its offsets known
+// to the compiler.
 enum RopeForm {
   kWhole,      // pairs (i, i + D/2) of the whole head
   kHalf,     // pairs (i, i + rotary/2) of the first `rotary` dims

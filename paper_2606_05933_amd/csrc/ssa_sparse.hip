@@ -35,8 +35,9 @@ __device__ __forceinline__ int workgroup_id() {
 // instruction, so that the extremes are the keys' own bits.  Of the plan's append segments (a
 // page of new tokens each) the first one in a block stands for it.  A chunk has one such in
 // BLOCK / 16 of its segments: a wave looks at as many, so that every workgroup has work (with
-// a workgroup a segment, those with work fell to two of the eight dies, and 33768 tokens of
-// 8 heads in blocks of 64 took 29.5 us).
+// a workgroup a segment, those with work fell to two of the eight dies).  Memory bounds it:
+// 33768 tokens of 8 heads in blocks of 64, 71 MB, take 15 us, 4.7 TB/s (29.5 so); the blocks of
+// 64 decodes 4.1 us, three dependent loads and the launch.
 struct SummaryArgs {
   const uint8_t* plan;
   uint64_t hash;
@@ -71,8 +72,8 @@ __device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b) {
 
 // Block of request `req` from position `first` on.
 template <int D, int BLOCK>
-__device__ __forceinline__ void summarise(const SummaryArgs& a, int req, int first, int len, int kvh,
-                                          int lane) {
+__device__ __forceinline__ void summarise(const SummaryArgs& a, int req, int first, int len,
+                                          int kvh, int lane) {
   constexpr int CPR = D / 8, ROWS = 64 / CPR;  // lanes a row, rows a load
   constexpr int LOADS = BLOCK / ROWS, PER_PAGE = 16 / ROWS;
   const auto row = as_uniform<int32_t>(a.bt + (size_t)req * a.maxp);
@@ -186,7 +187,11 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
 // the registers of a lane and, from eight on, in 2 or 4 lanes.  A wave keeps two tiles of
 // blocks.  The queries of four tiles at a time go through LDS, split into their two parts, a
 // tile by each wave, the next four on their way meanwhile: read and split by every wave for
-// itself they bounded the kernel (512 rows on 32768 keys in blocks of 32: 33 us, so 22).
+// itself they bounded the kernel (512 rows on 32768 keys in blocks of 32, 32/8 heads: 33 us,
+// so 22).  What is left there is vector and matrix issue of few waves and the reads from LDS
+// (beside 16 decodes 24 us; 21 without the stores, 20 without the queries' loads); a decode's
+// scores wait for memory (64 rows of 8000 to 30000 keys in blocks of 16: 273 MB in 48 us, 5.7
+// TB/s).
 template <int D, int LOG_G>  // heads of a group: more than 2^(LOG_G - 1), up to 2^LOG_G
 __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseArgs a) {
   constexpr int KS = D / 32, TOKENS = 16 >> LOG_G;  // tokens of a tile
@@ -308,7 +313,11 @@ __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseA
 // highest key, what is not there the lowest.  WAVES waves hold a list in registers, 64 NR
 // scores each, and find the key of the last one that stays bit by bit, from the highest
 // bit in which the keys differ on: a count of the keys from a candidate on is a compare and
-// a count of the lanes' mask per register.
+// a count of the lanes' mask per register, and it ends once the candidate parts as many as
+// stay (some 12 to 18 counts of spread scores).  Lists in several waves meet at a barrier for
+// every count, so one wave takes a list where there are lists for every compute unit (4224 of
+// 1040 blocks: 30 us in four waves each, 16 so, 5 of them vector issue); 256 lists of 512 blocks
+// take 5.8 us, the launch, the plan, the scores and the search one after another.
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
                                         __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
@@ -470,29 +479,38 @@ struct PartReader {
 // Attention.  One workgroup takes as many neighbouring rows of a request as fit in 32 columns
 // (row, query head) of a kv head, and the union of their lists: neighbours mostly look at the
 // same blocks, whose keys and values are then read once, and a block costs the matrix cores the
-// same for one row as for 16 columns of them.  A mask per block says whose it is.  A row alone (a decode)
-// goes by its list as it is, and so do rows one after the other whose lists name a block
-// twice or whose masks would not fit in LDS.
+// same for one row as for 16 columns of them.  A mask per block says whose it is.  A row alone
+// (a decode) goes by its list as it is, and so do rows, one after the other, whose lists name a
+// block twice or whose masks would not fit in LDS.
 //
-// The pages (of no block left out) go to LDS; the four waves take two of them, 32 keys, in turn.  The 16x16x32 products have keys as rows; key r of a step is row (r & 3) + 4 (r >> 3)
+// The pages (of no block left out) go to LDS; the four waves take two of them, 32 keys, in
+// turn.  The 16x16x32 products have keys as rows; key r of a step is row (r & 3) + 4 (r >> 3)
 // of product (r >> 2) & 1, so that the logits of a lane are those whose weights it multiplies
 // with the values (dim-major pages) next.  Keys and values go from memory to registers, a step
-// ahead.
+// ahead; the steps' loads are what bounds it, and the registers for them leave two waves a SIMD
+// (three waves had to spill, and were slower).  64/8 heads of 128, lists of 64 blocks of 64 keys:
+//   32 decode rows     105 us  537 MB from memory, 5.1 TB/s (96 rows 5.9)
+//   128 rows of a chunk 89 us  151 with a workgroup a row (2.1 GB through the caches at 14
+//                             TB/s), 110 with 16 columns a workgroup, 144 with two waves for each 16
+// One row of 2048 keys, 11 us, is launch, plan, list, table, keys, join and the pieces' join.
 constexpr int kPassPages = 512;     // pages in LDS at a time
 constexpr int kMaskBlocks = 8192;   // blocks of a union, 16 bits each
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // The highest x of a column: over the four lanes 16 apart.
 __device__ __forceinline__ float max_over_quads(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  u = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 // Keeps the first n of 8 packed bf16 values.
 __device__ __forceinline__ u32x4 first_values(int n) {
   u32x4 keep;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) keep[w] = (n > 2 * w ? 0xFFFFu : 0u) | (n > 2 * w + 1 ? 0xFFFF0000u : 0u);
+  for (int w = 0; w < 4; ++w)
+    keep[w] = (n > 2 * w ? 0xFFFFu : 0u) | (n > 2 * w + 1 ? 0xFFFF0000u : 0u);
   return keep;
 }
 
@@ -588,7 +606,8 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
       const int column = min(r16 + n * 16, columns - 1);  // the others repeat the last
       token[n] = token_of(column);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) qf[n][s] = as_bf16x8(ld16(a.q + row_of(column) + s * 32 + quad * 8));
+      for (int s = 0; s < KS; ++s)
+        qf[n][s] = as_bf16x8(ld16(a.q + row_of(column) + s * 32 + quad * 8));
     }
     float m[NT], l[NT];
     f32x4 o[NT][DT];
@@ -644,7 +663,8 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int t = 0; t < 2; ++t) logits[n][t] = mfma(as_bf16x8(kf[t][k]), qf[n][k], logits[n][t]);
+          for (int t = 0; t < 2; ++t)
+            logits[n][t] = mfma(as_bf16x8(kf[t][k]), qf[n][k], logits[n][t]);
       if constexpr (more) load_keys(p0, p1);
       __builtin_amdgcn_sched_barrier(0);
       if (far > last) {
@@ -955,7 +975,8 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
         if (++t >= rows) break;
         base = split * a.split_entries << log_pages;
       }
-      const int total = joint ? union_pages(base, min(kPassPages, end - base)) : list_pages(t, base, end);
+      const int total =
+          joint ? union_pages(base, min(kPassPages, end - base)) : list_pages(t, base, end);
       __syncthreads();
       if (finite && columns <= 16)
         multiply(total, std::integral_constant<int, 1>{});
@@ -1029,9 +1050,8 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
   // m and l of all pieces, their weights, then the sums
   for (int e = tid; e < a.nsplit * 2 * columns; e += kSparseThreads) {
     const int s = e / (2 * columns), i = e - s * 2 * columns;
-    lds.weight[e] =
-        __hip_atomic_load(records + (int64_t)s * rec_floats + (i < columns ? i : cols + i - columns),
-                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const float* from = records + (int64_t)s * rec_floats + (i < columns ? i : cols + i - columns);
+    lds.weight[e] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   const PartReader read(records);

@@ -170,11 +170,13 @@ int build(const ssa_shape* s, const ssa_sparse_config* cfg, const int32_t* q_len
   // 16 rows of scores are within a 32-bit byte offset
   if ((int64_t)hkv * h.max_blocks > kMaxScoreRow) return SSA_ERR_LENGTH;
   // workgroups of a launch
+  const int64_t rows = (int64_t)h.num_groups * kRowGroup + h.num_singles;
   if ((int64_t)h.num_scores * hkv > INT32_MAX ||
-      std::max(((int64_t)h.num_groups * kRowGroup + h.num_singles) * hkv, lists * h.nsplit) > INT32_MAX)
+      std::max(rows * hkv, lists * h.nsplit) > INT32_MAX)
     return SSA_ERR_LENGTH;
   h.ws_bytes = kSparseTickets * 4;
-  if (h.nsplit > 1) h.ws_bytes += lists * h.nsplit * (int64_t)sparse_rec_floats(sparse_tokens(g) * g, d) * 4;
+  if (h.nsplit > 1)
+    h.ws_bytes += lists * h.nsplit * (int64_t)sparse_rec_floats(sparse_tokens(g) * g, d) * 4;
   uint64_t hv = 1469598103934665603ull;
   const int32_t f[10] = {s->num_q_heads,         s->num_kv_heads, s->head_dim,     s->page_size,
                          s->num_pages,           s->max_pages_per_req, cfg->block_keys,
@@ -252,7 +254,8 @@ int ssa_sparse_plan(const ssa_shape* shape, const ssa_sparse_config* config,
       std::memcpy(rows + sizeof(ssa::SparseRows) * p.groups.size(), p.singles.data(),
                   sizeof(ssa::SparseRows) * p.singles.size());
     if (!p.scores.empty())
-      std::memcpy(b + p.hdr.off_scores, p.scores.data(), sizeof(ssa::SparseScore) * p.scores.size());
+      std::memcpy(b + p.hdr.off_scores, p.scores.data(),
+                  sizeof(ssa::SparseScore) * p.scores.size());
     return SSA_OK;
   } catch (const std::bad_alloc&) {
     return SSA_ERR_LENGTH;
