@@ -83,7 +83,8 @@ typedef struct ssa_sparse_config {
  *               token, rounded up to a multiple of four (at least four)
  * Errors: those of ssa_plan_size (without TUNING); SHAPE also for Hq D > 2^24; LENGTH
  * also for a request of more than 32768 blocks, for Hkv max_blocks > 2^24, and where the
- * plan would pass 2 GiB or a launch 2^31 workgroups; ARG (config); PLAN_SIZE (plan_bytes too small).
+ * plan would pass 2 GiB or a launch 2^31 workgroups; ARG (config); PLAN_SIZE (plan_bytes too
+ * small).
  */
 int ssa_sparse_plan_size(const ssa_shape* shape, const ssa_sparse_config* config,
                          const int32_t* q_len_host, const int32_t* ctx_len_host, int32_t num_reqs,
@@ -125,6 +126,7 @@ int ssa_block_select(const ssa_shape* shape, const void* plan_host, const void* 
  *              entry outside 0 .. p / B names no block, a block named twice counts
  *              twice.  A row and kv head without any key gives zeros.
  *   block_table  as ssa_mixed_attention; only entries of named blocks are read
+ *   out        another buffer than q
  *   workspace  ws_bytes of the plan.  Its first 4096 bytes hold tickets: zero before the
  *              first call (a zeroed allocation) and zero again after every call, whatever
  *              the plan.  Calls that share a workspace must be ordered on one stream.

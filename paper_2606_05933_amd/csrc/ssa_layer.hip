@@ -84,17 +84,14 @@ struct RopeArgs {
   int rotary;  // dims of a head that turn: the table's row (kWhole: D)
 };
 
-// Heads per workgroup of a grouped segment: group y < rot_groups rotates
-// query/key heads 8 y .. 8 y + 7 (of the Hq + Hkv rotated ones); the others copy
-// value heads.
 // Which dims of a head turn, in which pairs.  A head is D / 16 units of 16 dims, two
 // 16-byte pieces; the first rotary / 16 of them turn, the others are copied.  So every form moves
-// the same bytes in the same pieces (memory bounds them alike: 3881 rows of 64/8 heads, 160 MB, take
-// 35.5 us with 96 dims in halves, 4.5 TB/s); the whole head stays a form of its own, its offsets known
-// to the compiler.
+// the same bytes in the same pieces (memory bounds them alike: 3881 rows of 64/8 heads, 160 MB,
+// take 35.5 us with 96 dims in halves, 4.5 TB/s); the whole head stays a form of its own, its
+// offsets known to the compiler.
 enum RopeForm {
-  kWhole,      // pairs (i, i + D/2) of the whole head
-  kHalf,     // pairs (i, i + rotary/2) of the first `rotary` dims
+  kWhole,       // pairs (i, i + D/2) of the whole head
+  kHalf,        // pairs (i, i + rotary/2) of the first `rotary` dims
   kInterleaved  // pairs (2 i, 2 i + 1) of the first `rotary` dims
 };
 template <int D, int FORM>
@@ -123,6 +120,9 @@ struct Unit {
   }
 };
 
+// Heads per workgroup of a grouped segment: group y < rot_groups rotates
+// query/key heads 8 y .. 8 y + 7 (of the Hq + Hkv rotated ones); the others copy
+// value heads.
 constexpr int kHeadGroup = 8;
 constexpr int kSingleMaxHeads = 16 * kHeadGroup;  // rotated heads of one row per workgroup
 // Workgroups go in rows of this many: one row of more than 2^24 workgroups would

@@ -16,9 +16,10 @@ constexpr int kPage = SSA_PAGE_SIZE;
 constexpr int kMaxReqs = 65536;
 constexpr int kMaxTokens = 1 << 30;  // of a request
 constexpr int kWavesPerGroup = 4;
+constexpr int kWholeWaves = 512;  // requests that have a wave (and its pieces) to themselves
 
 struct PagesArgs {
-  int32_t n, pieces;
+  int32_t n, per, pieces;  // requests: all, of a wave; pieces of a request
   int32_t num_pages, maxp, most;  // most: of a request's tokens
   const int32_t* old_len;
   const int32_t* new_len;
@@ -55,22 +56,28 @@ struct Sums {
   static __device__ __forceinline__ int pages_of(int len) { return (len + kPage - 1) / kPage; }
 };
 
-// A wave takes one piece of one request.  It adds up what the requests take, give and add
-// itself, those before its own apart: one launch, and no workgroup waits for another.
+// A wave takes one piece of each of `per` requests.  It adds up what all requests take, give
+// and add itself, those before its own apart: one launch, and no workgroup waits for another.
 // The lengths are read by every wave that has something to write (64 requests 512 bytes), so
 // latency bounds it as long as the requests are some thousands: the lengths, then the ring
 // or the table.  (64 decodes 3.1 us; 504 requests with 58804 new rows 8.7; with waves
-// that had nothing to write adding up too 18.)
+// that had nothing to write adding up too 18.)  More than 512 requests share waves, which
+// would read too much between them otherwise: 1000 decodes take 10 us (with a wave each 16),
+// 5000 30 (178).
 __global__ __launch_bounds__(64 * kWavesPerGroup) void pages_resize_kernel(PagesArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * kWavesPerGroup +
                        __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int req = (int)(unit / a.pieces), piece = (int)(unit % a.pieces);
-  if (req > 0 && req >= a.n) return;  // no requests: one wave copies the state
-  const int from = a.n > 0 ? a.old_len[req] : 0, to = a.n > 0 ? a.new_len[req] : 0;
-  // lengths that are none differ by more than any piece's first token, or are of no piece
-  const int64_t tokens = (int64_t)to - from;
-  if (piece > 0 && tokens <= piece * 64 && -tokens / kPage < piece * 64) return;
+  const int req0 = (int)(unit / a.pieces) * a.per, piece = (int)(unit % a.pieces);
+  if (req0 > 0 && req0 >= a.n) return;  // no requests: one wave copies the state
+  const int count_own = min(a.per, a.n - req0);
+  // lane i: lengths of request req0 + i
+  const int own_from = lane < count_own ? a.old_len[req0 + lane] : 0;
+  const int own_to = lane < count_own ? a.new_len[req0 + lane] : 0;
+  // has the piece anything to write?  (Whatever lengths that are none say: the first piece is
+  // there, and the others write nothing then.)
+  const int64_t tokens = (int64_t)own_to - own_from;
+  if (piece > 0 && !__any(tokens > piece * 64 || -tokens / kPage >= piece * 64)) return;
   const int head = a.state[0], count = a.state[1];
   Sums before{0, 0, 0}, all{0, 0, 0};
   bool bad = false;
@@ -82,7 +89,7 @@ __global__ __launch_bounds__(64 * kWavesPerGroup) void pages_resize_kernel(Pages
       continue;
     }
     all.count(f, t);
-    if (i < req) before.count(f, t);
+    if (i < req0) before.count(f, t);
   }
   all = all.over_wave();
   before = before.over_wave();
@@ -106,30 +113,33 @@ __global__ __launch_bounds__(64 * kWavesPerGroup) void pages_resize_kernel(Pages
     a.state_out[3] = (int)min(missing, (uint32_t)INT32_MAX);
     if (!status && a.row_start) a.row_start[0] = 0;
   }
-  if (status || req >= a.n) return;
-  const int p = Sums::pages_of(from), q = Sums::pages_of(to);
-  int32_t* row = a.table + (size_t)req * a.maxp;
-  if (piece == 0 && lane == 0 && a.row_start)
-    a.row_start[req + 1] = (int32_t)(before.rows + max(to - from, 0));
-  // entry k >= p takes ring entry (head + before.taken + k - p) mod num_pages
+  if (status) return;
   auto wrapped = [&](uint32_t at) {
     return at < (uint32_t)a.num_pages ? at : at - (uint32_t)a.num_pages;
   };
-  const uint32_t take0 = wrapped((uint32_t)head + before.taken);
-  const uint32_t give0 = wrapped(wrapped((uint32_t)head + count) + before.given);
   const int step = a.pieces * 64, mine = piece * 64 + lane;
+  for (int i = 0; i < count_own; ++i) {
+    const int from = __shfl(own_from, i, 64), to = __shfl(own_to, i, 64), req = req0 + i;
+    const int p = Sums::pages_of(from), q = Sums::pages_of(to);
+    int32_t* row = a.table + (size_t)req * a.maxp;
+    // entry k >= p takes ring entry (head + before.taken + k - p) mod num_pages
+    const uint32_t take0 = wrapped((uint32_t)head + before.taken);
+    const uint32_t give0 = wrapped(wrapped((uint32_t)head + count) + before.given);
+    int64_t* slots = a.slots + before.rows;
+    before.count(from, to);
+    if (piece == 0 && lane == 0 && a.row_start) a.row_start[req + 1] = (int32_t)before.rows;
 #pragma unroll 4
-  for (int k = p + mine; k < q; k += step) row[k] = a.ring[wrapped(take0 + (uint32_t)(k - p))];
+    for (int k = p + mine; k < q; k += step) row[k] = a.ring[wrapped(take0 + (uint32_t)(k - p))];
 #pragma unroll 4
-  for (int k = q + mine; k < p; k += step) a.ring[wrapped(give0 + (uint32_t)(k - q))] = row[k];
-  if (!a.slots) return;
-  int64_t* slots = a.slots + before.rows;
+    for (int k = q + mine; k < p; k += step) a.ring[wrapped(give0 + (uint32_t)(k - q))] = row[k];
+    if (!a.slots) continue;
 #pragma unroll 4
-  for (int t = from + mine; t < to; t += step) {
-    const int k = t / kPage;
-    // a page taken by this call from the ring, one of before from the table
-    const int32_t* at = k < p ? row + k : a.ring + wrapped(take0 + (uint32_t)(k - p));
-    slots[t - from] = (int64_t)*at * kPage + t % kPage;
+    for (int t = from + mine; t < to; t += step) {
+      const int k = t / kPage;
+      // a page taken by this call from the ring, one of before from the table
+      const int32_t* at = k < p ? row + k : a.ring + wrapped(take0 + (uint32_t)(k - p));
+      slots[t - from] = (int64_t)*at * kPage + t % kPage;
+    }
   }
 }
 
@@ -161,7 +171,8 @@ extern "C" int ssa_pages_resize(const ssa_shape* shape, int32_t num_reqs, const 
   a.slots = slots;
   a.max_rows = max_rows;
   a.pieces = 32;
-  const int64_t units = (int64_t)std::max(1, num_reqs) * a.pieces;
+  a.per = std::min(64, std::max(1, (num_reqs + kWholeWaves - 1) / kWholeWaves));  // one a lane
+  const int64_t units = std::max<int64_t>(1, (num_reqs + a.per - 1) / a.per) * a.pieces;
   (void)hipGetLastError();
   hipLaunchKernelGGL(pages_resize_kernel, dim3((units + kWavesPerGroup - 1) / kWavesPerGroup),
                      dim3(64 * kWavesPerGroup), 0, static_cast<hipStream_t>(stream), a);

@@ -490,8 +490,8 @@ struct PartReader {
 // ahead; the steps' loads are what bounds it, and the registers for them leave two waves a SIMD
 // (three waves had to spill, and were slower).  64/8 heads of 128, lists of 64 blocks of 64 keys:
 //   32 decode rows     105 us  537 MB from memory, 5.1 TB/s (96 rows 5.9)
-//   128 rows of a chunk 89 us  151 with a workgroup a row (2.1 GB through the caches at 14
-//                             TB/s), 110 with 16 columns a workgroup, 144 with two waves for each 16
+//   128 rows of a chunk 89 us  151 with a workgroup a row (2.1 GB through the caches at 14 TB/s),
+//                              110 with 16 columns a workgroup, 144 with two waves for each 16
 // One row of 2048 keys, 11 us, is launch, plan, list, table, keys, join and the pieces' join.
 constexpr int kPassPages = 512;     // pages in LDS at a time
 constexpr int kMaskBlocks = 8192;   // blocks of a union, 16 bits each
@@ -779,7 +779,8 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
       for (int i = 0; i < PER; ++i) {
         store_state(n * 16 + c0 + i * CSTEP, d0, x[i]);
         // 0 times what is not finite is NaN
-        const float zero = (x[i].l + (x[i].sum[0] + x[i].sum[1]) + (x[i].sum[2] + x[i].sum[3])) * 0.f;
+        const float sums = (x[i].sum[0] + x[i].sum[1]) + (x[i].sum[2] + x[i].sum[3]);
+        const float zero = (x[i].l + sums) * 0.f;
         if (__any(zero != 0.f) && lane == 0) lds.odd = 1;
       }
     }

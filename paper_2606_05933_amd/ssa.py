@@ -751,6 +751,12 @@ class LayerWeights:
                                  int(max_position), float(eps))
 
 
+def _check_rotary_table(weights: LayerWeights, rotary: int):
+    """The layer reads rows of `rotary` entries of the weights' table."""
+    if weights.cos_sin.numel() != weights.c.max_position * rotary:
+        raise ValueError(f"the weights' cos_sin has not rows of {rotary}")
+
+
 def check_block_table(shape: SsaShape, plan_host, block_table_host) -> None:
     """ssa_check_block_table on a host copy of the block table (int32 numpy
     array [num_reqs, max_pages_per_req]); raises SsaError on a bad entry and
@@ -811,6 +817,7 @@ def layer_forward(shape: SsaShape, plan_host, plan_dev, weights: LayerWeights, x
     [T, hidden] bf16; out may be x)."""
     h = _plan_header(plan_host)
     T, n = h["num_tokens"], h["num_reqs"]
+    _check_rotary_table(weights, shape.head_dim)
     pool = shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim
     _check_dev("x", x, T * weights.hidden, 2)
     _check_dev("out", out, T * weights.hidden, 2)
@@ -1170,6 +1177,7 @@ def layer_forward_evicting(shape: SsaShape, plan_host, plan_dev, weights: LayerW
     what = "ssa_layer_forward_evicting"
     at, h = _header(plan_host, _PLAN_MAGIC, what)
     check = _Buffers()
+    _check_rotary_table(weights, shape.head_dim)
     n, tokens = h[_PLAN_REQS], h[_PLAN_TOKENS]
     slots = shape.num_pages * shape.num_kv_heads * shape.page_size
     e = SsaLayerEviction(decay=decay)
@@ -1290,7 +1298,7 @@ def block_summary(shape: SsaShape, plan_host, plan_dev, block_keys: int, k_cache
     check = _Buffers()
     rows = shape.num_pages * shape.num_kv_heads * shape.head_dim
     rc = LIB.ssa_block_summary(
-        shape, at, check.plan(plan_dev, plan_host), block_keys,
+        shape, at, check.plan(plan_dev, plan_host), int(block_keys),
         check("k_cache", k_cache, rows * shape.page_size, 2),
         check("block_table", block_table, h[_PLAN_REQS] * shape.max_pages_per_req, 4),
         check("summary", summary, rows * 2, 2), check.stream(stream))
@@ -1395,8 +1403,7 @@ def layer_forward_sparse(shape: SsaShape, plan_host, plan_dev, weights: LayerWei
     form = SsaRopeForm(_choice("layout", layout, ROPE_LAYOUTS), rotary)
     if form.layout or rotary != d:
         p.rope = ctypes.pointer(form)
-    if weights.cos_sin.numel() != weights.c.max_position * rotary:
-        raise ValueError(f"the weights' cos_sin has not rows of {rotary}")
+    _check_rotary_table(weights, rotary)
     p.shift_dev = check("shift_dev", shift_dev, n, 4)
     if shift_host is not None:
         shift_host = np.ascontiguousarray(shift_host, dtype=np.int32)

@@ -91,6 +91,17 @@ def test_requests_grow_shrink_and_end(torch_dev, n, longest):
     assert sorted(held + free) == list(range(p.num_pages)), "a page is lost or held twice"
 
 
+@pytest.mark.parametrize("n", [513, 1025, 32769, 65536])
+def test_more_requests_than_waves(torch_dev, n):
+    rng = np.random.default_rng(n)
+    p = Pages(torch_dev, n, 3 * n, 3, rng, 48 * n)
+    p.resize(rng.integers(0, 49, n))
+    new = rng.integers(0, 49, n)
+    free = p.state[1]
+    new[np.cumsum(np.maximum(-(-new // 16) - -(-p.len // 16), 0)) > free] = 0
+    p.resize(new)
+
+
 def test_no_requests_and_maps_left_out(torch_dev):
     rng = np.random.default_rng(0)
     p = Pages(torch_dev, 0, 9, 3, rng, 1)
@@ -413,7 +424,7 @@ def test_a_sparse_layer_is_its_calls(torch_dev, hq, hkv, d, cu, selected):
 def test_a_sparse_layer_refuses_half_given_parts(torch_dev):
     from paper_2606_05933_amd import ssa
     torch = torch_dev
-    b, shape, _, w, plan, x, ws = layer_setup(torch, 8, 2, 64, [(2, 30), (1, 5)])
+    b, shape, host, w, plan, x, ws = layer_setup(torch, 8, 2, 64, [(2, 30), (1, 5)])
     k, v, xd = dev(torch, b.k_cache), dev(torch, b.v_cache), dev(torch, x)
     before = bits(k), bits(v)
     shift = np.array([7, 9], np.int32)
@@ -432,4 +443,9 @@ def test_a_sparse_layer_refuses_half_given_parts(torch_dev):
             call(**{name: some})
     with pytest.raises(ValueError):
         call(rotary_dim=32)  # the weights' table has whole rows
+    part = ssa.LayerWeights(host, 8, 2, 64, 2048, cos_sin=ssa.rope_cos_sin(2048, 32))
+    for f in (ssa.layer_forward, ssa.layer_forward_evicting, ssa.layer_forward_sparse):
+        with pytest.raises(ValueError):  # and these would read past one of 32
+            f(shape, plan, dev(torch, plan), part, xd, torch.empty_like(xd), k, v,
+              dev(torch, b.block_table), ws)
     assert np.array_equal(bits(k), before[0]) and np.array_equal(bits(v), before[1])
