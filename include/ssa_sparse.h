@@ -47,6 +47,8 @@ extern "C" {
  * c_i - 1), each over all its keys up to u_i + c_i - 1.  The keys must be in the cache
  * (ssa_kv_append, ssa_append_attention or a RoPE + append ran before on the stream).
  * Blocks before u_i / B are left as they are, as is what lies behind the last one.
+ * Requests that share pages of the cache share whole blocks of them: a block has one
+ * summary, with its first page.
  * After a call that moved or dropped keys (ssa_evict_compact, rejected tokens), a plan
  * of the changed positions makes the summaries anew; a plan of c_i = all, u_i = 0 makes
  * all of them.

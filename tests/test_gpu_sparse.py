@@ -199,6 +199,38 @@ def test_scores_bound_every_logit(torch_dev):
                 assert logits.max() <= got[row, h, n] + 2 * 256 * 2.0 ** -24 * size
 
 
+@pytest.mark.parametrize("heads", [(4, 4, 64), (4, 2, 128), (6, 2, 64), (8, 2, 64), (28, 4, 128),
+                                   (16, 1, 64), (13, 1, 128)])
+def test_scores_of_queries_that_are_no_numbers(torch_dev, heads):
+    """A NaN counts only where all heads of a group have one, and then as the highest score."""
+    from oracle import sparse
+    x = Sparse(torch_dev, heads, (7, 1), (400, 900), 32, 4, seed=8)
+    b, s, g = x.b, x.b.shape, x.b.shape.group
+    for row in range(8):
+        for h in range(s.hkv):
+            if (row + h) % 3 == 2:
+                b.q[row, h * g:(h + 1) * g, row] = 0x7FC0
+            elif g > 1:
+                b.q[row, h * g + (row + h) % g, s.d - 1] = 0xFFC0
+    x.upload()
+    whole = x.whole_summary()
+    x.score()
+    got = x.scores.cpu().numpy().astype(np.float64)
+    for i, row, pos in x.rows():
+        n = pos // 32 + 1
+        at = b.block_table[i, np.arange(n) * 2]
+        for h in range(s.hkv):
+            q, hl = sparse._f64(b.q[row, h * g:(h + 1) * g]), sparse._f64(whole[at, h])
+            q = q[~np.isnan(q).any(axis=1)]
+            if len(q) == 0:
+                assert np.isnan(got[row, h, :n]).all(), (row, h)
+                continue
+            ref, size = sparse.bounds(q, hl[:, 0], hl[:, 1])
+            assert (np.abs(got[row, h, :n] - ref) <= 2 * s.d * 2.0 ** -24 * size).all(), (row, h)
+    x.select()
+    x.check_lists()
+
+
 @pytest.mark.parametrize("heads,c,u,block", [
     ((8, 8, 64), (1, 1, 3), (10, 600, 900), 16),
     ((28, 4, 128), (40, 1), (3000, 7000), 16),       # up to 438 blocks: one wave
@@ -342,6 +374,34 @@ def test_the_calls_in_order(torch_dev, heads, block, top, cu, plan):
     x.check_scores(whole)
     x.check_lists()
     x.check_out()
+
+
+def test_calls_on_two_streams(torch_dev):
+    """Two batches at once, each with buffers of its own, give what each gives alone."""
+    torch = torch_dev
+    batches = [Sparse(torch, (32, 8, 128), (1, 4, 1), (5000, 300, 40), 32, 20, 1, 2, seed=30),
+               Sparse(torch, (16, 2, 64), (9, 1), (3000, 9000), 16, 40, 1, 1, seed=31)]
+    want = []
+    for x in batches:
+        x.whole_summary()
+        for f in (x.summarise, x.score, x.select, x.attend):
+            f()
+        x.check_lists()
+        x.check_out()
+        want.append(bits(x.out))
+    streams = [torch.cuda.Stream() for _ in batches]
+    for i in range(5):
+        for x in batches:
+            x.out[:-1] = 7.0
+            x.blocks.fill_(-9)
+        torch.cuda.synchronize()
+        for call in ("summarise", "score", "select", "attend"):
+            for x, s in zip(batches, streams):
+                getattr(x, call)(s)
+        torch.cuda.synchronize()
+        for x, w in zip(batches, want):
+            assert np.array_equal(bits(x.out), w), i
+            assert not x.ws[:4096].any()
 
 
 def test_replayed_graph(torch_dev):
