@@ -82,8 +82,9 @@ int layer_ws(const ssa_shape* shape, const void* plan_host, const ssa_layer_weig
 // e: the parts of ssa_layer_forward_evicting, sp: of ssa_layer_forward_sparse; or null.
 int layer_forward(const ssa_shape* shape, const void* plan_host, const void* plan_dev,
                   const ssa_layer_weights* w, const ssa_layer_eviction* e,
-                  const ssa_layer_sparse* sp, const uint16_t* x, uint16_t* out, uint16_t* k_cache, uint16_t* v_cache, const int32_t* block_table,
-                  void* workspace, size_t ws_bytes, void* stream) {
+                  const ssa_layer_sparse* sp, const uint16_t* x, uint16_t* out, uint16_t* k_cache,
+                  uint16_t* v_cache, const int32_t* block_table, void* workspace, size_t ws_bytes,
+                  void* stream) {
   const PlanHeader* h = nullptr;
   LayerWs l;
   int rc = layer_ws(shape, plan_host, w, &h, &l);
@@ -170,9 +171,9 @@ int layer_forward(const ssa_shape* shape, const void* plan_host, const void* pla
     rc = ssa_rope_append_as(shape, plan_host, plan_dev, sp->rope, qkv, w->cos_sin, w->max_position,
                             shift, shift_dev, q, k_cache, v_cache, block_table, stream);
   else
-    rc = shift ? ssa_rope_append_shifted(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position,
-                                         shift, shift_dev, q, k_cache, v_cache, block_table,
-                                         stream)
+    rc = shift ? ssa_rope_append_shifted(shape, plan_host, plan_dev, qkv, w->cos_sin,
+                                         w->max_position, shift, shift_dev, q, k_cache, v_cache,
+                                         block_table, stream)
                : ssa_rope_append(shape, plan_host, plan_dev, qkv, w->cos_sin, w->max_position, q,
                                  k_cache, v_cache, block_table, stream);
   if (rc) return rc;
