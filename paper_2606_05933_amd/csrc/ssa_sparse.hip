@@ -188,10 +188,12 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
 // blocks.  The queries of four tiles at a time go through LDS, split into their two parts, a
 // tile by each wave, the next four on their way meanwhile: read and split by every wave for
 // itself they bounded the kernel (512 rows on 32768 keys in blocks of 32, 32/8 heads: 33 us,
-// so 22).  What is left there is vector and matrix issue of few waves and the reads from LDS
-// (beside 16 decodes 24 us; 21 without the stores, 20 without the queries' loads); a decode's
-// scores wait for memory (64 rows of 8000 to 30000 keys in blocks of 16: 273 MB in 48 us, 5.7
-// TB/s).
+// 21 so).  A tile's last reads from LDS are the next one's, on their way while its sums are
+// looked at, and which blocks a row sees is one comparison a store (with reads before each
+// product and the rows' conditions apart 23.8 us beside 16 decodes, 21.5 so).  What is left
+// there is the way to the first products, 6 us of plan, table and summaries, then queries, products
+// and stores, none of which alone is half of it; a decode's scores wait for memory (64 rows of
+// 8000 to 30000 keys in blocks of 16: 273 MB in 48 us, 5.7 TB/s).
 template <int D, int LOG_G>  // heads of a group: more than 2^(LOG_G - 1), up to 2^LOG_G
 __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseArgs a) {
   constexpr int KS = D / 32, TOKENS = 16 >> LOG_G;  // tokens of a tile
@@ -229,7 +231,13 @@ __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseA
     // a row's scores from block b0 on; rows j0 .. j0 + TOKENS - 1 are `step` floats apart
     const int step = a.hkv * a.max_blocks;  // at most 2^24
     float* to = a.scores + ((size_t)row0 * a.hkv + kvh) * a.max_blocks + b0;
-    const bool inner = b0 + 32 <= blk1;
+    // Block b0 + 16 t + r16 has a score in rows first[t] .. n - 1.
+    int first[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int b = b0 + t * 16 + r16;
+      first[t] = b < blk1 ? min(max((b << a.log_block) - pos0, 0), n) : n;
+    }
     for (int g0 = 0; g0 < n; g0 += 4 * TOKENS) {
       __syncthreads();  // the tiles before have been read
 #pragma unroll
@@ -247,34 +255,42 @@ __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseA
       if (g0 + 4 * TOKENS < n) load_queries(g0 + 4 * TOKENS);
       __syncthreads();
       if (b0 >= blk1) continue;
+      u32x4 query[2 * KS];
+      auto read_tile = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          query[k] = s_query[i][k][lane];
+          query[KS + k] = s_query[i][KS + k][lane];
+        }
+      };
+      read_tile(0);
       const int end = min(n, g0 + 4 * TOKENS);
       for (int j0 = g0; j0 < end; j0 += TOKENS, to += (size_t)TOKENS * step) {
-        const auto& query = s_query[(j0 - g0) / TOKENS];
         // the products with the high and with the low values apart: half as many terms in a
         // row, and no product waits for the one before
         f32x4 x[2], y[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) x[t] = y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const bf16x8 plus = as_bf16x8(query[k][lane]), minus = as_bf16x8(query[KS + k][lane]);
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            x[t] = mfma(plus, s[t][k], x[t]);
-            y[t] = mfma(minus, s[t][KS + k], y[t]);
+            x[t] = mfma(as_bf16x8(query[k]), s[t][k], x[t]);
+            y[t] = mfma(as_bf16x8(query[KS + k]), s[t][KS + k], y[t]);
           }
-        }
+        // the next tile (after the last one any), while this one's sums are looked at
+        __builtin_amdgcn_sched_barrier(0);
+        read_tile(((j0 - g0) / TOKENS + 1) & 3);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 2; ++t) x[t] += y[t];
-        // every row of the tile sees every block of it
-        const bool whole = inner && j0 + TOKENS <= n && b0 + 31 <= (pos0 + j0) >> a.log_block;
         // Lanes without a score store outside the buffer's range, which drops it: every tile has
         // as many stores, so that the next one's queries are not waited for behind them.
         const PartWriter tile(to);
         auto put = [&](int token, int t, float x, bool mine = true) {
-          const int b = t * 16 + r16, j = j0 + token;
-          const bool ok = whole || (j < n && b0 + b < blk1 && b0 + b <= (pos0 + j) >> a.log_block);
-          const uint32_t at = mine && ok ? (uint32_t)(token * step + b) * 4 : 0x80000000u;
+          const int from = t ? first[1] : first[0];
+          const bool ok = mine && (uint32_t)(j0 + token - from) < (uint32_t)(n - from);
+          const uint32_t at = ok ? (uint32_t)(token * step + t * 16 + r16) * 4 : 0x80000000u;
           __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), tile.rsrc, (int)at, 0, 0);
         };
         if constexpr (LOG_G == 0) {
