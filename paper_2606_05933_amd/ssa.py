@@ -994,6 +994,11 @@ def _header(plan_host, magic: int, what: str):
     return at, words
 
 
+# An empty tensor's address, which torch gives as 0: the library takes 0 for a buffer that
+# was left out.  Nothing is read or written there.
+_EMPTY = 4096
+
+
 class _Buffers:
     """Checks the buffers of one call, which have to be on the current device (the
     call's stream is one of it), and gives their addresses."""
@@ -1009,7 +1014,7 @@ class _Buffers:
             return None
         if (t.get_device() == self.device and t.is_contiguous() and t.element_size() == itemsize
                 and t.numel() >= numel):
-            return t.data_ptr()
+            return t.data_ptr() or _EMPTY
         if t.get_device() != self.device:
             raise ValueError(f"{name} must be a tensor on the current device")
         if not t.is_contiguous():

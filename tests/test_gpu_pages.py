@@ -146,6 +146,21 @@ def test_what_the_device_refuses_changes_nothing(torch_dev, what):
     assert (p.slots == -3).all() and (p.row_start == -3).all()
 
 
+def test_a_slot_map_without_room(torch_dev):
+    """Room for no row: growing requests are refused, and shrinking ones are not."""
+    rng = np.random.default_rng(2)
+    p = Pages(torch_dev, 2, 9, 4, rng, 0)
+    p.row_start.fill_(-3)
+    p.call([17, 0])
+    p.state = np.array([p.state[0], p.state[1], p.ssa.PAGES_ROWS, 0])
+    p.same()
+    assert (p.row_start == -3).all()
+    q = Pages(torch_dev, 2, 9, 4, rng, 40)
+    q.resize([17, 20])
+    q.slots = q.slots[:0]
+    q.resize([5, 20])
+
+
 FORMS = [("half", None), ("half", 32), ("half", 16), ("half", 48), ("interleaved", None),
          ("interleaved", 32), ("interleaved", 16)]
 

@@ -217,6 +217,60 @@ def test_pages_resize_refuses_before_it_launches():
     assert call(s=ssa.make_shape(8, 2, 64, 100, 20, 0.125, page_size=8)) == PAGE_SIZE
 
 
+@pytest.fixture
+def host_calls(monkeypatch):
+    """The binding's checks on host tensors: a list of what reaches the library, whose calls
+    launch nothing here."""
+    calls = []
+
+    class Buffers(ssa._Buffers):
+        __slots__ = ()
+
+        def __init__(self):
+            self.device = -1  # a host tensor's
+
+        def stream(self, stream):
+            return None
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *args: calls.append((name, args)) or 0
+
+    monkeypatch.setattr(ssa, "_Buffers", Buffers)
+    monkeypatch.setattr(ssa, "LIB", Lib())
+    return calls
+
+
+def test_an_empty_slot_map_is_not_one_left_out(host_calls):
+    """A slot map without room for a row: the library has to see that it is there, so that
+    new rows are refused and nothing changes."""
+    import torch
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    for slots, rows in ((None, 0), (torch.zeros(0, dtype=torch.int64), 0),
+                        (torch.zeros(7, dtype=torch.int64), 7)):
+        ssa.pages_resize(shape, ints(3), ints(3), ints(3, 20), ints(100), ints(4), ints(4), None,
+                         slots)
+        name, args = host_calls.pop()
+        assert name == "ssa_pages_resize" and args[8] is None and args[10] == rows
+        assert (args[9] is None) == (slots is None) and args[9] != 0
+
+
+def test_shifts_of_a_batch_without_requests(host_calls):
+    import torch
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    plan = np.zeros(256, np.uint8)
+    plan[:4].view(np.uint32)[0] = ssa._PLAN_MAGIC
+    none = torch.zeros(0, dtype=torch.int32)
+    pool = torch.zeros(100 * 2 * 16 * 64, dtype=torch.bfloat16)
+    rows = torch.zeros(0, dtype=torch.bfloat16)
+    dev = torch.from_numpy(plan)
+    ssa.rope_append_as(shape, plan, dev, rows, torch.zeros(1, 64), rows, pool, pool, none,
+                       shift_host=np.zeros(0, np.int32), shift_dev=none)
+    _, args = host_calls.pop()
+    assert args[7] and args[8], "both shift arrays are there, and empty"
+
+
 def test_rope_append_as_refuses_before_it_launches():
     shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
     plan, _ = ssa.ssa_plan(shape, [1, 3], [10, 20])
