@@ -615,6 +615,15 @@ def rope_cos_sin(max_position: int, d: int, base: float = 500000.0) -> np.ndarra
     return out
 
 
+def _table_positions(cos_sin, rotary: int) -> int:
+    """Positions of a rotary table [max_position, rotary] (flat ones are taken by their size).
+    A table of other rows would be read as one of more or fewer positions."""
+    n = cos_sin.numel()
+    if n % rotary or (cos_sin.dim() > 1 and n != cos_sin.shape[0] * rotary):
+        raise ValueError(f"cos_sin of shape {tuple(cos_sin.shape)} has not rows of {rotary}")
+    return n // rotary
+
+
 def rope_append(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_cache, v_cache,
                 block_table, stream=None):
     """ssa_rope_append: RoPE of the new queries and keys, and kv_append of the
@@ -629,7 +638,7 @@ def rope_append(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_cac
     _check_dev("k_cache", k_cache, pool, 2)
     _check_dev("v_cache", v_cache, pool, 2)
     _check_dev("block_table", block_table, n * shape.max_pages_per_req, 4)
-    max_pos = cos_sin.numel() // d
+    max_pos = _table_positions(cos_sin, d)
     vp = ctypes.c_void_p
     rc = LIB.ssa_rope_append(ctypes.byref(shape), vp(_ptr(plan_host)), vp(_ptr(plan_dev)),
                              vp(_ptr(qkv)), vp(_ptr(cos_sin)), int(max_pos), vp(_ptr(q_out)),
@@ -1162,7 +1171,7 @@ def rope_append_shifted(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, shif
     rc = LIB.ssa_rope_append_shifted(
         shape, at, check.plan(plan_dev, plan_host),
         check("qkv", qkv, tokens * (hq + 2 * hkv) * d, 2), check("cos_sin", cos_sin, d, 4),
-        cos_sin.numel() // d, _address(shift_host), check("shift_dev", shift_dev, n, 4),
+        _table_positions(cos_sin, d), _address(shift_host), check("shift_dev", shift_dev, n, 4),
         check("q_out", q_out, tokens * hq * d, 2), check("k_cache", k_cache, pool, 2),
         check("v_cache", v_cache, pool, 2),
         check("block_table", block_table, n * shape.max_pages_per_req, 4), check.stream(stream))
@@ -1266,7 +1275,7 @@ def rope_append_as(shape: SsaShape, plan_host, plan_dev, qkv, cos_sin, q_out, k_
     rc = LIB.ssa_rope_append_as(
         shape, at, check.plan(plan_dev, plan_host), form,
         check("qkv", qkv, tokens * (hq + 2 * hkv) * d, 2), check("cos_sin", cos_sin, rotary, 4),
-        cos_sin.numel() // rotary, _address(shift_host), check("shift_dev", shift_dev, n, 4),
+        _table_positions(cos_sin, rotary), _address(shift_host), check("shift_dev", shift_dev, n, 4),
         check("q_out", q_out, tokens * hq * d, 2), check("k_cache", k_cache, pool, 2),
         check("v_cache", v_cache, pool, 2),
         check("block_table", block_table, n * shape.max_pages_per_req, 4), check.stream(stream))

@@ -271,6 +271,40 @@ def test_shifts_of_a_batch_without_requests(host_calls):
     assert args[7] and args[8], "both shift arrays are there, and empty"
 
 
+def test_rotary_tables_of_other_rows(host_calls, monkeypatch):
+    """A table whose rows are not the rotated dims is refused; a flat one goes by its size."""
+    import torch
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    plan = np.zeros(256, np.uint8)
+    plan[:4].view(np.uint32)[0] = ssa._PLAN_MAGIC
+    bf = lambda n: torch.zeros(n, dtype=torch.bfloat16)  # noqa: E731
+    none, shift = torch.zeros(0, dtype=torch.int32), np.zeros(0, np.int32)
+    monkeypatch.setattr(ssa, "_check_dev", lambda *a: None)
+    monkeypatch.setattr(ssa, "_stream", lambda s: 0)
+
+    def positions(name, table, rotary):
+        args = [shape, plan, torch.from_numpy(plan), bf(0), table]
+        pools = [bf(0), bf(100 * 2 * 16 * 64), bf(100 * 2 * 16 * 64), none]
+        if name == "rope_append_as":
+            ssa.rope_append_as(*args, *pools, rotary_dim=rotary)
+        elif name == "rope_append_shifted":
+            ssa.rope_append_shifted(*args, shift, none, *pools)
+        else:
+            ssa.rope_append(*args, *pools)
+        got, args = host_calls.pop()
+        assert got == "ssa_" + name
+        return args[6 if name == "rope_append_as" else 5]
+
+    for name, rotary in (("rope_append_as", 32), ("rope_append_as", 64),
+                         ("rope_append_shifted", 64), ("rope_append", 64)):
+        for size in ((7, rotary), (7, 2, rotary // 2), (7 * rotary,), (1, rotary)):
+            assert positions(name, torch.zeros(size), rotary) == (1 if size[0] == 1 else 7)
+        for size in ((7, 2 * rotary), (14, rotary // 2), (7 * rotary + 1,), (4, rotary + 16)):
+            with pytest.raises(ValueError):
+                positions(name, torch.zeros(size), rotary)
+            assert not host_calls
+
+
 def test_rope_append_as_refuses_before_it_launches():
     shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
     plan, _ = ssa.ssa_plan(shape, [1, 3], [10, 20])
