@@ -993,10 +993,14 @@ def _header(plan_host, magic: int, what: str):
     try:  # a writable array: a third of the time
         words = _HeaderWords.from_buffer(plan_host)
         at = ctypes.addressof(words)
-    except (TypeError, ValueError, BufferError):
+    except ValueError:  # shorter than a header
+        raise SsaError(SSA_ERR_PLAN_MISMATCH, what) from None
+    except (TypeError, BufferError):
         at = _address(plan_host)
         if at is None:
-            raise SsaError(SSA_ERR_NULL, what)
+            raise SsaError(SSA_ERR_NULL, what) from None
+        if plan_host.nbytes < ctypes.sizeof(_HeaderWords):
+            raise SsaError(SSA_ERR_PLAN_MISMATCH, what) from None
         words = _HeaderWords.from_address(at)
     if words[0] != magic:
         raise SsaError(SSA_ERR_PLAN_MISMATCH, what)

@@ -256,6 +256,30 @@ def test_an_empty_slot_map_is_not_one_left_out(host_calls):
         assert (args[9] is None) == (slots is None) and args[9] != 0
 
 
+def test_a_buffer_shorter_than_a_header_is_no_plan():
+    """Refused by its size: its words would be read past its end (here from a plan that it is
+    the beginning of)."""
+    import torch
+    shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
+    assert min(ssa.sparse_plan(shape, [], [], 16, 4)[0].nbytes, ssa.ssa_plan(shape, [], [])[0].nbytes,
+               ssa.score_plan(shape, [], [])[0].nbytes,
+               ssa.evict_plan(shape, [], [], 0, 0)[0].nbytes) >= 128
+    plan, _, _ = ssa.sparse_plan(shape, [1], [20], 16, 4)
+    fixed = plan.copy()
+    fixed.flags.writeable = False
+    for p in (plan, fixed, torch.from_numpy(plan)):
+        at, words = ssa._header(p, ssa._SPARSE_MAGIC, "")
+        assert words[ssa._SPARSE_TOKENS] == 1 and at
+        for n in (0, 8, 127):
+            with pytest.raises(ssa.SsaError) as e:
+                ssa._header(p[:n], ssa._SPARSE_MAGIC, "")
+            assert e.value.code == MISMATCH
+        ssa._header(p[:128], ssa._SPARSE_MAGIC, "")
+    with pytest.raises(ssa.SsaError) as e:
+        ssa._header(None, ssa._SPARSE_MAGIC, "")
+    assert e.value.code == NULL
+
+
 def test_shifts_of_a_batch_without_requests(host_calls):
     import torch
     shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
