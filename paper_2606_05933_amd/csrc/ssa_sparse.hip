@@ -160,9 +160,11 @@ struct SparseArgs {
   float* records;
 };
 
+// Before any record is read: another plan may be a shorter one.  Both words are read before
+// either is looked at.
 __device__ __forceinline__ bool plan_ok(const SparseArgs& a) {
   const auto h = as_uniform<SparseHeader>(a.plan);
-  return h->magic == kSparseMagic && h->hash == a.hash;
+  return (h->magic == kSparseMagic) & (h->hash == a.hash);
 }
 
 // One row: `unit` counts kRowGroup rows of every chunk record, then the single ones.
@@ -173,11 +175,12 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
   const bool single = unit >= a.num_groups * kRowGroup;
   const int record = single ? a.num_groups + (unit - a.num_groups * kRowGroup) : unit / kRowGroup;
   const int j = single ? 0 : unit % kRowGroup;
+  if (!plan_ok(a)) return false;
   const auto x = as_uniform<SparseRows>(a.plan + a.off_rows) + record;
   r->req = x->req;
   r->row = x->row0 + j;
   r->pos = x->pos0 + j;
-  return plan_ok(a) && j < x->n;
+  return j < x->n;
 }
 
 // ---------------------------------------------------------------------------
@@ -561,8 +564,9 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
   const int j0 = single ? 0 : unit % a.subs * a.tokens;
   const auto record = as_uniform<SparseRows>(a.plan + a.off_rows) +
                       (single ? a.num_groups + (unit - a.num_groups * a.subs) : unit / a.subs);
+  if (!plan_ok(a)) return;
   const int rows = min(single ? 1 : a.tokens, record->n - j0);
-  if (!plan_ok(a) || rows <= 0) return;
+  if (rows <= 0) return;
   const int row0 = record->row0 + j0, pos0 = record->pos0 + j0, last = pos0 + rows - 1;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

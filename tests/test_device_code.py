@@ -113,3 +113,24 @@ def test_streamed_loads_keep_their_registers_until_they_land(kernels):
                     bad.append((name[1][:60], ins, use))
     assert loads >= 4 * 3 * 4
     assert not bad, (len(bad), bad[:3])
+
+
+def test_a_sparse_plan_is_checked_before_its_records_are_read(kernels):
+    """Another plan than the host's may be a shorter one: until its magic and hash have been
+    compared, a kernel reads its own arguments and the plan's header alone."""
+    seen = 0
+    for name, code in kernels.items():
+        text = [ins for _, ins in code]
+        at = [i for i, t in enumerate(text) if re.match(r"s_cmp_\w+ s\d+, 0x31505353", t)]
+        if not at:
+            continue
+        seen += 1
+        magic = re.match(r"s_cmp_\w+ (s\d+),", text[at[0]]).group(1)
+        end = next(i for i in range(at[0], len(text)) if re.match(r"s_cmp_\w+_u64", text[i]))
+        loads = [m.groups() for m in (re.match(r"s_load_\w+ (\S+), (s\[\d+:\d+\]), (\S+)", t)
+                                      for t in text[:end]) if m]
+        header = [base for to, base, _ in loads if to == magic][-1]
+        bad = [x for x in loads if x[1] not in (loads[0][1], header)]
+        assert not bad, (name[1], bad)
+        assert not any(t.startswith(("global_load", "buffer_load", "flat_load")) for t in text[:end])
+    assert seen >= 19, seen

@@ -404,6 +404,35 @@ def test_calls_on_two_streams(torch_dev):
             assert not x.ws[:4096].any()
 
 
+@pytest.mark.parametrize("what", ["stale", "other", "short"])
+def test_another_plan_on_the_device_writes_nothing(torch_dev, what):
+    """A plan of the batch before, of other rows, or a shorter one at plan_dev."""
+    torch = torch_dev
+    x = Sparse(torch, (16, 2, 64), (20, 1, 1), (700, 300, 40), 32, 12, 1, 1, seed=12)
+    assert x.ws.numel() > 4096
+    x.whole_summary()
+    before = bits(x.summary)
+    plans = []
+    for mine, make in ((x.plan, lambda c, u: x.ssa.sparse_plan(x.shape, c, u, 32, 12, 1, 1)[0]),
+                       (x.batch_plan, lambda c, u: x.ssa.ssa_plan(x.shape, c, u)[0])):
+        if what == "stale":
+            other = mine.copy()
+            other[8] ^= 1  # its hash
+        else:
+            other = make(*(((20, 1, 1), (699, 300, 40)) if what == "other" else ((1,), (3,))))
+        # what lies behind a shorter one is no record
+        buf = np.full(mine.nbytes, 0xFF, np.uint8)
+        buf[:min(len(other), len(buf))] = other[:len(buf)]
+        plans.append(dev(torch, buf))
+    x.plan_dev, x.batch_dev = plans
+    for f in (x.summarise, x.score, x.select, x.attend):
+        f()
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(x.summary), before)
+    assert (x.scores == -7.0).all() and (x.blocks == -9).all() and (x.out == 3.0).all()
+    assert not x.ws[:4096].any() and (x.ws[4096:] == 0xFF).all()
+
+
 def test_replayed_graph(torch_dev):
     """All calls in one graph, replayed with eager work of the same workspace between."""
     torch = torch_dev
