@@ -17,6 +17,7 @@ import numpy as np
 import pytest
 
 from test_gpu_evict import HEADS, dev, say
+from test_sparse_boundary import LARGE_SCORES, parse
 
 pytestmark = pytest.mark.gpu
 
@@ -199,6 +200,50 @@ def test_scores_bound_every_logit(torch_dev):
                 assert logits.max() <= got[row, h, n] + 2 * 256 * 2.0 ** -24 * size
 
 
+@pytest.mark.parametrize("heads,c,u,block,tiles,span", LARGE_SCORES)
+def test_scores_of_large_batches(torch_dev, heads, c, u, block, tiles, span):
+    """Only the plan, queries, summaries and scores.  Requests share pages, and the pages in which
+    no block begins hold NaN."""
+    from oracle import sparse
+    from paper_2606_05933_amd import ssa, workload
+    torch = torch_dev
+    hq, hkv, d = heads
+    g, c, u = hq // hkv, np.array(c), np.array(u)
+    say(f"[gpu sparse scores] {heads} c={c[:4]} u={u[:4]} block={block}")
+    width, pool = int(-(-(c + u).max() // 16)), 600
+    shape = ssa.make_shape(hq, hkv, d, 2 * pool, width, 0.1)
+    plan, _, stride = ssa.sparse_plan(shape, c, u, block, 8)
+    head, _, items = parse(plan)
+    assert head["tiles"] == tiles and max(items["blk1"] - items["blk0"]) == span
+    rng = np.random.default_rng(block + hq)
+    table = rng.integers(pool, 2 * pool, (len(c), width))
+    table[:, ::block // 16] = rng.integers(0, pool, table[:, ::block // 16].shape)
+    T = int(c.sum())
+    q = workload.normal_bf16((T, hq, d), 1)
+    summary = np.full((2 * pool, hkv, 2, d), 0x7FC0, np.uint16)
+    summary[:pool] = workload.normal_bf16((pool, hkv, 2, d), 2)
+    scores = torch.full((T + 1, hkv, stride), -7.0, device="cuda")
+    ssa.block_scores(shape, plan, dev(torch, plan), dev(torch, q), dev(torch, summary),
+                     dev(torch, table.astype(np.int32)), scores)
+    got = scores.cpu().numpy()
+    assert (got[-1] == -7.0).all()
+    row = 0
+    for i in range(len(c)):
+        rows, n = slice(row, row + c[i]), -(-(c[i] + u[i]) // block)
+        seen = np.arange(n) <= (u[i] + np.arange(c[i]))[:, None] // block
+        at = table[i, np.arange(n) * (block // 16)]
+        for h in range(hkv):
+            x = sparse._f64(q[rows, h * g:(h + 1) * g]).reshape(-1, d)
+            high, low = (np.ascontiguousarray(sparse._f64(summary[at, h, j]).T) for j in range(2))
+            over = lambda y: y.reshape(c[i], g, n).max(axis=1)  # noqa: E731
+            up, down = np.maximum(x, 0), np.minimum(x, 0)
+            ref, size = over(up @ high + down @ low), over(up @ np.abs(high) - down @ np.abs(low))
+            err = np.abs(got[rows, h, :n] - ref)
+            assert (err <= 2 * d * 2.0 ** -24 * size)[seen].all(), (i, h, err[seen].max())
+            assert (got[rows, h, :n][~seen] == -7.0).all() and (got[rows, h, n:] == -7.0).all()
+        row += c[i]
+
+
 @pytest.mark.parametrize("heads", [(4, 4, 64), (4, 2, 128), (6, 2, 64), (8, 2, 64), (28, 4, 128),
                                    (16, 1, 64), (13, 1, 128)])
 def test_scores_of_queries_that_are_no_numbers(torch_dev, heads):
@@ -271,6 +316,48 @@ def test_selection(torch_dev, heads, c, u, block, kind, top, sink, recent):
                 ref = sparse.select(s[row, h, :(u[i] + j) // block + 1], top, sink, recent)
                 assert np.array_equal(got[row, h], ref), (i, j, h)
             row += 1
+
+
+def stable_select(score, top, sink, recent):
+    """oracle.sparse.select of a list of more than `top` blocks, by one stable sort."""
+    n = len(score)
+    x = np.where(np.isnan(score), np.inf, score.astype(np.float64))[sink:n - recent]
+    most = np.argsort(-x, kind="stable")[:top - sink - recent] + sink
+    return np.sort(np.concatenate([np.arange(sink), most, np.arange(n - recent, n)]))
+
+
+@pytest.mark.parametrize("hkv,c,most", [(8, 130, 700), (8, 130, 1024), (8, 130, 1025), (16, 67, 2048),
+                                        (8, 130, 2049), (2, 3, 700)])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd", "narrow"])
+@pytest.mark.parametrize("top,sink,recent", [(1, 0, 1), (64, 3, 1), (100, 50, 50), (513, 0, 2)])
+def test_selection_of_many_lists(torch_dev, hkv, c, most, kind, top, sink, recent):
+    """1024 lists and more, which one wave each takes up to 2048 blocks; and few of 700."""
+    from oracle import sparse
+    from paper_2606_05933_amd import ssa
+    torch = torch_dev
+    u = most * 16 - c
+    say(f"[gpu sparse select] {hkv} heads, {c} rows, {most} blocks {kind} top={top}")
+    shape = ssa.make_shape(hkv, hkv, 64, 1 << 20, 40000, 0.1)
+    plan, _, stride = ssa.sparse_plan(shape, (c, 1), (u, 9), 16, top, sink, recent)
+    rng = np.random.default_rng(top + most)
+    size = (c + 1, hkv, stride)
+    s = {"spread": lambda: rng.lognormal(0, 3, size) * rng.choice([-1, 1], size),
+         "ties": lambda: rng.integers(0, 3, size).astype(np.float64),
+         "odd": lambda: rng.choice([np.nan, -np.nan, np.inf, -np.inf, 0.0, -0.0, 1.0, -1e-40, 3e38], size),
+         "narrow": lambda: 1.0 + rng.integers(0, 2000, size) * 2.0 ** -23}[kind]().astype(np.float32)
+    blocks = torch.full((c + 2, hkv, top), -9, dtype=torch.int32, device="cuda")
+    ssa.block_select(shape, plan, dev(torch, plan), dev(torch, s), blocks)
+    got = blocks.cpu().numpy()
+    assert (got[-1] == -9).all()
+    for j in range(c):
+        n = (u + j) // 16 + 1
+        for h in range(hkv):
+            ref = stable_select(s[j, h, :n], top, sink, recent)
+            assert np.array_equal(got[j, h], ref), (j, h)
+    for h in range(hkv):  # the oracle's own word for some of them
+        assert np.array_equal(got[h % c, h], sparse.select(s[h % c, h, :(u + h % c) // 16 + 1], top, sink,
+                                                           recent))
+        assert np.array_equal(got[c, h], sparse.select(s[c, h, :1], top, sink, recent))
 
 
 def random_lists(rng, x):
@@ -559,6 +646,146 @@ def test_logits_of_minus_infinity(torch_dev):
     x.attend()
     got = x.out[:-1].float().cpu().numpy().reshape(3, 2, 2, 64)
     assert np.isnan(got[1:, 0]).all() and np.isfinite(got[0, 0]).all() and (got[:, 1] == 0).all()
+
+
+def test_a_long_chunk(torch_dev):
+    """A chunk of more than 512 rows on a context of ten times its lists, by its own scores."""
+    x = Sparse(torch_dev, (8, 2, 128), (530, 1), (7000, 300), 32, 20, 1, 2, seed=17)
+    whole = x.whole_summary()
+    x.score()
+    x.check_scores(whole)
+    x.select()
+    x.check_lists()
+    x.attend()
+    x.check_out()
+
+
+def cut_decode(torch):
+    """One decode row of two kv heads, and its list of 32 blocks, cut into pieces of four."""
+    x = Sparse(torch, (4, 2, 64), (1,), (4000,), 64, 32, seed=13)
+    x.b.q[:, :, 0] = 0x3F80  # 1
+    h = parse(x.plan)[0]
+    assert (h["nsplit"], h["entries"]) == (8, 4) and x.ws.numel() > 4096
+    lists = np.random.default_rng(4).permutation(62)[:32].astype(np.int32)
+    x.blocks.copy_(dev(torch, np.tile(lists, (1, 2, 1))))
+    return x, lists
+
+
+def cut_bar(x, lists):
+    """Oracle of the caches as they are over `lists` (as x's, or fewer), and its bar."""
+    from oracle import sparse
+    ref, mass, a = sparse.attention(x.b, x.kc, x.vc, lists, x.block)
+    rel = 2.0 ** -24 * (2 * (2 * 64 * a + 8 * a + 2 * x.top * x.block / 32 + 256) + 1)
+    return ref[0].reshape(2, 2, 64), (2.0 ** -8 * np.abs(ref) + rel * mass)[0].reshape(2, 2, 64)
+
+
+def cut_out(x):
+    x.upload()
+    x.attend()
+    assert not x.ws[:4096].any(), "tickets are left"
+    return x.out[0].float().cpu().numpy().astype(np.float64).reshape(2, 2, 64)
+
+
+def test_pieces_of_minus_infinity(torch_dev):
+    """Pieces of a cut list whose keys' logits are all -infinity: they weigh nothing beside others;
+    all of them together are NaN; and beside pieces without a key they are too."""
+    torch = torch_dev
+    for dead in (range(4), range(28, 32), range(4, 32), [*range(8), 9, 17, 30]):
+        x, lists = cut_decode(torch)
+        left = np.tile(np.delete(lists, list(dead)), (1, 2, 1))
+        left[0, 1] = lists[:left.shape[2]]  # kv head 1 is as it was
+        ref, bar = cut_bar(x, left)
+        ref[1], bar[1] = (y[1] for y in cut_bar(x, np.tile(lists, (1, 2, 1))))
+        for b in lists[list(dead)]:
+            x.kc[x.b.block_table[0, b * 4:b * 4 + 4], 0, :, 0] = 0xFF80
+        got = cut_out(x)
+        assert (np.abs(got - ref) <= bar).all(), list(dead)
+    x, lists = cut_decode(torch)
+    ref, bar = cut_bar(x, np.tile(lists, (1, 2, 1)))
+    x.kc[:, 0, :, 0] = 0xFF80
+    got = cut_out(x)
+    assert np.isnan(got[0]).all() and (np.abs(got - ref) <= bar)[1].all()
+    # one piece of them, the others without a key; kv head 1 without any
+    x.blocks.fill_(-1)
+    x.blocks[0, 0, 13] = int(lists[0])
+    got = cut_out(x)
+    assert np.isnan(got[0]).all() and (got[1] == 0).all()
+
+
+def test_pieces_of_values_that_are_no_numbers(torch_dev):
+    """One piece of a cut list goes key by key, the others do not."""
+    torch = torch_dev
+    for at in (0, 14, 31):
+        x, lists = cut_decode(torch)
+        ref, bar = cut_bar(x, np.tile(lists, (1, 2, 1)))
+        page = x.b.block_table[0, lists[at] * 4]
+        x.vc[page, 1, 7, 3] = 0x7F80
+        x.vc[page, 1, 9, 5] = 0x7FC0
+        got = cut_out(x)
+        assert (got[1, :, 7] == np.inf).all() and np.isnan(got[1, :, 9]).all()
+        ref[1, :, [7, 9]] = got[1, :, [7, 9]] = 0
+        assert (np.abs(got - ref) <= bar).all(), at
+        # a key that is no number, of the other kv head
+        x.kc[page, 0, 2, 11] = 0x7FC0
+        got = cut_out(x)
+        assert np.isnan(got[0]).all()
+        got[1, :, [7, 9]] = 0
+        assert (np.abs(got - ref) <= bar)[1].all(), at
+    # an infinite value of a key that weighs nothing: 0 times infinity
+    x, lists = cut_decode(torch)
+    page = x.b.block_table[0, lists[20] * 4]
+    x.kc[page, 0, 4, 0] = 0xFF80
+    x.vc[page, 0, 30, 4] = 0xFF80
+    got = cut_out(x)
+    assert np.isnan(got[0, :, 30]).all()
+    got[0, :, 30] = 0
+    assert np.isfinite(got).all()
+
+
+def test_an_infinite_value_behind_the_first_pass(torch_dev):
+    """Workgroups of more than 512 pages: the sums of all their passes are made anew, key by key."""
+    from oracle import sparse
+    torch = torch_dev
+    rng = np.random.default_rng(18)
+    x = Sparse(torch, (64, 64, 64), (128,), (9000,), 16, 100, seed=26)
+    assert x.ws.numel() == 4096, "the lists are cut"
+    # even rows name block 3, of the first pass, odd ones block 560, of the second
+    others = np.delete(np.arange(563), [3, 560])
+    lists = others[np.argsort(rng.random((128, 64, 561)), axis=2)[:, :, :100]]
+    lists[0::2, :, 40], lists[1::2, :, 40] = 3, 560
+    lists = np.sort(lists, axis=2).astype(np.int32)
+    for h in (5, 6):
+        for at in range(0, 128, 16):
+            union = np.unique(lists[at:at + 16, h])
+            assert list(union).index(3) < 512 <= list(union).index(560)
+    x.blocks.copy_(dev(torch, lists))
+    ref, mass, a = sparse.attention(x.b, x.kc, x.vc, lists, 16)
+    rel = 2.0 ** -24 * (2 * (2 * 64 * a + 8 * a + 2 * 1600 / 32 + 256) + 1)
+    bar = 2.0 ** -8 * np.abs(ref) + rel * mass
+    for block, slot, h, d in ((3, 1, 5, 2), (560, 9, 6, 60)):
+        x.vc[x.b.block_table[0, block], h, d, slot] = 0x7F80
+    x.upload()
+    x.attend()
+    got = x.out[:-1].float().cpu().numpy().astype(np.float64)
+    for first, h, d in ((0, 5, 2), (1, 6, 60)):
+        assert (got[first::2, h, d] == np.inf).all()
+        got[first::2, h, d] = ref[first::2, h, d]
+    assert (np.abs(got - ref) <= bar).all()
+    # one row that goes by its list, in pieces of eight passes: a key of the second pass
+    x = Sparse(torch, (4, 2, 64), (1,), (20000,), 128, 32768, seed=27)
+    lists = np.full((1, 2, 32768), -1, np.int32)
+    lists[0, :, :150] = rng.permutation(156)[:150]
+    x.blocks.copy_(dev(torch, lists))
+    ref, mass, a = sparse.attention(x.b, x.kc, x.vc, lists, 128)
+    rel = 2.0 ** -24 * (2 * (2 * 64 * a + 8 * a + 2 * 512 * 128 / 32 + 256) + 1)
+    bar = 2.0 ** -8 * np.abs(ref) + rel * mass
+    x.vc[x.b.block_table[0, lists[0, 1, 100] * 8 + 5], 1, 33, 2] = 0xFF80
+    x.upload()
+    x.attend()
+    got = x.out[:-1].float().cpu().numpy().astype(np.float64)
+    assert (got[0, 2:, 33] == -np.inf).all()
+    got[0, 2:, 33] = ref[0, 2:, 33]
+    assert (np.abs(got - ref) <= bar).all()
 
 
 def test_far_offsets(torch_dev):

@@ -89,6 +89,35 @@ def test_plans_cover_every_row_and_block_once(seed):
         assert ws == 4096
 
 
+# Batches whose score items hold more than four tiles of queries or more than one pass of 128
+# blocks: heads, new tokens, cached ones, block, tiles of a chunk's item, blocks of a decode's.
+LARGE_SCORES = [
+    ((32, 8, 128), (550, 37, 1), (30000, 500, 4000), 32, 16, 128),
+    ((8, 8, 64), (603, 1), (29990, 30), 16, 8, 128),
+    ((28, 4, 128), (597, 1, 1), (30001, 16, 900), 32, 16, 128),
+    ((8, 4, 128), (1030, 2), (33000, 100), 32, 8, 128),
+    ((16, 1, 64), (611,), (30000,), 16, 16, 128),
+    ((64, 8, 128), (1,) * 64, tuple(28000 + 31 * i for i in range(64)), 16, 16, 384),
+    ((64, 8, 128), (1,) * 40 + (530,), tuple(20000 + 777 * i for i in range(40)) + (31000,), 16, 16, 256),
+]
+
+
+@pytest.mark.parametrize("heads,c,u,block,tiles,span", LARGE_SCORES)
+def test_large_score_items_cover_every_row_and_block_once(heads, c, u, block, tiles, span):
+    c, u = np.array(c), np.array(u)
+    h, _, scores = parse(ssa.sparse_plan(shape_of(*heads, c + u), c, u, block, 8)[0])
+    assert h["tiles"] == tiles and max(scores["blk1"] - scores["blk0"]) == span
+    start = np.cumsum(c) - c
+    for i in range(len(c)):
+        covered = np.zeros((int(u[i] + c[i] - 1) // block + 1, c[i]), int)
+        for s in scores[scores["req"] == i]:
+            j = s["row0"] - start[i]
+            assert 0 <= j and j + s["n"] <= c[i] and s["pos0"] == u[i] + j
+            covered[s["blk0"]:s["blk1"], j:j + s["n"]] += 1
+        seen = np.arange(len(covered))[:, None] <= (u[i] + np.arange(c[i])) // block
+        assert (covered[seen] == 1).all() and covered.max() == 1
+
+
 def test_sparse_plan_refusals():
     shape = ssa.make_shape(8, 2, 64, 100, 20, 0.125)
 
