@@ -167,6 +167,17 @@ __device__ __forceinline__ bool plan_ok(const SparseArgs& a) {
   return (h->magic == kSparseMagic) & (h->hash == a.hash);
 }
 
+// A record's fields in one load.  (Left alone, the row count is loaded, waited for and branched
+// on before the rest.)
+struct Rows {
+  int req, row0, pos0, n;
+  __device__ __forceinline__ Rows(const SparseArgs& a, int record) {
+    const auto x = as_uniform<SparseRows>(a.plan + a.off_rows) + record;
+    req = x->req, row0 = x->row0, pos0 = x->pos0, n = x->n;
+    asm volatile("" ::"s"(req), "s"(row0), "s"(pos0), "s"(n));
+  }
+};
+
 // One row: `unit` counts kRowGroup rows of every chunk record, then the single ones.
 struct Row {
   int req, row, pos;
@@ -176,11 +187,11 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
   const int record = single ? a.num_groups + (unit - a.num_groups * kRowGroup) : unit / kRowGroup;
   const int j = single ? 0 : unit % kRowGroup;
   if (!plan_ok(a)) return false;
-  const auto x = as_uniform<SparseRows>(a.plan + a.off_rows) + record;
-  r->req = x->req;
-  r->row = x->row0 + j;
-  r->pos = x->pos0 + j;
-  return j < x->n;
+  const Rows x(a, record);
+  r->req = x.req;
+  r->row = x.row0 + j;
+  r->pos = x.pos0 + j;
+  return j < x.n;
 }
 
 // ---------------------------------------------------------------------------
@@ -562,16 +573,15 @@ __global__ __launch_bounds__(kSparseThreads, 2) void sparse_attention_kernel(Spa
   // the rows: `rows` of them from token row row0, position pos0 on
   const bool single = unit >= a.num_groups * a.subs;
   const int j0 = single ? 0 : unit % a.subs * a.tokens;
-  const auto record = as_uniform<SparseRows>(a.plan + a.off_rows) +
-                      (single ? a.num_groups + (unit - a.num_groups * a.subs) : unit / a.subs);
   if (!plan_ok(a)) return;
-  const int rows = min(single ? 1 : a.tokens, record->n - j0);
+  const Rows record(a, single ? a.num_groups + (unit - a.num_groups * a.subs) : unit / a.subs);
+  const int rows = min(single ? 1 : a.tokens, record.n - j0);
   if (rows <= 0) return;
-  const int row0 = record->row0 + j0, pos0 = record->pos0 + j0, last = pos0 + rows - 1;
+  const int row0 = record.row0 + j0, pos0 = record.pos0 + j0, last = pos0 + rows - 1;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int columns = rows * a.g;
-  const int32_t* const table = a.bt + (size_t)record->req * a.maxp;
+  const int32_t* const table = a.bt + (size_t)record.req * a.maxp;
   const int log_pages = a.log_block - 4;
   auto token_of = [&](int column) { return (column * a.g_magic) >> 16; };
   auto list_of = [&](int t) { return a.blocks_in + ((size_t)(row0 + t) * a.hkv + kvh) * a.top; };
