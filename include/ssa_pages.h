@@ -7,6 +7,9 @@
  *               last entry again from the first
  *   state       int32 [4]: head, count, the status of the call that wrote it, and how
  *               many pages that call was short of
+ * A page belongs to one request: the ring knows no sharing.  If two requests' rows named the
+ * same page (a common prefix), each that shrank past it would give it back, and it would be
+ * handed out twice later: a request must not shrink past a page that another one holds.
  * A program starts with all pages free: free_pages = 0 .. num_pages - 1, state =
  * {0, num_pages, 0, 0}.
  */
