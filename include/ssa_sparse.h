@@ -22,7 +22,8 @@
  *   blocks   int32 [T, Hkv, top_blocks]: block indexes, -1 for none
  * Plans are blobs as in ssa.h: filled on the host, read by the kernels through
  * plan_dev (a device copy, or the pinned host buffer itself).  A kernel that finds
- * another plan at plan_dev than the host checked writes nothing.
+ * another plan at plan_dev than the host checked reads its header alone and writes
+ * nothing.
  * Pointers to queries, pools, summaries, scores, outputs and workspaces are 16-byte
  * aligned, plan_dev is 8-byte aligned.
  * Results do not depend on the order in which workgroups run.  All calls can be

@@ -206,8 +206,10 @@ __device__ __forceinline__ bool take_row(const SparseArgs& a, int unit, Row* r) 
 // looked at, and which blocks a row sees is one comparison a store (with reads before each
 // product and the rows' conditions apart 23.8 us beside 16 decodes, 21.5 so).  What is left
 // there is the way to the first products, 6 us of plan, table and summaries, then queries, products
-// and stores, none of which alone is half of it; a decode's scores wait for memory (64 rows of
-// 8000 to 30000 keys in blocks of 16: 273 MB in 48 us, 5.7 TB/s).
+// and stores, none of which alone is half of it.  Every four tiles begin with a wait for all that
+// is on its way, stores included: the loop over the tiles has a count that the compiler does not
+// know, so it cannot tell the queries' loads from the stores behind them.  A decode's scores wait
+// for memory (64 rows of 8000 to 30000 keys in blocks of 16: 273 MB in 48 us, 5.7 TB/s).
 template <int D, int LOG_G>  // heads of a group: more than 2^(LOG_G - 1), up to 2^LOG_G
 __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseArgs a) {
   constexpr int KS = D / 32, TOKENS = 16 >> LOG_G;  // tokens of a tile
@@ -298,8 +300,8 @@ __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseA
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 2; ++t) x[t] += y[t];
-        // Lanes without a score store outside the buffer's range, which drops it: every tile has
-        // as many stores, so that the next one's queries are not waited for behind them.
+        // Lanes without a score store outside the buffer's range, which drops it: no branch
+        // stands between a tile's stores and the next tile's products.
         const PartWriter tile(to);
         auto put = [&](int token, int t, float x, bool mine = true) {
           const int from = t ? first[1] : first[0];
@@ -346,8 +348,12 @@ __global__ __launch_bounds__(kSparseThreads, 3) void block_scores_kernel(SparseA
 // a count of the lanes' mask per register, and it ends once the candidate parts as many as
 // stay (some 12 to 18 counts of spread scores).  Lists in several waves meet at a barrier for
 // every count, so one wave takes a list where there are lists for every compute unit (4224 of
-// 1040 blocks: 30 us in four waves each, 16 so, 5 of them vector issue); 256 lists of 512 blocks
-// take 5.8 us, the launch, the plan, the scores and the search one after another.
+// 1040 blocks: 30 us in four waves each, 16 so, 5 of them vector issue).  A wave holds 2048 blocks
+// at most, and the longest request decides for all rows of the batch: beside one of 2063 blocks
+// the same lists take 78 us in sixteen waves each, beside one of 2032 18.  The loads go as the
+// counts do, four registers at a time: four scores are waited for before the next four are asked
+// for, so that a list of 1040 blocks is five trips to memory, one of 512 two.  256 lists of 512
+// blocks take 5.8 us, the launch, the plan, the scores and the search one after another.
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
                                         __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
@@ -519,9 +525,13 @@ struct PartReader {
 // with the values (dim-major pages) next.  Keys and values go from memory to registers, a step
 // ahead; the steps' loads are what bounds it, and the registers for them leave two waves a SIMD
 // (three waves had to spill, and were slower).  64/8 heads of 128, lists of 64 blocks of 64 keys:
-//   32 decode rows     105 us  537 MB from memory, 5.1 TB/s (96 rows 5.9)
-//   128 rows of a chunk 89 us  151 with a workgroup a row (2.1 GB through the caches at 14 TB/s),
+//   32 decode rows     105 us  538 MB from memory, 5.1 TB/s (96 rows 5.9)
+//   128 rows of a chunk 87 us  151 with a workgroup a row (2.1 GB through the caches at 14 TB/s),
 //                              110 with 16 columns a workgroup, 144 with two waves for each 16
+//   512 and 2048 rows   280 and 1070 us: it grows with the rows, as every four of them read their
+//                              own union (59 and 235 us of products at the library's rate)
+// Where rows of one workgroup see more than kMaskBlocks blocks there is no union, and it goes row by
+// row: 128 rows, 32/8 heads, 256 blocks of 16, on 130800 keys 81 us, on 131072 224.
 // One row of 2048 keys, 11 us, is launch, plan, list, table, keys, join and the pieces' join.
 constexpr int kPassPages = 512;     // pages in LDS at a time
 constexpr int kMaskBlocks = 8192;   // blocks of a union, 16 bits each
@@ -1305,8 +1315,8 @@ int ssa_block_select(const ssa_shape* shape, const void* plan_host, const void* 
   a.workgroups = rows_of(h) * h->hkv;
   a.scores_in = scores;
   a.blocks = blocks;
-  // the longest list's waves and registers: one wave where the lists fill the chip, several
-  // where there are few
+  // the longest list's waves and registers: up to 2048 blocks one wave where the lists fill the
+  // chip, several where there are few; past that sixteen, however many lists there are
   const bool many = (int64_t)h->num_tokens * h->hkv >= 1024;
   const int32_t most = h->most_blocks;
   if (most <= 512) return launch(block_select_kernel<1, 8>, a, 64, stream);
